@@ -254,6 +254,117 @@ int qtale_graph_capture_stack(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const 
 int qtale_graph_launch(qtale_graph* graph, void* stream);
 void qtale_graph_destroy(qtale_graph* graph);
 
+/* ---- paged K/V cache -------------------------------------------------------------------------------------
+ * A layer's cache holds the tokens that executed it, so its length differs from layer to layer and only the device knows it.  Instead of
+ * `cap` entries per layer and sequence, a paged cache takes pages of page_size tokens from one pool as they are needed; sequences that begin
+ * alike share them.
+ *   page    keys and values of page_size consecutive tokens of one slot: [n_kv_heads][page_size][head_dim] each, fp16 or bf16
+ *   slot    the cache of one sequence; 0 .. n_slots - 1, the same number in every layer
+ *   table   page of every page_size tokens of a slot, per layer; -1 = none: its tokens are not seen by attention, and not stored by an append
+ * The caller allocates all arrays; qtale_pages_init makes an empty cache of them.  Invariants that the calls keep: page_refs[p] is the number
+ * of table entries that name p, bit p is set in free_bits iff it is 0, and entries from kv_cap / page_size on are -1.
+ * Calls on slots: `slots` [B] int32 device, the slot of each sequence of the call, all different (nullable: sequence b is slot b); a number
+ * out of range is skipped.  The calls only enqueue kernels (no synchronisation, no allocation; they can be captured into a graph), and
+ * every result, page numbers included, depends on the state and the arguments alone. */
+typedef struct {
+    void* k_pages;          /* [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned */
+    void* v_pages;
+    int32_t* page_refs;     /* [n_pages] table entries that name the page */
+    uint32_t* free_bits;    /* [ceil(n_pages / 32)] bit p % 32 of word p / 32: page p is free */
+    int32_t* table;         /* [n_layers][n_slots][max_pages] */
+    int32_t* kv_len;        /* [n_layers][n_slots] tokens in the slot */
+    int32_t* kv_cap;        /* [n_layers][n_slots] tokens that the slot's pages have room for */
+    int n_pages;
+    int page_size;          /* 16, 32, 64, ..., 1024 */
+    int n_kv_heads, head_dim;   /* head_dim 64 or 128 */
+    int n_layers, n_slots, max_pages;
+    int dtype;              /* QTALE_ACT_FP16 | QTALE_ACT_BF16, of keys and values (and of the queries and outputs of the calls on them) */
+} qtale_paged_kv;
+
+/* All pages free, all slots empty. */
+int qtale_pages_init(const qtale_paged_kv* kv, void* stream);
+
+/* Scratch of qtale_pages_reserve (at most max_seqs sequences) and qtale_pages_compact (0 sequences); 0 for invalid arguments. */
+size_t qtale_pages_workspace_bytes(const qtale_paged_kv* kv, int max_seqs);
+
+/* Slot dst[i] becomes a copy of slot src[i] in every layer (i < n): it shares the pages that hold tokens.  dst[i] has to be empty (released), a
+ * slot that is not is left alone; no slot may be a target twice, or a target and a source. */
+int qtale_pages_fork(const qtale_paged_kv* kv, const int32_t* src, const int32_t* dst, int n, void* stream);
+
+/* Makes room for the new tokens of a call: seq_offsets[b+1] - seq_offsets[b] for sequence b (seq_offsets [B+1] int32 device), in one layer or
+ * in all (layer = -1).  Pages are taken lowest number first, in the order of layers, then sequences, then places.  A slot that will write into
+ * a page it shares (its last, partly filled) first gets a copy of it, unless it is the page's last holder by then: of several in one call the
+ * earlier ones take copies.
+ *   first     nullable: only make room.  Otherwise the slots' lengths are advanced as well and first [layers of the call][B] receives the
+ *             lengths before: token i of sequence b is entry first[b] + i of its slot, for qtale_paged_rope_append and qtale_paged_attention
+ *   missing   nullable [1] out: pages that the pool could not give.  A slot that got fewer than it needs holds as many of the new tokens as
+ *             fit (the first ones); the others are dropped by the append, and its length stops there.  Likewise at max_pages * page_size.
+ *   workspace qtale_pages_workspace_bytes(kv, B) bytes, 256-byte aligned; B <= 2048 */
+int qtale_pages_reserve(const qtale_paged_kv* kv, int layer, const int32_t* seq_offsets, const int32_t* slots, int B, int32_t* first,
+                        int32_t* missing, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Empties n slots in every layer; pages that nobody else holds are free again. */
+int qtale_pages_release(const qtale_paged_kv* kv, const int32_t* slots, int n, void* stream);
+
+/* Lets go of the pages of n slots that attention with this window (>= 1) and these first tokens (sinks >= 0) no longer reaches, seen from each
+ * slot's next token: those whose tokens all lie before the window and after the first `sinks`.  Lengths and room stay. */
+int qtale_pages_trim(const qtale_paged_kv* kv, const int32_t* slots, int n, int window, int sinks, void* stream);
+
+/* Moves the pages in use to the front of the pool, 0 .. n_live - 1 (nullable [1] out): the k-th page in use from n_live on, by number, goes to
+ * the k-th free one below it.  What lies in pages from n_live on is then unused (the pool can shrink, or be saved as one block). */
+int qtale_pages_compact(const qtale_paged_kv* kv, int32_t* n_live, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies the contents of pages src[i] of one pool to pages dst[i] of another (or of the same, if no page is written that is also read or
+ * written by another i); counts and tables are not touched.  Both of one page shape and type. */
+int qtale_pages_copy(const qtale_paged_kv* from, const qtale_paged_kv* to, const int32_t* src, const int32_t* dst, int n, void* stream);
+
+/* Rotary embedding: pair i < rotary_dim / 2 of a head turns by position * freqs[i]; columns from rotary_dim on stay as they are. */
+enum { QTALE_ROPE_HALF = 0, QTALE_ROPE_INTERLEAVED = 1 };   /* pairs (i, i + rotary_dim / 2) or (2 i, 2 i + 1) */
+enum {                        /* frequencies w_i = base^(-2 i / rotary_dim), and how a longer context stretches them by `factor` */
+    QTALE_ROPE_PLAIN = 0,
+    QTALE_ROPE_LINEAR = 1,    /* w_i / factor */
+    QTALE_ROPE_BASE = 2,      /* base * factor^(r / (r - 2)) for base: the slowest pair is stretched by factor, the fastest not at all */
+    QTALE_ROPE_BANDS = 3,     /* pairs that make more than `high` turns over original_len tokens stay, fewer than `low`: w_i / factor, linear between */
+    QTALE_ROPE_PARTS = 4      /* the same ends, linear in i between the pairs that make `high` and `low` turns; magnitude 0.1 ln(factor) + 1 */
+};
+typedef struct {
+    int layout;               /* QTALE_ROPE_HALF | QTALE_ROPE_INTERLEAVED */
+    int rotary_dim;           /* even, 2 .. head_dim */
+    const double* freqs;      /* device [rotary_dim / 2]: angle per position */
+    float magnitude;          /* factor on cosine and sine, usually 1 */
+} qtale_rope;
+
+/* freqs (host out [rotary_dim / 2]) and magnitude (host out) of one of the scalings above; original_len, low and high are read for BANDS and
+ * PARTS only, factor by all but PLAIN. */
+int qtale_rope_frequencies(int rotary_dim, float base, int scaling, float factor, int original_len, float low, float high,
+                           double* freqs, float* magnitude);
+
+/* Turns the queries and the new keys of T tokens and stores keys and values into the pages of one layer.  q [T][n_heads * head_dim],
+ * k, v [T][n_kv_heads * head_dim], q_out like q (may be q itself): kv->dtype, *_stride elements between tokens (a multiple of 8), 16-byte aligned.
+ *   seq_offsets [B+1], positions [T] (absolute, for the angles); first [B]: entry of each sequence's first new token in its slot (nullable:
+ *   kv_len minus its new tokens).  Entries at or past kv_len, and those without a page, are not stored. */
+int qtale_paged_rope_append(const qtale_paged_kv* kv, int layer, const qtale_rope* rope, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
+                            int n_heads, int T, const int32_t* seq_offsets, const int32_t* slots, const int32_t* first, int B,
+                            const int32_t* positions, void* stream);
+
+/* Causal attention of T new tokens over the pages of one layer, from one token per sequence to whole prompts:
+ *   out_p = sum_j softmax_j(scale q_p . k_j) v_j,  j <= p, j < kv_len, page of j present, and (window == 0 or j > p - window or j < sinks),
+ * p = first[b] + i for token i of sequence b.  A token that sees no entry gets zeros.  Head h reads kv head h / (n_heads / n_kv_heads).
+ * q and out [T][n_heads * head_dim], *_stride elements between tokens (q: a multiple of 8, 16-byte aligned; out: of 4, 8-byte aligned). */
+typedef struct {
+    int n_heads;
+    int window;               /* entries that a token sees, itself included; 0 = all before it */
+    int sinks;                /* first entries of the slot that stay visible with a window */
+    float scale;              /* > 0, e.g. 1 / sqrt(head_dim) */
+    int max_new;              /* bound on the new tokens of a sequence; 0 = T.  The launches follow from it: a bound near the truth pays */
+    int max_len;              /* bound on kv_len; 0 = max_pages * page_size.  Entries from max_len on are not seen */
+} qtale_paged_attn;
+size_t qtale_paged_attention_workspace_bytes(const qtale_paged_kv* kv, const qtale_paged_attn* attn, int T, int B);
+int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged_attn* attn, const void* q, int64_t q_stride,
+                          void* out, int64_t out_stride, int T, const int32_t* seq_offsets, const int32_t* slots, const int32_t* first,
+                          int B, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing with HIP events recorded on the forward call's stream.  While enabled, every
  * layer/stack forward brackets its kernels with events; qtale_profile_read waits for them and
  * returns, per kernel class, accumulated milliseconds and launch counts since the last read.

@@ -25,8 +25,13 @@ EXPORTS = ["qtale_strerror", "qtale_create", "qtale_destroy", "qtale_set_exec_ra
            "qtale_linear_w4a16", "qtale_swiglu_w4a16", "qtale_profile_enable", "qtale_profile_read",
            "qtale_calibration_scratch_bytes", "qtale_calibrate_threshold_from_scores", "qtale_calibrate_threshold",
            "qtale_graph_capture_stack", "qtale_graph_launch", "qtale_graph_destroy", "qtale_router_mlp_scores",
-           "qtale_static_scratch_bytes", "qtale_layer_forward_static"]
+           "qtale_static_scratch_bytes", "qtale_layer_forward_static",
+           "qtale_pages_init", "qtale_pages_workspace_bytes", "qtale_pages_fork", "qtale_pages_reserve", "qtale_pages_release",
+           "qtale_pages_trim", "qtale_pages_compact", "qtale_pages_copy", "qtale_rope_frequencies", "qtale_paged_rope_append",
+           "qtale_paged_attention_workspace_bytes", "qtale_paged_attention"]
 QTALE_THETA_GRID = 50
+QTALE_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+QTALE_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "parts": 4}
 
 
 class QtaleError(RuntimeError):
@@ -56,6 +61,22 @@ class qtale_layer_weights(C.Structure):
 
 class qtale_kv(C.Structure):
     _fields_ = [("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("kv_len", C.c_void_p), ("cap", C.c_int)]
+
+
+class qtale_paged_kv(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_refs", C.c_void_p), ("free_bits", C.c_void_p),
+                ("table", C.c_void_p), ("kv_len", C.c_void_p), ("kv_cap", C.c_void_p), ("n_pages", C.c_int),
+                ("page_size", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("n_layers", C.c_int),
+                ("n_slots", C.c_int), ("max_pages", C.c_int), ("dtype", C.c_int)]
+
+
+class qtale_rope(C.Structure):
+    _fields_ = [("layout", C.c_int), ("rotary_dim", C.c_int), ("freqs", C.c_void_p), ("magnitude", C.c_float)]
+
+
+class qtale_paged_attn(C.Structure):
+    _fields_ = [("n_heads", C.c_int), ("window", C.c_int), ("sinks", C.c_int), ("scale", C.c_float), ("max_new", C.c_int),
+                ("max_len", C.c_int)]
 
 
 _lib = None
@@ -108,9 +129,25 @@ def load_library():
     lib.qtale_graph_destroy.restype = None
     lib.qtale_profile_enable.argtypes = [vp, i]
     lib.qtale_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
+    pk, i64 = C.POINTER(qtale_paged_kv), C.c_int64
+    lib.qtale_pages_init.argtypes = [pk, vp]
+    lib.qtale_pages_workspace_bytes.argtypes = [pk, i]
+    lib.qtale_pages_workspace_bytes.restype = sz
+    lib.qtale_pages_fork.argtypes = [pk, vp, vp, i, vp]
+    lib.qtale_pages_reserve.argtypes = [pk, i, vp, vp, i, vp, vp, vp, sz, vp]
+    lib.qtale_pages_release.argtypes = [pk, vp, i, vp]
+    lib.qtale_pages_trim.argtypes = [pk, vp, i, i, i, vp]
+    lib.qtale_pages_compact.argtypes = [pk, vp, vp, sz, vp]
+    lib.qtale_pages_copy.argtypes = [pk, pk, vp, vp, i, vp]
+    lib.qtale_rope_frequencies.argtypes = [i, f, i, f, i, f, f, C.POINTER(C.c_double), fp]
+    lib.qtale_paged_rope_append.argtypes = [pk, i, C.POINTER(qtale_rope), vp, i64, vp, i64, vp, i64, vp, i64, i, i, vp, vp, vp, i, vp, vp]
+    lib.qtale_paged_attention_workspace_bytes.argtypes = [pk, C.POINTER(qtale_paged_attn), i, i]
+    lib.qtale_paged_attention_workspace_bytes.restype = sz
+    lib.qtale_paged_attention.argtypes = [pk, i, C.POINTER(qtale_paged_attn), vp, i64, vp, i64, i, vp, vp, vp, i, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("qtale_strerror", "qtale_prepacked_bytes", "qtale_workspace_bytes",
-                        "qtale_calibration_scratch_bytes", "qtale_graph_destroy", "qtale_static_scratch_bytes"):
+                        "qtale_calibration_scratch_bytes", "qtale_graph_destroy", "qtale_static_scratch_bytes",
+                        "qtale_pages_workspace_bytes", "qtale_paged_attention_workspace_bytes"):
             getattr(lib, name).restype = i
     _lib = lib
     return lib
@@ -438,6 +475,194 @@ def qtale_swiglu_w4a16(gate, up, A, out=None):
     g, u = gate.c_struct(), up.c_struct()
     _check(load_library().qtale_swiglu_w4a16(C.byref(g), C.byref(u), gate.bits, gate.group, _ptr(A), M, _ptr(out), _stream()),
            "qtale_swiglu_w4a16")
+    return out
+
+
+# ---- paged K/V cache ------------------------------------------------------------------------------------------
+def _same_device(device, *tensors):
+    for t in tensors:
+        assert t is None or t.device == device, "all tensors of a call are on the cache's device"
+
+
+def _ints(t, device, *shape):
+    """An int32 tensor of that shape, contiguous, on the device (or None)."""
+    if t is not None:
+        assert t.dtype == torch.int32 and t.is_contiguous() and t.device == device and tuple(t.shape) == shape, (t.dtype, tuple(t.shape), shape)
+    return _ptr(t)
+
+
+class PagedKV:
+    """Device arrays of a paged K/V cache (see qtale_paged_kv).  k, v: [n_pages, n_kv_heads, page_size, head_dim] fp16 or bf16; page_refs
+    [n_pages], free_bits [ceil(n_pages / 32)], table [n_layers, n_slots, max_pages], kv_len and kv_cap [n_layers, n_slots]: int32."""
+
+    def __init__(self, k, v, page_refs, free_bits, table, kv_len, kv_cap):
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous()
+        assert table.dim() == 3 and kv_len.shape == kv_cap.shape == table.shape[:2]
+        assert page_refs.shape == (k.shape[0],) and free_bits.shape == ((k.shape[0] + 31) // 32,)
+        for t in (page_refs, free_bits, table, kv_len, kv_cap):
+            assert t.dtype == torch.int32 and t.is_contiguous()
+        _same_device(k.device, v, page_refs, free_bits, table, kv_len, kv_cap)
+        self.k, self.v, self.page_refs, self.free_bits = k, v, page_refs, free_bits
+        self.table, self.kv_len, self.kv_cap = table, kv_len, kv_cap
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.n_layers, self.n_slots, self.max_pages = table.shape
+        self.device, self.dtype = k.device, k.dtype
+        self._c = qtale_paged_kv(k.data_ptr(), v.data_ptr(), page_refs.data_ptr(), free_bits.data_ptr(), table.data_ptr(),
+                                 kv_len.data_ptr(), kv_cap.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
+                                 self.n_layers, self.n_slots, self.max_pages, _act_code(k.dtype))
+
+    @classmethod
+    def empty(cls, n_pages, page_size, n_kv_heads, head_dim, n_slots, max_pages, n_layers=1, dtype=torch.float16, device="cuda"):
+        """Allocates an empty cache."""
+        ints = lambda *size: torch.empty(size, dtype=torch.int32, device=device)
+        k, v = (torch.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype, device=device) for _ in range(2))
+        kv = cls(k, v, ints(n_pages), ints((n_pages + 31) // 32), ints(n_layers, n_slots, max_pages), ints(n_layers, n_slots),
+                 ints(n_layers, n_slots))
+        qtale_pages_init(kv)
+        return kv
+
+    def c_struct(self):
+        return self._c
+
+
+def qtale_pages_init(kv):
+    _check(load_library().qtale_pages_init(C.byref(kv.c_struct()), _stream()), "qtale_pages_init")
+
+
+def qtale_pages_workspace_bytes(kv, max_seqs):
+    return load_library().qtale_pages_workspace_bytes(C.byref(kv.c_struct()), max_seqs)
+
+
+def alloc_pages_workspace(kv, max_seqs):
+    """Scratch of qtale_pages_reserve with up to max_seqs sequences, and of qtale_pages_compact."""
+    n = qtale_pages_workspace_bytes(kv, max_seqs)
+    if n == 0:
+        raise QtaleError(-1, "qtale_pages_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=kv.device)
+
+
+def qtale_pages_fork(kv, src, dst):
+    """Slots dst (empty) become copies of slots src in every layer, sharing their pages."""
+    n = src.numel()
+    _check(load_library().qtale_pages_fork(C.byref(kv.c_struct()), _ints(src, kv.device, n), _ints(dst, kv.device, n), n, _stream()),
+           "qtale_pages_fork")
+
+
+def qtale_pages_reserve(kv, seq_offsets, slots=None, layer=-1, first=None, missing=None, workspace=None):
+    """Room for the new tokens of a call in one layer (or all: -1).  With `first` ([layers, B]) lengths advance too and it gets the old ones."""
+    B = seq_offsets.numel() - 1
+    if workspace is None:
+        workspace = alloc_pages_workspace(kv, B)
+    _same_device(kv.device, workspace)
+    if first is not None:
+        assert first.numel() == (kv.n_layers if layer < 0 else 1) * B
+        first = first.view(-1)
+    _check(load_library().qtale_pages_reserve(
+        C.byref(kv.c_struct()), layer, _ints(seq_offsets, kv.device, B + 1), _ints(slots, kv.device, B), B,
+        None if first is None else _ints(first, kv.device, first.numel()), _ints(missing, kv.device, 1), _ptr(workspace), workspace.numel(),
+        _stream()), "qtale_pages_reserve")
+
+
+def qtale_pages_release(kv, slots=None):
+    """Empties the slots (None: all) in every layer."""
+    n = kv.n_slots if slots is None else slots.numel()
+    _check(load_library().qtale_pages_release(C.byref(kv.c_struct()), _ints(slots, kv.device, n), n, _stream()), "qtale_pages_release")
+
+
+def qtale_pages_trim(kv, window, sinks=0, slots=None):
+    """Lets go of the pages of the slots (None: all) that this window and these first tokens no longer reach."""
+    n = kv.n_slots if slots is None else slots.numel()
+    _check(load_library().qtale_pages_trim(C.byref(kv.c_struct()), _ints(slots, kv.device, n), n, window, sinks, _stream()),
+           "qtale_pages_trim")
+
+
+def qtale_pages_compact(kv, n_live=None, workspace=None):
+    """Moves the pages in use to the front of the pool; n_live: int32 [1], gets their number."""
+    if workspace is None:
+        workspace = alloc_pages_workspace(kv, 0)
+    _same_device(kv.device, workspace)
+    _check(load_library().qtale_pages_compact(C.byref(kv.c_struct()), _ints(n_live, kv.device, 1), _ptr(workspace), workspace.numel(),
+                                              _stream()), "qtale_pages_compact")
+
+
+def qtale_pages_copy(src_kv, dst_kv, src, dst):
+    """Contents of pages src of one pool to pages dst of another of the same page shape."""
+    n = src.numel()
+    _same_device(src_kv.device, dst_kv.k)
+    _check(load_library().qtale_pages_copy(C.byref(src_kv.c_struct()), C.byref(dst_kv.c_struct()), _ints(src, src_kv.device, n),
+                                           _ints(dst, src_kv.device, n), n, _stream()), "qtale_pages_copy")
+
+
+def qtale_rope_frequencies(rotary_dim, base=10000.0, scaling="none", factor=1.0, original_len=0, low=0.0, high=0.0):
+    """(angle per position of every pair: float64 CPU tensor [rotary_dim / 2], factor on cosine and sine)."""
+    freqs, magnitude = (C.c_double * max(rotary_dim // 2, 1))(), C.c_float()
+    _check(load_library().qtale_rope_frequencies(rotary_dim, base, QTALE_ROPE_SCALINGS[scaling], factor, original_len, low, high, freqs,
+                                                 C.byref(magnitude)), "qtale_rope_frequencies")
+    return torch.tensor(list(freqs), dtype=torch.float64), float(magnitude.value)
+
+
+class Rope:
+    """Rotary embedding of a model: layout "half" (pairs i, i + rotary_dim / 2) or "interleaved" (2i, 2i + 1), and its frequencies on the device."""
+
+    def __init__(self, rotary_dim, base=10000.0, layout="half", scaling="none", device="cuda", **how):
+        self.rotary_dim, self.layout = rotary_dim, layout
+        freqs, self.magnitude = qtale_rope_frequencies(rotary_dim, base, scaling, **how)
+        self.freqs = freqs.to(device)
+        self._c = qtale_rope(QTALE_ROPE_LAYOUTS[layout], rotary_dim, self.freqs.data_ptr(), self.magnitude)
+
+    def c_struct(self):
+        return self._c
+
+
+def _heads(t, kv, T, n_heads=None):
+    """[T, heads, head_dim] of the cache's type, heads contiguous; (pointer, elements between tokens)."""
+    assert t.dim() == 3 and t.shape[0] == T and t.shape[2] == kv.head_dim and t.dtype == kv.dtype and t.device == kv.device
+    assert n_heads is None or t.shape[1] == n_heads
+    assert t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == kv.head_dim)
+    return _ptr(t), t.stride(0) if T > 1 else t.shape[1] * kv.head_dim
+
+
+def qtale_paged_rope_append(kv, layer, rope, q, k, v, seq_offsets, positions, first=None, slots=None, q_out=None):
+    """Turns q ([T, n_heads, head_dim]) and k and stores k and v ([T, n_kv_heads, head_dim]) into the pages of one layer.  The heads of a token
+    are contiguous, tokens may be further apart (parts of one q|k|v row).  Returns q_out (None: a new tensor; q itself: in place)."""
+    T, nh = q.shape[0], q.shape[1]
+    B = seq_offsets.numel() - 1
+    if q_out is None:
+        q_out = torch.empty((T, nh, kv.head_dim), dtype=q.dtype, device=q.device)
+    _same_device(kv.device, rope.freqs)
+    _check(load_library().qtale_paged_rope_append(
+        C.byref(kv.c_struct()), layer, C.byref(rope.c_struct()), *_heads(q, kv, T), *_heads(k, kv, T, kv.n_kv_heads),
+        *_heads(v, kv, T, kv.n_kv_heads), *_heads(q_out, kv, T, nh), nh, T, _ints(seq_offsets, kv.device, B + 1),
+        _ints(slots, kv.device, B), _ints(first, kv.device, B), B, _ints(positions, kv.device, T), _stream()), "qtale_paged_rope_append")
+    return q_out
+
+
+def _paged_attn(kv, n_heads, max_new, max_len, window=0, sinks=0, scale=None):
+    return qtale_paged_attn(n_heads, window, sinks, kv.head_dim ** -0.5 if scale is None else scale, max_new, max_len)
+
+
+def alloc_paged_workspace(kv, n_heads, T, B, max_new=0, max_len=0):
+    """Scratch of qtale_paged_attention for calls of at most T tokens with these bounds and B sequences."""
+    n = load_library().qtale_paged_attention_workspace_bytes(C.byref(kv.c_struct()), C.byref(_paged_attn(kv, n_heads, max_new, max_len)), T, B)
+    if n == 0:
+        raise QtaleError(-1, "qtale_paged_attention_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=kv.device)
+
+
+def qtale_paged_attention(kv, layer, q, seq_offsets, first=None, slots=None, out=None, window=0, sinks=0, scale=None, max_new=0, max_len=0,
+                          workspace=None):
+    """Attention of the new tokens q ([T, n_heads, head_dim], turned) over the pages of one layer; returns out ([T, n_heads, head_dim])."""
+    T, nh = q.shape[0], q.shape[1]
+    B = seq_offsets.numel() - 1
+    if out is None:
+        out = torch.empty((T, nh, kv.head_dim), dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = alloc_paged_workspace(kv, nh, T, B, max_new, max_len)
+    _same_device(kv.device, workspace)
+    attn = _paged_attn(kv, nh, max_new, max_len, window, sinks, scale)
+    _check(load_library().qtale_paged_attention(
+        C.byref(kv.c_struct()), layer, C.byref(attn), *_heads(q, kv, T), *_heads(out, kv, T, nh), T, _ints(seq_offsets, kv.device, B + 1),
+        _ints(slots, kv.device, B), _ints(first, kv.device, B), B, _ptr(workspace), workspace.numel(), _stream()), "qtale_paged_attention")
     return out
 
 
