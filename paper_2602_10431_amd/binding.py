@@ -479,16 +479,18 @@ def qtale_swiglu_w4a16(gate, up, A, out=None):
 
 
 # ---- paged K/V cache ------------------------------------------------------------------------------------------
-def _same_device(device, *tensors):
-    for t in tensors:
-        assert t is None or t.device == device, "all tensors of a call are on the cache's device"
+# A decode step calls these once per layer with little work behind each call, so the checks are the few attribute reads that are enough.
+def _ints(t, kv, n):
+    """Address of a contiguous int32 tensor of n elements on the cache's device (None: none)."""
+    if t is None:
+        return None
+    assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous() and t.device == kv.device, (t.dtype, t.shape, n, t.device)
+    return t.data_ptr()
 
 
-def _ints(t, device, *shape):
-    """An int32 tensor of that shape, contiguous, on the device (or None)."""
-    if t is not None:
-        assert t.dtype == torch.int32 and t.is_contiguous() and t.device == device and tuple(t.shape) == shape, (t.dtype, tuple(t.shape), shape)
-    return _ptr(t)
+def _scratch(t, kv):
+    assert t.dtype is torch.uint8 and t.is_contiguous() and t.device == kv.device
+    return t.data_ptr(), t.numel()
 
 
 class PagedKV:
@@ -501,7 +503,8 @@ class PagedKV:
         assert page_refs.shape == (k.shape[0],) and free_bits.shape == ((k.shape[0] + 31) // 32,)
         for t in (page_refs, free_bits, table, kv_len, kv_cap):
             assert t.dtype == torch.int32 and t.is_contiguous()
-        _same_device(k.device, v, page_refs, free_bits, table, kv_len, kv_cap)
+        for t in (v, page_refs, free_bits, table, kv_len, kv_cap):
+            assert t.device == k.device
         self.k, self.v, self.page_refs, self.free_bits = k, v, page_refs, free_bits
         self.table, self.kv_len, self.kv_cap = table, kv_len, kv_cap
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
@@ -510,6 +513,7 @@ class PagedKV:
         self._c = qtale_paged_kv(k.data_ptr(), v.data_ptr(), page_refs.data_ptr(), free_bits.data_ptr(), table.data_ptr(),
                                  kv_len.data_ptr(), kv_cap.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
                                  self.n_layers, self.n_slots, self.max_pages, _act_code(k.dtype))
+        self._ref = C.byref(self._c)
 
     @classmethod
     def empty(cls, n_pages, page_size, n_kv_heads, head_dim, n_slots, max_pages, n_layers=1, dtype=torch.float16, device="cuda"):
@@ -526,11 +530,11 @@ class PagedKV:
 
 
 def qtale_pages_init(kv):
-    _check(load_library().qtale_pages_init(C.byref(kv.c_struct()), _stream()), "qtale_pages_init")
+    _check(load_library().qtale_pages_init(kv._ref, _stream()), "qtale_pages_init")
 
 
 def qtale_pages_workspace_bytes(kv, max_seqs):
-    return load_library().qtale_pages_workspace_bytes(C.byref(kv.c_struct()), max_seqs)
+    return load_library().qtale_pages_workspace_bytes(kv._ref, max_seqs)
 
 
 def alloc_pages_workspace(kv, max_seqs):
@@ -544,8 +548,7 @@ def alloc_pages_workspace(kv, max_seqs):
 def qtale_pages_fork(kv, src, dst):
     """Slots dst (empty) become copies of slots src in every layer, sharing their pages."""
     n = src.numel()
-    _check(load_library().qtale_pages_fork(C.byref(kv.c_struct()), _ints(src, kv.device, n), _ints(dst, kv.device, n), n, _stream()),
-           "qtale_pages_fork")
+    _check(load_library().qtale_pages_fork(kv._ref, _ints(src, kv, n), _ints(dst, kv, n), n, _stream()), "qtale_pages_fork")
 
 
 def qtale_pages_reserve(kv, seq_offsets, slots=None, layer=-1, first=None, missing=None, workspace=None):
@@ -553,44 +556,36 @@ def qtale_pages_reserve(kv, seq_offsets, slots=None, layer=-1, first=None, missi
     B = seq_offsets.numel() - 1
     if workspace is None:
         workspace = alloc_pages_workspace(kv, B)
-    _same_device(kv.device, workspace)
-    if first is not None:
-        assert first.numel() == (kv.n_layers if layer < 0 else 1) * B
-        first = first.view(-1)
     _check(load_library().qtale_pages_reserve(
-        C.byref(kv.c_struct()), layer, _ints(seq_offsets, kv.device, B + 1), _ints(slots, kv.device, B), B,
-        None if first is None else _ints(first, kv.device, first.numel()), _ints(missing, kv.device, 1), _ptr(workspace), workspace.numel(),
-        _stream()), "qtale_pages_reserve")
+        kv._ref, layer, _ints(seq_offsets, kv, B + 1), _ints(slots, kv, B), B, _ints(first, kv, (kv.n_layers if layer < 0 else 1) * B),
+        _ints(missing, kv, 1), *_scratch(workspace, kv), _stream()), "qtale_pages_reserve")
 
 
 def qtale_pages_release(kv, slots=None):
     """Empties the slots (None: all) in every layer."""
     n = kv.n_slots if slots is None else slots.numel()
-    _check(load_library().qtale_pages_release(C.byref(kv.c_struct()), _ints(slots, kv.device, n), n, _stream()), "qtale_pages_release")
+    _check(load_library().qtale_pages_release(kv._ref, _ints(slots, kv, n), n, _stream()), "qtale_pages_release")
 
 
 def qtale_pages_trim(kv, window, sinks=0, slots=None):
     """Lets go of the pages of the slots (None: all) that this window and these first tokens no longer reach."""
     n = kv.n_slots if slots is None else slots.numel()
-    _check(load_library().qtale_pages_trim(C.byref(kv.c_struct()), _ints(slots, kv.device, n), n, window, sinks, _stream()),
-           "qtale_pages_trim")
+    _check(load_library().qtale_pages_trim(kv._ref, _ints(slots, kv, n), n, window, sinks, _stream()), "qtale_pages_trim")
 
 
 def qtale_pages_compact(kv, n_live=None, workspace=None):
     """Moves the pages in use to the front of the pool; n_live: int32 [1], gets their number."""
     if workspace is None:
         workspace = alloc_pages_workspace(kv, 0)
-    _same_device(kv.device, workspace)
-    _check(load_library().qtale_pages_compact(C.byref(kv.c_struct()), _ints(n_live, kv.device, 1), _ptr(workspace), workspace.numel(),
-                                              _stream()), "qtale_pages_compact")
+    _check(load_library().qtale_pages_compact(kv._ref, _ints(n_live, kv, 1), *_scratch(workspace, kv), _stream()), "qtale_pages_compact")
 
 
 def qtale_pages_copy(src_kv, dst_kv, src, dst):
     """Contents of pages src of one pool to pages dst of another of the same page shape."""
     n = src.numel()
-    _same_device(src_kv.device, dst_kv.k)
-    _check(load_library().qtale_pages_copy(C.byref(src_kv.c_struct()), C.byref(dst_kv.c_struct()), _ints(src, src_kv.device, n),
-                                           _ints(dst, src_kv.device, n), n, _stream()), "qtale_pages_copy")
+    assert dst_kv.device == src_kv.device
+    _check(load_library().qtale_pages_copy(src_kv._ref, dst_kv._ref, _ints(src, src_kv, n), _ints(dst, src_kv, n), n, _stream()),
+           "qtale_pages_copy")
 
 
 def qtale_rope_frequencies(rotary_dim, base=10000.0, scaling="none", factor=1.0, original_len=0, low=0.0, high=0.0):
@@ -609,31 +604,32 @@ class Rope:
         freqs, self.magnitude = qtale_rope_frequencies(rotary_dim, base, scaling, **how)
         self.freqs = freqs.to(device)
         self._c = qtale_rope(QTALE_ROPE_LAYOUTS[layout], rotary_dim, self.freqs.data_ptr(), self.magnitude)
+        self._ref = C.byref(self._c)
 
     def c_struct(self):
         return self._c
 
 
-def _heads(t, kv, T, n_heads=None):
-    """[T, heads, head_dim] of the cache's type, heads contiguous; (pointer, elements between tokens)."""
-    assert t.dim() == 3 and t.shape[0] == T and t.shape[2] == kv.head_dim and t.dtype == kv.dtype and t.device == kv.device
-    assert n_heads is None or t.shape[1] == n_heads
-    assert t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == kv.head_dim)
-    return _ptr(t), t.stride(0) if T > 1 else t.shape[1] * kv.head_dim
+def _heads(t, kv, T, n):
+    """(address, elements between tokens) of [T, n, head_dim] of the cache's type, the heads of a token contiguous."""
+    step = t.stride()
+    assert t.shape == (T, n, kv.head_dim) and step[1:] == (kv.head_dim, 1) and t.dtype is kv.dtype and t.device == kv.device, (t.shape, step)
+    return t.data_ptr(), step[0]
 
 
 def qtale_paged_rope_append(kv, layer, rope, q, k, v, seq_offsets, positions, first=None, slots=None, q_out=None):
     """Turns q ([T, n_heads, head_dim]) and k and stores k and v ([T, n_kv_heads, head_dim]) into the pages of one layer.  The heads of a token
     are contiguous, tokens may be further apart (parts of one q|k|v row).  Returns q_out (None: a new tensor; q itself: in place)."""
-    T, nh = q.shape[0], q.shape[1]
+    T, nh, _ = q.shape
     B = seq_offsets.numel() - 1
     if q_out is None:
         q_out = torch.empty((T, nh, kv.head_dim), dtype=q.dtype, device=q.device)
-    _same_device(kv.device, rope.freqs)
+    assert rope.freqs.device == kv.device
+    nkv = kv.n_kv_heads
     _check(load_library().qtale_paged_rope_append(
-        C.byref(kv.c_struct()), layer, C.byref(rope.c_struct()), *_heads(q, kv, T), *_heads(k, kv, T, kv.n_kv_heads),
-        *_heads(v, kv, T, kv.n_kv_heads), *_heads(q_out, kv, T, nh), nh, T, _ints(seq_offsets, kv.device, B + 1),
-        _ints(slots, kv.device, B), _ints(first, kv.device, B), B, _ints(positions, kv.device, T), _stream()), "qtale_paged_rope_append")
+        kv._ref, layer, rope._ref, *_heads(q, kv, T, nh), *_heads(k, kv, T, nkv), *_heads(v, kv, T, nkv), *_heads(q_out, kv, T, nh), nh, T,
+        _ints(seq_offsets, kv, B + 1), _ints(slots, kv, B), _ints(first, kv, B), B, _ints(positions, kv, T), _stream()),
+        "qtale_paged_rope_append")
     return q_out
 
 
@@ -643,7 +639,7 @@ def _paged_attn(kv, n_heads, max_new, max_len, window=0, sinks=0, scale=None):
 
 def alloc_paged_workspace(kv, n_heads, T, B, max_new=0, max_len=0):
     """Scratch of qtale_paged_attention for calls of at most T tokens with these bounds and B sequences."""
-    n = load_library().qtale_paged_attention_workspace_bytes(C.byref(kv.c_struct()), C.byref(_paged_attn(kv, n_heads, max_new, max_len)), T, B)
+    n = load_library().qtale_paged_attention_workspace_bytes(kv._ref, C.byref(_paged_attn(kv, n_heads, max_new, max_len)), T, B)
     if n == 0:
         raise QtaleError(-1, "qtale_paged_attention_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=kv.device)
@@ -652,17 +648,16 @@ def alloc_paged_workspace(kv, n_heads, T, B, max_new=0, max_len=0):
 def qtale_paged_attention(kv, layer, q, seq_offsets, first=None, slots=None, out=None, window=0, sinks=0, scale=None, max_new=0, max_len=0,
                           workspace=None):
     """Attention of the new tokens q ([T, n_heads, head_dim], turned) over the pages of one layer; returns out ([T, n_heads, head_dim])."""
-    T, nh = q.shape[0], q.shape[1]
+    T, nh, _ = q.shape
     B = seq_offsets.numel() - 1
     if out is None:
         out = torch.empty((T, nh, kv.head_dim), dtype=q.dtype, device=q.device)
     if workspace is None:
         workspace = alloc_paged_workspace(kv, nh, T, B, max_new, max_len)
-    _same_device(kv.device, workspace)
     attn = _paged_attn(kv, nh, max_new, max_len, window, sinks, scale)
     _check(load_library().qtale_paged_attention(
-        C.byref(kv.c_struct()), layer, C.byref(attn), *_heads(q, kv, T), *_heads(out, kv, T, nh), T, _ints(seq_offsets, kv.device, B + 1),
-        _ints(slots, kv.device, B), _ints(first, kv.device, B), B, _ptr(workspace), workspace.numel(), _stream()), "qtale_paged_attention")
+        kv._ref, layer, C.byref(attn), *_heads(q, kv, T, nh), *_heads(out, kv, T, nh), T, _ints(seq_offsets, kv, B + 1), _ints(slots, kv, B),
+        _ints(first, kv, B), B, *_scratch(workspace, kv), _stream()), "qtale_paged_attention")
     return out
 
 

@@ -76,4 +76,75 @@ struct SeqView {
     }
 };
 
+// One column by one wave on the vector ALUs, keys [key(s0), ...) of steps s0 .. s1 - 1, touching only keys that the column sees; lane l gets the
+// numerators of columns (D / 64) l ..  For the rare column whose sum is not finite: the matrix products serve columns that see a key and columns
+// that do not, and a masked key's probability of zero times an infinity or a NaN is NaN.  A finite sum has met neither, so it stands; one that
+// is not is done again here.  (About 45 cycles per key.)
+template <int D, bool BF16, int G>
+__device__ void redo_column(const PagedAttnDev& p, const KeySteps<G>& walk, int slot, int hk, const uint16_t* q, int place, int s0, int s1, float* num,
+                            float* m_out, float* l_out) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    const int32_t* row = p.table + static_cast<size_t>(slot) * p.max_pages;
+    auto at = [&](int page, int key) { return (((static_cast<size_t>(page) * p.nkv + hk) << p.shift) + (key & ((1 << p.shift) - 1))) * D; };
+    float m = kPagedNone, l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) num[e] = 0.0f;
+#pragma unroll 1
+    for (int st = s0; st < s1; ++st) {
+        const int key = walk.key(st) + lane;
+        int page = -1;
+        if (lane < G && key <= place && key < walk.hi && (p.window == 0 || key > place - p.window || key < p.sinks)) page = row[min(key >> p.shift, p.max_pages - 1)];
+        const bool seen = static_cast<uint32_t>(page) < static_cast<uint32_t>(p.n_pages);
+        uint64_t who = __ballot(seen);
+        if (who == 0) continue;
+        float score = -INFINITY;
+        if (seen) {
+            const uint16_t* k = p.k + at(page, key);
+            float sum = 0.0f;
+#pragma unroll 1
+            for (int e = 0; e < D; e += 2) {
+                const uint32_t a = *reinterpret_cast<const uint32_t*>(k + e), b = *reinterpret_cast<const uint32_t*>(q + e);
+                sum = fmaf(Act16<BF16>::low(a), Act16<BF16>::low(b), sum);
+                sum = fmaf(Act16<BF16>::high(a), Act16<BF16>::high(b), sum);
+            }
+            score = sum * p.scale_log2;
+        }
+        const float m_new = fmaxf(m, wave_max(score)), alpha = __builtin_amdgcn_exp2f(m - m_new);
+        const float w = seen ? __builtin_amdgcn_exp2f(score - m_new) : 0.0f;
+        m = m_new;
+        l = l * alpha + wave_sum(w);
+#pragma unroll
+        for (int e = 0; e < E; ++e) num[e] *= alpha;
+#pragma unroll 1
+        for (; who != 0; who &= who - 1) {
+            const int j = __ffsll(static_cast<long long>(who)) - 1;
+            const float wj = __shfl(w, j, 64);
+            const uint16_t* v = p.v + at(__shfl(page, j, 64), walk.key(st) + j) + E * lane;
+#pragma unroll
+            for (int e = 0; e < E; ++e) num[e] = fmaf(wj, act_to_float<BF16>(v[e]), num[e]);
+        }
+    }
+    *m_out = m;
+    *l_out = l;
+}
+
+// Where a (row, head)'s result goes: range z of `ranges` to the partial sums, or the output.  One wave, lane l with columns (D / 64) l ..
+template <int D, bool BF16>
+__device__ void put_column(const PagedAttnDev& p, size_t token, int head, int z, int ranges, const float* num, float m, float l) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    if (ranges > 1) {
+        float* dst = p.part + ((token * p.nh + head) * p.n_split + z) * part_stride(D);
+#pragma unroll
+        for (int e = 0; e < E; ++e) dst[E * lane + e] = num[e];
+        if (lane == 0) { dst[D] = m; dst[D + 1] = l; }
+        return;
+    }
+    const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+    uint16_t* out = p.out + token * p.out_stride + head * D + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e] = static_cast<uint16_t>(Act16<BF16>::pack(num[e] * inv, 0.0f) & 0xffffu);
+}
+
 }  // namespace qtale

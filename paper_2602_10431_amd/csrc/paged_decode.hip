@@ -236,6 +236,8 @@ paged_decode_kernel(PagedAttnDev p) {
 
     // the four waves meet in LDS
     __shared__ float sm[4][kDecodeCols][D + 2];
+    __shared__ uint32_t s_redo;                                  // columns whose sum is not finite
+    if (tid == 0) s_redo = 0;
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
     if (c < cols) {
@@ -260,6 +262,7 @@ paged_decode_kernel(PagedAttnDev p) {
             den += sm[w][r][D + 1] * f;
         }
         const int i = r / p.rep, h = hk * p.rep + r - i * p.rep;
+        if (n_minus > 0 && fmaf(n0, 0.0f, fmaf(n1, 0.0f, den * 0.0f)) != 0.0f) atomicOr(&s_redo, 1u << r);
         if (SPLIT && ranges > 1) {
             float* dst = p.part + (static_cast<size_t>(s.row0 + i) * p.nh + h) * p.n_split * part_stride(D) + static_cast<size_t>(z) * part_stride(D);
             *reinterpret_cast<float2_t*>(dst + e) = float2_t{n0, n1};
@@ -269,6 +272,20 @@ paged_decode_kernel(PagedAttnDev p) {
             *reinterpret_cast<uint32_t*>(p.out + (s.row0 + i) * p.out_stride + h * D + e) = A::pack(n0 * inv, n1 * inv);
             if (SPLIT && e == 0) p.part[(static_cast<size_t>(s.row0 + i) * p.nh + h) * p.n_split * part_stride(D) + D + 2] = 1.0f;
         }
+    }
+    // Several queries: a value that is not finite, seen by the later ones, has met the earlier ones' zeros (redo_column).  A single query meets
+    // no key that it does not see.
+    if (n_minus == 0) return;
+    __syncthreads();
+    uint32_t redo = s_redo;
+    const int begin = SPLIT ? z * per : 0, end = SPLIT && z < ranges - 1 ? min((z + 1) * per, walk.steps) : walk.steps;
+#pragma unroll 1
+    for (int j = 0; redo != 0; ++j, redo &= redo - 1) {
+        if ((j & 3) != wave) continue;
+        const int r = __ffs(static_cast<int>(redo)) - 1, i = r / p.rep, h = hk * p.rep + r - i * p.rep;
+        float num[D / 64], m, l;
+        redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + i) * p.q_stride + h * D, s.first + i, begin, end, num, &m, &l);
+        put_column<D, BF16>(p, s.row0 + i, h, z, ranges, num, m, l);
     }
 }
 

@@ -276,19 +276,39 @@ paged_chunk_kernel(PagedAttnDev p) {
     }
 
     const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+    // columns whose sum is not finite (redo_column): both lanes of a column are left out below
+    float zero = l_tot * 0.0f;
+#pragma unroll
+    for (int f = 0; f < DF; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero = fmaf(o[f][r], 0.0f, zero);
+    uint64_t redo = __ballot(zero != 0.0f && c_lo + wave * 32 + l32 <= c_hi);
+    redo = (redo | redo >> 32) & 0xffffffffull;
+#pragma unroll 1
+    for (uint64_t left = redo; left != 0; left &= left - 1) {
+        const int j = __ffsll(static_cast<long long>(left)) - 1;
+        const int qj = __shfl(qi, j, 64), hj = __shfl(head, j, 64);
+        float num[D / 64], m, l;
+        redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + qj) * p.q_stride + hj * D, s.first + qj, t0, t1, num, &m, &l);
+        put_column<D, BF16>(p, s.row0 + qj, hj, z, ranges, num, m, l);
+    }
     if (c_lo + wave * 32 + l32 > c_hi) return;
+    const bool done = (redo >> l32 & 1) != 0;
     const size_t pair = static_cast<size_t>(s.row0 + qi) * p.nh + head;
     if (SPLIT && ranges > 1) {
         float* dst = p.part + (pair * p.n_split + z) * part_stride(D);
+        if (lhi == 0) dst[D + 2] = static_cast<float>(ranges);
+        if (done) return;
 #pragma unroll
         for (int f = 0; f < DF; ++f)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4)
                 *reinterpret_cast<float4_t*>(dst + f * 32 + 8 * q4 + 4 * lhi) = float4_t{o[f][4 * q4], o[f][4 * q4 + 1], o[f][4 * q4 + 2], o[f][4 * q4 + 3]};
-        if (lhi == 0) *reinterpret_cast<float4_t*>(dst + D) = float4_t{m_run, l_tot, static_cast<float>(ranges), 0.0f};
+        if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{m_run, l_tot};
         return;
     }
     if (SPLIT && lhi == 0) p.part[pair * p.n_split * part_stride(D) + D + 2] = 1.0f;
+    if (done) return;
     const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;       // a row that sees no key is zero
     uint16_t* orow = p.out + (s.row0 + qi) * p.out_stride + head * D;
 #pragma unroll
