@@ -61,29 +61,36 @@ struct PagedAttnDev {
     int B, nh, nkv, rep, shift, max_pages, n_slots, n_pages;
     int window, sinks, max_len;
     float scale_log2;
-    int items;                   // chunk kernel: bound on its column tiles
-    int ranges;                  // key ranges per (sequence, kv head) or column tile that this kernel may cut
-    int n_split;                 // ... and that the partial sums have room for; 1 = none
-    int target;                  // decode with key ranges: workgroups that the ranges of the call are to be
     int take;                    // 0: every sequence; 1: only those of this kernel (the other one is launched too)
-    float* part;                 // [T * nh][n_split][part_stride(d)]
+    // chunk kernel: column tiles (bound), key ranges that one may be cut into (1: none), workgroups that the call's ranges are to be, and the
+    // ranges' sums [T * nh][ranges][part_stride(d)]
+    int items, ranges, target;
+    float* part;
+    // decode kernel: spans per kv head that the call's keys are cut into (0: a workgroup per sequence), the sums of a span's first and last
+    // piece [nkv][spans][2][kDecodeCols][part_stride(d)], and where a sequence's pieces are: [B] (first span, pieces, place of the first, -)
+    int spans, cols;             // cols: bound on a sequence's columns
+    float* span_part;
+    int4* pieces;
 };
 struct PagedAttnPlan {
     bool decode, chunk;          // which kernels run
-    int decode_split, chunk_split, items, target;
+    int spans;                   // decode
+    int ranges, target, groups, items;   // chunk; groups of waves per workgroup
     bool too_large;              // more workgroups than a grid has
-    size_t bytes;                // of workspace
+    size_t decode_bytes, bytes;  // of workspace: the decode kernel's, all
 };
 constexpr int kDecodeCols = 16;                  // (query, head) pairs per kv head that the decode kernel holds
 constexpr int kChunkCols = 128;                  // ... and a workgroup of the chunk kernel
-constexpr int kDecodeRangeKeys = 256;            // a key range of the decode kernel is a multiple of this
-constexpr int part_stride(int d) { return d + 4; }   // floats of a range's sums: numerators, reference point, denominator, ranges, unused
-PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max_new, int max_len);
-// All launches of a call; a: everything but items, key ranges, `take` and the partial sums, which follow from the plan.
+constexpr int kChunkTileKeys = 64;
+constexpr int kSpanSeqs = 1024;                  // bound on the sequences of a call that is cut into spans
+constexpr int part_stride(int d) { return d + 4; }   // floats of a column's sums: numerators, reference point, denominator, (chunk) ranges, unused
+PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks);
+size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B);   // of workspace, for any call of at most T tokens and B sequences
+// All launches of a call; a: everything but `take` and what follows it, which the plan says.
 hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int bf16, int T, float* workspace, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);
-hipError_t launch_paged_chunk(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);
-hipError_t launch_paged_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream);
+hipError_t launch_paged_chunk(const PagedAttnDev& a, int groups, int d, int bf16, hipStream_t stream);
+hipError_t launch_chunk_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream);
 
 #ifdef __HIP_DEVICE_COMPILE__
 #define QT_CONST_AS __attribute__((address_space(4)))

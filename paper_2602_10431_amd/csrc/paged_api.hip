@@ -161,9 +161,7 @@ int qtale_paged_rope_append(const qtale_paged_kv* kv, int layer, const qtale_rop
 
 size_t qtale_paged_attention_workspace_bytes(const qtale_paged_kv* kv, const qtale_paged_attn* attn, int T, int B) {
     if (check_paged(kv, false) || check_paged_attn(attn, kv) || T < 0 || B < 0) return 0;
-    if (T == 0 || B == 0) return 256;
-    const PagedAttnBounds m = attn_bounds(attn, kv, T);
-    return plan_paged_attention(attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B, m.max_new, m.max_len).bytes;
+    return T == 0 || B == 0 ? 256 : paged_attention_bytes(attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B);
 }
 
 int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged_attn* attn, const void* q, int64_t q_stride, void* out,
@@ -180,7 +178,7 @@ int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged
     const int64_t row = static_cast<int64_t>(attn->n_heads) * kv->head_dim;
     if ((e = check_rows(q, q_stride, row, 8)) || (e = check_rows(out, out_stride, row, 4))) return e;
     const PagedAttnBounds m = attn_bounds(attn, kv, T);
-    const PagedAttnPlan plan = plan_paged_attention(attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B, m.max_new, m.max_len);
+    const PagedAttnPlan plan = plan_paged_attention(attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B, m.max_new, m.max_len, attn->window, attn->sinks);
     if (plan.too_large) return QTALE_ERR_UNSUPPORTED;
     if ((e = check_workspace(workspace, workspace_bytes, plan.bytes))) return e;
     PagedAttnDev a = attn_device(kv, layer, attn, m);

@@ -129,22 +129,72 @@ __device__ void redo_column(const PagedAttnDev& p, const KeySteps<G>& walk, int 
     *l_out = l;
 }
 
-// Where a (row, head)'s result goes: range z of `ranges` to the partial sums, or the output.  One wave, lane l with columns (D / 64) l ..
+// A column's result, by one wave, lane l with columns (D / 64) l ..: to its place among the partial sums, or (none) to the output.
 template <int D, bool BF16>
-__device__ void put_column(const PagedAttnDev& p, size_t token, int head, int z, int ranges, const float* num, float m, float l) {
+__device__ void put_column(const float* num, float m, float l, float* part, uint16_t* out) {
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
-    if (ranges > 1) {
-        float* dst = p.part + ((token * p.nh + head) * p.n_split + z) * part_stride(D);
+    if (part) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) dst[E * lane + e] = num[e];
-        if (lane == 0) { dst[D] = m; dst[D + 1] = l; }
+        for (int e = 0; e < E; ++e) part[E * lane + e] = num[e];
+        if (lane == 0) { part[D] = m; part[D + 1] = l; }
         return;
     }
     const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-    uint16_t* out = p.out + token * p.out_stride + head * D + E * lane;
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = static_cast<uint16_t>(Act16<BF16>::pack(num[e] * inv, 0.0f) & 0xffffu);
+    for (int e = 0; e < E; ++e) out[E * lane + e] = static_cast<uint16_t>(Act16<BF16>::pack(num[e] * inv, 0.0f) & 0xffffu);
 }
+
+// Sums of key ranges, 16 bytes per lane: lane l of D / 4 has columns 4 l .. 4 l + 3.
+struct RangeSum {
+    float m = kPagedNone, den = 0.0f;
+    float4_t num = {0.f, 0.f, 0.f, 0.f};
+    // adds N ranges at once (those with on[u]); the reference point of a range without keys lets it drop out
+    template <int N>
+    __device__ __forceinline__ void add(const float4_t* x, const float2_t* s, const bool* on) {
+        float m_new = m;
+#pragma unroll
+        for (int u = 0; u < N; ++u) m_new = on[u] ? fmaxf(m_new, s[u][0]) : m_new;
+        const float a = __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        den *= a;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) num[e] *= a;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            if (!on[u]) continue;                                // (what was loaded in its place may be anything)
+            const float f = __builtin_amdgcn_exp2f(s[u][0] - m);
+            den += s[u][1] * f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) num[e] += x[u][e] * f;
+        }
+    }
+    // ranges z0, z0 + step, ... < ranges; row_of(z): the sums of range z
+    template <int D, class RowOf>
+    __device__ __forceinline__ void add_all(int z0, int step, int ranges, int lane, RowOf row_of) {
+        constexpr int N = 4;                                     // ranges whose loads are in flight together
+        for (int z = z0; z < ranges; z += N * step) {
+            float4_t x[N];
+            float2_t s[N];
+            bool on[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                on[u] = z + u * step < ranges;
+                const float* row = row_of(on[u] ? z + u * step : z);
+                s[u] = *reinterpret_cast<const float2_t*>(row + D);
+                x[u] = *reinterpret_cast<const float4_t*>(row + 4 * lane);
+            }
+            add<N>(x, s, on);
+        }
+    }
+    template <bool BF16>
+    __device__ __forceinline__ void put(uint16_t* out, int lane) const {
+        const float inv = den != 0.0f ? 1.0f / den : 0.0f;       // a row that sees no key is zero
+        u32x2_t w;
+        w[0] = Act16<BF16>::pack(num[0] * inv, num[1] * inv);
+        w[1] = Act16<BF16>::pack(num[2] * inv, num[3] * inv);
+        *reinterpret_cast<u32x2_t*>(out + 4 * lane) = w;
+    }
+};
 
 }  // namespace qtale

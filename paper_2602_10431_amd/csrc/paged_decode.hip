@@ -10,8 +10,9 @@
 // maybe, would be NaN).  Probabilities are 32-bit sums; as operands they go in as two 16-bit terms, p = hi + lo, through two products into one
 // accumulator, which leaves 2^-16 (bf16) or 2^-22 of them: the matrix cores have time (about a tenth of the stream's), and a bf16 probability
 // alone would add as much error as the output's own rounding.
-// What bounds it is the stream of keys and values.  Few (sequence, kv head) pairs: the keys of the call are cut into ranges of equal length so
-// that `target` workgroups run, and a second launch adds the ranges' sums.
+// What bounds it is the stream of keys and values, and a CU takes in no more than about 50 GB/s (1 x 3000 keys, 32 workgroups: 33 us, whatever
+// the waves per workgroup).  So with few (sequence, kv head) pairs the keys of the call, laid end to end over its sequences, are cut into equally
+// long spans, one per workgroup that fits the chip; a span may end one sequence and begin the next, and a second launch adds the pieces.
 #include <algorithm>
 
 #include "paged_attn.h"
@@ -19,22 +20,16 @@
 namespace qtale {
 
 constexpr int kStepKeys = 32;                    // per wave
-constexpr int kRangeSteps = kDecodeRangeKeys / kStepKeys;   // two per wave
+constexpr int kUnitSteps = 4;                    // spans are cut at multiples of this: a step per wave
 
-// Steps of a sequence's call, and how a call with key ranges is cut: ranges of `per` steps, numbered through the sequences in order.
-__device__ __forceinline__ int seq_steps(const PagedAttnDev& p, int b, bool* mine) {
+// Units of a sequence in a call with spans; 0: not this kernel's.  A sequence without keys has one, in which its zeros are written.
+__device__ __forceinline__ int seq_units(const PagedAttnDev& p, int b) {
     const SeqView s(p, b);
-    *mine = s.n > 0 && (p.take == 0 || s.n * p.rep <= kDecodeCols);
-    return *mine ? KeySteps<kStepKeys>(s.first, s.first + s.n - 1, s.len, p.window, p.sinks).steps : 0;
+    if (s.n == 0 || (p.take != 0 && s.n * p.rep > kDecodeCols)) return 0;
+    return max((KeySteps<kStepKeys>(s.first, s.first + s.n - 1, s.len, p.window, p.sinks).steps + kUnitSteps - 1) / kUnitSteps, 1);
 }
 
-__device__ __forceinline__ int wave_total(int v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
-template <int D, bool BF16, bool SPLIT>
+template <int D, bool BF16, bool SPANS>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : 3)
 paged_decode_kernel(PagedAttnDev p) {
     using A = Act16<BF16>;
@@ -45,47 +40,51 @@ paged_decode_kernel(PagedAttnDev p) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
+    __shared__ float sm[4][kDecodeCols][D + 2];
+    __shared__ uint32_t s_redo;                                  // columns whose sum is not finite
+    __shared__ int ends[SPANS ? kSpanSeqs : 1];                  // units up to and with sequence b
 
-    int b = blockIdx.y, z = 0, ranges = 1, per = 0;
-    if (SPLIT) {
-        int total = 0;
+    int b = blockIdx.y, cur = 0, end = 0, total = 0, spans = 1;
+    uint32_t span = 0;
+    if (SPANS) {
         for (int b0 = 0; b0 < p.B; b0 += 64) {
-            bool mine = false;
-            total += wave_total(b0 + lane < p.B ? seq_steps(p, b0 + lane, &mine) : 0);
-        }
-        const int wanted = max(p.target / p.nkv, 1);             // ranges of the call, per kv head
-        per = ((total + wanted - 1) / wanted + kRangeSteps - 1) / kRangeSteps * kRangeSteps;
-        per = max(per, kRangeSteps);
-        int item = blockIdx.y, found = -1;
-        for (int b0 = 0; b0 < p.B && found < 0; b0 += 64) {
-            bool mine = false;
-            const int steps = b0 + lane < p.B ? seq_steps(p, b0 + lane, &mine) : 0;
-            const int n = mine ? min(max((steps + per - 1) / per, 1), p.ranges) : 0;
-            int before = n;                                      // inclusive prefix sum over the lanes
+            int sum = b0 + lane < p.B ? seq_units(p, b0 + lane) : 0;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
-                const int y = __shfl_up(before, o, 64);
-                if (lane >= o) before += y;
+                const int y = __shfl_up(sum, o, 64);
+                if (lane >= o) sum += y;
             }
-            const uint64_t past = __ballot(before > item);
-            if (past) {
-                const int at = __ffsll(static_cast<long long>(past)) - 1;
-                found = b0 + at;
-                ranges = __shfl(n, at, 64);
-                z = item - (__shfl(before, at, 64) - ranges);
-            } else {
-                item -= __shfl(before, 63, 64);
-            }
+            if (wave == 0) ends[b0 + lane] = total + sum;
+            total += __shfl(sum, 63, 64);
         }
-        if (found < 0) return;
-        b = __builtin_amdgcn_readfirstlane(found);
-        z = __builtin_amdgcn_readfirstlane(z);
-        ranges = __builtin_amdgcn_readfirstlane(ranges);
+        total = __builtin_amdgcn_readfirstlane(total);
+        spans = min(p.spans, total);
+        span = blockIdx.y;
+        if (static_cast<int>(span) >= spans) return;
+        cur = static_cast<int>(static_cast<uint64_t>(span) * total / static_cast<uint32_t>(spans));
+        end = static_cast<int>(static_cast<uint64_t>(span + 1) * total / static_cast<uint32_t>(spans));
+        __syncthreads();
+        b = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 64) b += __popcll(__ballot(b0 + lane < p.B && ends[min(b0 + lane, p.B - 1)] <= cur));
     }
+    const int begin = cur;
+again:                                                           // the pieces of a span
+    b = __builtin_amdgcn_readfirstlane(b);
     SeqView s(p, b);
     s.uniform();
     const int cols = s.n * p.rep;
-    if (s.n == 0 || (p.take != 0 && cols > kDecodeCols)) return;
+    if (!SPANS && (s.n == 0 || (p.take != 0 && cols > kDecodeCols))) return;
+    const KeySteps<kStepKeys> walk(s.first, s.first + s.n - 1, s.len, p.window, p.sinks);
+    int first_step = 0, last_step = walk.steps;
+    bool whole = true;
+    int seq_begin = 0, seq_end = 0;
+    if (SPANS) {
+        seq_begin = b > 0 ? __builtin_amdgcn_readfirstlane(ends[b - 1]) : 0;
+        seq_end = __builtin_amdgcn_readfirstlane(ends[b]);
+        first_step = (cur - seq_begin) * kUnitSteps;
+        if (end < seq_end) last_step = min(last_step, (end - seq_begin) * kUnitSteps);
+        whole = cur == seq_begin && end >= seq_end;
+    }
     const int col = min(c, cols - 1);                            // this lane's column: query col / rep, head col % rep
     const int qi = col / p.rep, head = hk * p.rep + col - qi * p.rep;
     const int place = s.first + qi;                              // the query's place in its slot
@@ -95,14 +94,9 @@ paged_decode_kernel(PagedAttnDev p) {
 #pragma unroll
     for (int k = 0; k < S; ++k) q[k] = *reinterpret_cast<const u32x4_t*>(qrow + 32 * k);
 
-    const KeySteps<kStepKeys> walk(s.first, s.first + s.n - 1, s.len, p.window, p.sinks);
-    int s0 = wave, s1 = walk.steps;                              // this wave's steps: s0, s0 + 4, ...
-    if (SPLIT) {
-        s0 += z * per;
-        if (z < ranges - 1) s1 = min(s1, (z + 1) * per);         // (the last range takes what is left)
-    }
+    const int s0 = first_step + wave, s1 = last_step;            // this wave's steps: s0, s0 + 4, ...
     const PageRow pages(p, s.slot);
-    const int first = s.first, hi = walk.hi, lo = walk.lo, n_minus = s.n - 1;
+    const int hi = walk.hi, lo = walk.lo, n_minus = s.n - 1;
     const size_t head_elems = static_cast<size_t>(D) << p.shift;
 
     // page ids of the two fragments of a step: read one step before the loads that use them
@@ -192,7 +186,7 @@ paged_decode_kernel(PagedAttnDev p) {
         for (int u = 0; u < 2; ++u) st[u] = scores(kn[u]);
         next(0);
         // every key of the step is seen by every query, unless the step lies at an end of the keys or a page is gone
-        if (!(kb + kStepKeys <= min(first + 1, hi) && (kb >= lo + n_minus || kb + kStepKeys <= p.sinks) && (id.a | id.b) >= 0)) {
+        if (!(kb + kStepKeys <= min(s.first + 1, hi) && (kb >= lo + n_minus || kb + kStepKeys <= p.sinks) && (id.a | id.b) >= 0)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -235,8 +229,6 @@ paged_decode_kernel(PagedAttnDev p) {
     }
 
     // the four waves meet in LDS
-    __shared__ float sm[4][kDecodeCols][D + 2];
-    __shared__ uint32_t s_redo;                                  // columns whose sum is not finite
     if (tid == 0) s_redo = 0;
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
@@ -248,6 +240,13 @@ paged_decode_kernel(PagedAttnDev p) {
         if (g == 0) { sm[wave][c][D] = m_run; sm[wave][c][D + 1] = l_run; }
     }
     __syncthreads();
+    // a piece that begins its span goes to the span's first place, another one (it reaches the span's end) to the second
+    float* piece = SPANS ? p.span_part + ((static_cast<size_t>(hk) * p.spans + span) * 2 + (cur == begin ? 0 : 1)) * (kDecodeCols * part_stride(D)) : nullptr;
+    if (SPANS && hk == 0 && tid == 0 && cur == seq_begin) {
+        // the span of unit x is the last one that begins at or before it
+        const int last = whole ? static_cast<int>(span) : static_cast<int>((static_cast<uint64_t>(seq_end) * static_cast<uint32_t>(spans) - 1) / static_cast<uint32_t>(total));
+        p.pieces[b] = int4{static_cast<int>(span), last - static_cast<int>(span) + 1, cur == begin ? 0 : 1, 0};
+    }
     for (int t = tid; t < min(cols, kDecodeCols) * (D / 2); t += 256) {
         const int r = t / (D / 2), e = 2 * (t % (D / 2));
         float mn = kPagedNone;
@@ -261,90 +260,81 @@ paged_decode_kernel(PagedAttnDev p) {
             n1 += sm[w][r][e + 1] * f;
             den += sm[w][r][D + 1] * f;
         }
-        const int i = r / p.rep, h = hk * p.rep + r - i * p.rep;
         if (n_minus > 0 && fmaf(n0, 0.0f, fmaf(n1, 0.0f, den * 0.0f)) != 0.0f) atomicOr(&s_redo, 1u << r);
-        if (SPLIT && ranges > 1) {
-            float* dst = p.part + (static_cast<size_t>(s.row0 + i) * p.nh + h) * p.n_split * part_stride(D) + static_cast<size_t>(z) * part_stride(D);
+        if (!whole) {
+            float* dst = piece + r * part_stride(D);
             *reinterpret_cast<float2_t*>(dst + e) = float2_t{n0, n1};
-            if (e == 0) *reinterpret_cast<float4_t*>(dst + D) = float4_t{mn, den, static_cast<float>(ranges), 0.0f};
+            if (e == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{mn, den};
         } else {
+            const int i = r / p.rep, h = hk * p.rep + r - i * p.rep;
             const float inv = den != 0.0f ? 1.0f / den : 0.0f;   // a row that sees no key is zero
             *reinterpret_cast<uint32_t*>(p.out + (s.row0 + i) * p.out_stride + h * D + e) = A::pack(n0 * inv, n1 * inv);
-            if (SPLIT && e == 0) p.part[(static_cast<size_t>(s.row0 + i) * p.nh + h) * p.n_split * part_stride(D) + D + 2] = 1.0f;
         }
     }
     // Several queries: a value that is not finite, seen by the later ones, has met the earlier ones' zeros (redo_column).  A single query meets
     // no key that it does not see.
-    if (n_minus == 0) return;
-    __syncthreads();
-    uint32_t redo = s_redo;
-    const int begin = SPLIT ? z * per : 0, end = SPLIT && z < ranges - 1 ? min((z + 1) * per, walk.steps) : walk.steps;
+    if (n_minus > 0) {
+        __syncthreads();
+        uint32_t redo = s_redo;
 #pragma unroll 1
-    for (int j = 0; redo != 0; ++j, redo &= redo - 1) {
-        if ((j & 3) != wave) continue;
-        const int r = __ffs(static_cast<int>(redo)) - 1, i = r / p.rep, h = hk * p.rep + r - i * p.rep;
-        float num[D / 64], m, l;
-        redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + i) * p.q_stride + h * D, s.first + i, begin, end, num, &m, &l);
-        put_column<D, BF16>(p, s.row0 + i, h, z, ranges, num, m, l);
+        for (int j = 0; redo != 0; ++j, redo &= redo - 1) {
+            if ((j & 3) != wave) continue;
+            const int r = __ffs(static_cast<int>(redo)) - 1, i = r / p.rep, h = hk * p.rep + r - i * p.rep;
+            float num[D / 64], m, l;
+            redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + i) * p.q_stride + h * D, s.first + i, first_step, last_step, num, &m, &l);
+            put_column<D, BF16>(num, m, l, whole ? nullptr : piece + r * part_stride(D), p.out + (s.row0 + i) * p.out_stride + h * D);
+        }
+    }
+    if (SPANS && end > seq_end) {
+        cur = seq_end;
+        while (ends[++b] == cur) {}                              // (a later sequence holds unit `cur`)
+        __syncthreads();                                         // the sums have been read
+        goto again;
     }
 }
 
-// Adds the key ranges of a (row, head): one wave each.  The reference point of a range without keys lets it drop out.
+// Adds the pieces of a (sequence, kv head, column): 1024 / D groups of D / 4 lanes take every so manieth piece and meet in LDS.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256)
-paged_combine_kernel(PagedAttnDev p, int T) {
-    const int pair = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (pair >= T * p.nh || pair / p.nh >= p.offs[p.B]) return;
-    constexpr int E = D / 64, W = part_stride(D);
-    const float* src = p.part + static_cast<size_t>(pair) * p.n_split * W;
-    const int ranges = min(static_cast<int>(src[D + 2]), p.n_split);
-    if (ranges <= 1) return;
-    float m = kPagedNone;
-    for (int r = lane; r < ranges; r += 64) m = fmaxf(m, src[static_cast<size_t>(r) * W + D]);
+paged_pieces_kernel(PagedAttnDev p) {
+    constexpr int W = part_stride(D), LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ float4_t nums[GROUPS][LANES];
+    __shared__ float2_t stats[GROUPS];
+    const int hk = blockIdx.x, b = blockIdx.y, r = blockIdx.z, lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int4 at = p.pieces[b];                                 // (of a sequence that is not the decode kernel's: not written, not used)
+    const int row0 = p.offs[b], n = p.offs[b + 1] - row0, cols = n * p.rep;
+    if (n <= 0 || cols > kDecodeCols || r >= cols || at.y <= 1) return;
+    const float* span0 = p.span_part + (static_cast<size_t>(hk) * p.spans + at.x) * (2 * kDecodeCols * W);
+    RangeSum sum;
+    sum.add_all<D>(group, GROUPS, at.y, lane, [&](int z) { return span0 + (static_cast<size_t>(2 * z + (z == 0 ? at.z : 0)) * kDecodeCols + r) * W; });
+    nums[group][lane] = sum.num;
+    if (lane == 0) stats[group] = float2_t{sum.m, sum.den};
+    __syncthreads();
+    if (group != 0) return;
+    float4_t x[GROUPS - 1];
+    float2_t s[GROUPS - 1];
+    bool on[GROUPS - 1];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    float num[E], den = 0.0f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) num[e] = 0.0f;
-#pragma unroll 4
-    for (int r = 0; r < ranges; ++r) {
-        const float* row = src + static_cast<size_t>(r) * W;
-        const float f = __builtin_amdgcn_exp2f(row[D] - m);
-#pragma unroll
-        for (int e = 0; e < E; ++e) num[e] += row[E * lane + e] * f;
-        den += row[D + 1] * f;
-    }
-    const float inv = den != 0.0f ? 1.0f / den : 0.0f;
-    uint16_t* out = p.out + (pair / p.nh) * p.out_stride + (pair % p.nh) * D;
-    if constexpr (E == 2) *reinterpret_cast<uint32_t*>(out + 2 * lane) = Act16<BF16>::pack(num[0] * inv, num[1] * inv);
-    else out[lane] = static_cast<uint16_t>(Act16<BF16>::pack(num[0] * inv, 0.0f) & 0xffffu);
+    for (int k = 0; k < GROUPS - 1; ++k) { x[k] = nums[k + 1][lane]; s[k] = stats[k + 1]; on[k] = k + 1 < at.y; }
+    sum.add<GROUPS - 1>(x, s, on);
+    const int i = r / p.rep, h = hk * p.rep + r - i * p.rep;
+    sum.put<BF16>(p.out + (row0 + i) * p.out_stride + h * D, lane);
 }
 
 template <int D, bool BF16>
 static hipError_t decode_form(const PagedAttnDev& a, hipStream_t stream) {
-    const bool split = a.n_split > 1;
-    // every sequence has a range, and the target is passed by less than one per sequence
-    const dim3 grid(a.nkv, split ? a.B + std::max(a.target / a.nkv, 1) : a.B), block(256);
-    if (split) hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false>), grid, block, 0, stream, a);
+    if (a.spans > 0) {
+        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true>), dim3(a.nkv, a.spans), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_pieces_kernel<D, BF16>), dim3(a.nkv, a.B, a.cols), dim3(256), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false>), dim3(a.nkv, a.B), dim3(256), 0, stream, a);
+    }
     return hipGetLastError();
 }
 
 hipError_t launch_paged_decode(const PagedAttnDev& a, int d, int bf16, hipStream_t stream) {
     if (d == 128) return bf16 ? decode_form<128, true>(a, stream) : decode_form<128, false>(a, stream);
     return bf16 ? decode_form<64, true>(a, stream) : decode_form<64, false>(a, stream);
-}
-
-hipError_t launch_paged_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream) {
-    const dim3 grid((static_cast<int64_t>(T) * a.nh + 3) / 4), block(256);
-    if (d == 128) {
-        if (bf16) hipLaunchKernelGGL((paged_combine_kernel<128, true>), grid, block, 0, stream, a, T);
-        else hipLaunchKernelGGL((paged_combine_kernel<128, false>), grid, block, 0, stream, a, T);
-    } else {
-        if (bf16) hipLaunchKernelGGL((paged_combine_kernel<64, true>), grid, block, 0, stream, a, T);
-        else hipLaunchKernelGGL((paged_combine_kernel<64, false>), grid, block, 0, stream, a, T);
-    }
-    return hipGetLastError();
 }
 
 }  // namespace qtale

@@ -18,7 +18,7 @@
 
 namespace qtale {
 
-constexpr int kTileKeys = 64;
+constexpr int kTileKeys = kChunkTileKeys;
 
 typedef __fp16 fp16x4_t __attribute__((ext_vector_type(4)));
 
@@ -37,8 +37,19 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint32_
 #endif
 }
 
-template <int D, bool BF16, bool SPLIT>
-__global__ void __launch_bounds__(256, 2)
+// Work of a call, in tiles per kv head: the column tiles of a sequence see a number of key tiles that grows evenly from the first to the last.
+__device__ __forceinline__ int chunk_work(const PagedAttnDev& p, int b) {
+    const SeqView s(p, b);
+    const int cols = s.n * p.rep;
+    if (cols == 0 || (p.take != 0 && cols <= kDecodeCols)) return 0;
+    const int nt = (cols + kChunkCols - 1) / kChunkCols;
+    const int least = KeySteps<kTileKeys>(s.first, s.first + (min(kChunkCols, cols) - 1) / p.rep, s.len, p.window, p.sinks).steps;
+    const int most = KeySteps<kTileKeys>(s.first + (nt - 1) * kChunkCols / p.rep, s.first + s.n - 1, s.len, p.window, p.sinks).steps;
+    return nt * (least + most) / 2;
+}
+
+template <int D, bool BF16, bool SPLIT, int KG>
+__global__ void __launch_bounds__(256 * KG, 2)
 paged_chunk_kernel(PagedAttnDev p) {
     using A = Act16<BF16>;
     constexpr int KS = D / 16;                   // k-steps of the scores
@@ -46,10 +57,12 @@ paged_chunk_kernel(PagedAttnDev p) {
     constexpr int CPR = D / 8;                   // 16-byte chunks of a row
     constexpr int RPF = 64 / CPR;                // rows per fetch instruction (1 KB)
     constexpr int NF = 16 / RPF;                 // fetch instructions per wave for 16 keys
-    __shared__ __attribute__((aligned(1024))) uint16_t K0[kTileKeys * D], K1[kTileKeys * D], V0[kTileKeys * D], V1[kTileKeys * D];
+    constexpr int TILE = kTileKeys * D;
+    __shared__ __attribute__((aligned(1024))) uint16_t K0s[KG * TILE], K1s[KG * TILE], V0s[KG * TILE], V1s[KG * TILE];
 
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = KG > 1 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
+    const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) & 3);   // of its group
     const int l32 = lane & 31, lhi = lane >> 5;
 
     // Workgroup -> (range, column tile, kv head).  Ids go round-robin to the 8 XCDs: with a multiple of 8 kv heads each XCD has its own, whose
@@ -130,7 +143,13 @@ paged_chunk_kernel(PagedAttnDev p) {
     const KeySteps<kTileKeys> walk(place_of(c_lo), place_of(c_hi), s.len, p.window, p.sinks);
     int t0 = 0, t1 = walk.steps, ranges = 1;
     if (SPLIT) {
-        const int per = __builtin_amdgcn_readfirstlane(max((walk.steps + p.ranges - 1) / p.ranges, 4));
+        // ranges of about equal length over the whole call, as many as are to run at once; no item is cut into more than p.ranges
+        int work = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 64) work += b0 + lane < p.B ? chunk_work(p, b0 + lane) : 0;
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) work += __shfl_xor(work, x, 64);
+        const int wanted = max(p.target / p.nkv, 1);
+        const int per = __builtin_amdgcn_readfirstlane(max(max((work + wanted - 1) / wanted, (walk.steps + p.ranges - 1) / p.ranges), 4 * KG));
         ranges = __builtin_amdgcn_readfirstlane(max((walk.steps + per - 1) / per, 1));
         if (z >= ranges) return;
         t0 = z * per;
@@ -257,25 +276,55 @@ paged_chunk_kernel(PagedAttnDev p) {
     };
 
     if (t0 < t1) {
-        // page ids are read a tile before the fetch that uses them
-        Ids now = ids_of(t0), next = ids_of(t0 + 1);
-        fetch(t0, now.page, K0, V0);
+        // page ids are read a tile before the fetch that uses them; the groups of waves take every KG-th tile
+        uint16_t *K0 = K0s + group * TILE, *K1 = K1s + group * TILE, *V0 = V0s + group * TILE, *V1 = V1s + group * TILE;
+        const int own = t0 + group;
+        Ids now = ids_of(own), next = ids_of(own + KG);
+        if (own < t1) fetch(own, now.page, K0, V0);
         auto turn = [&](int t, uint16_t* K, uint16_t* V, uint16_t* K_next, uint16_t* V_next) {
             __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): this wave's part of the tile is in LDS
             __syncthreads();                                     // everybody's is, and the other buffers have been read
-            if (t + 1 < t1) fetch(t + 1, next.page, K_next, V_next);
+            if (t + KG < t1) fetch(t + KG, next.page, K_next, V_next);
             const int gone = now.gone;
             now = next;
-            next = ids_of(t + 2);
-            if (wave_live && walk.key(t) <= w_last) compute(t, gone, K, V);
+            next = ids_of(t + 2 * KG);
+            if (wave_live && t < t1 && walk.key(t) <= w_last) compute(t, gone, K, V);
         };
-        for (int t = t0; t < t1; t += 2) {
-            turn(t, K0, V0, K1, V1);
-            if (t + 1 < t1) turn(t + 1, K1, V1, K0, V0);
+        for (int t = t0; t < t1; t += 2 * KG) {
+            turn(t + group, K0, V0, K1, V1);
+            if (t + KG < t1) turn(t + KG + group, K1, V1, K0, V0);
         }
     }
 
-    const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+    float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+    if constexpr (KG > 1) {
+        // the second group's sums go through LDS, in the tiles' buffers, to the first
+        static_assert(KG == 2, "two groups");
+        float4_t* sums = reinterpret_cast<float4_t*>((wave < 2 ? K0s : K1s) + (wave & 1) * TILE) + lane;   // [DF * 4][64 lanes] per wave
+        float2_t* stats = reinterpret_cast<float2_t*>(V0s) + wave * 64 + lane;
+        __syncthreads();
+        if (group == 1) {
+#pragma unroll
+            for (int f = 0; f < DF; ++f)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) sums[(4 * f + q4) * 64] = float4_t{o[f][4 * q4], o[f][4 * q4 + 1], o[f][4 * q4 + 2], o[f][4 * q4 + 3]};
+            *stats = float2_t{m_run, l_tot};
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float2_t other = *stats;
+        const float m = fmaxf(m_run, other[0]), a0 = __builtin_amdgcn_exp2f(m_run - m), a1 = __builtin_amdgcn_exp2f(other[0] - m);
+        m_run = m;
+        l_tot = l_tot * a0 + other[1] * a1;
+#pragma unroll
+        for (int f = 0; f < DF; ++f)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const float4_t x = sums[(4 * f + q4) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[f][4 * q4 + e] = o[f][4 * q4 + e] * a0 + x[e] * a1;
+            }
+    }
     // columns whose sum is not finite (redo_column): both lanes of a column are left out below
     float zero = l_tot * 0.0f;
 #pragma unroll
@@ -290,13 +339,14 @@ paged_chunk_kernel(PagedAttnDev p) {
         const int qj = __shfl(qi, j, 64), hj = __shfl(head, j, 64);
         float num[D / 64], m, l;
         redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + qj) * p.q_stride + hj * D, s.first + qj, t0, t1, num, &m, &l);
-        put_column<D, BF16>(p, s.row0 + qj, hj, z, ranges, num, m, l);
+        const size_t row = s.row0 + qj;
+        put_column<D, BF16>(num, m, l, ranges > 1 ? p.part + ((row * p.nh + hj) * p.ranges + z) * part_stride(D) : nullptr, p.out + row * p.out_stride + hj * D);
     }
     if (c_lo + wave * 32 + l32 > c_hi) return;
     const bool done = (redo >> l32 & 1) != 0;
     const size_t pair = static_cast<size_t>(s.row0 + qi) * p.nh + head;
     if (SPLIT && ranges > 1) {
-        float* dst = p.part + (pair * p.n_split + z) * part_stride(D);
+        float* dst = p.part + (pair * p.ranges + z) * part_stride(D);
         if (lhi == 0) dst[D + 2] = static_cast<float>(ranges);
         if (done) return;
 #pragma unroll
@@ -307,7 +357,7 @@ paged_chunk_kernel(PagedAttnDev p) {
         if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{m_run, l_tot};
         return;
     }
-    if (SPLIT && lhi == 0) p.part[pair * p.n_split * part_stride(D) + D + 2] = 1.0f;
+    if (SPLIT && lhi == 0) p.part[pair * p.ranges * part_stride(D) + D + 2] = 1.0f;
     if (done) return;
     const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;       // a row that sees no key is zero
     uint16_t* orow = p.out + (s.row0 + qi) * p.out_stride + head * D;
@@ -322,76 +372,52 @@ paged_chunk_kernel(PagedAttnDev p) {
         }
 }
 
-// CUs of the current device (queried once per device).
-static int device_cus() {
-    static int cus[64] = {0};
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-    if (cus[dev] == 0) {
-        int n = 0;
-        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-        cus[dev] = n;
-    }
-    return cus[dev];
-}
-
-PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max_new, int max_len) {
-    PagedAttnPlan l{};
-    const int rep = nh / nkv, cus = device_cus();
-    const int64_t most = static_cast<int64_t>(max_new) * rep;
-    // a sequence of few columns has a kernel of its own; both run where the call may hold sequences of either kind
-    l.chunk = most > kDecodeCols;
-    l.decode = !l.chunk || (static_cast<int64_t>(T) < static_cast<int64_t>(B) * max_new && rep <= kDecodeCols);
-    const int live = std::min(B, T);
-    l.items = static_cast<int>((static_cast<int64_t>(T) * rep + static_cast<int64_t>(kChunkCols - 1) * live) / kChunkCols);
-    l.decode_split = l.chunk_split = 1;
-    if (l.decode) {
-        l.target = 3 * cus;
-        if (static_cast<int64_t>(B) * nkv < 2 * cus) {
-            const int ranges = (max_len + kDecodeRangeKeys - 1) / kDecodeRangeKeys;
-            l.decode_split = std::max(std::min({ranges, (l.target + nkv - 1) / nkv, 64}), 1);
-        }
-    }
-    if (l.chunk) {
-        const int64_t wgs = std::max<int64_t>(static_cast<int64_t>(l.items) * nkv, 1);
-        const int tiles = (max_len + kTileKeys - 1) / kTileKeys;
-        if (wgs < 2 * cus) l.chunk_split = static_cast<int>(std::max<int64_t>(std::min<int64_t>({(2 * cus + wgs - 1) / wgs, tiles / 8, 32}), 1));
-    }
-    const int split = std::max(l.decode_split, l.chunk_split);
-    l.too_large = (static_cast<int64_t>(T) * rep + static_cast<int64_t>(kChunkCols - 1) * live) / kChunkCols * nkv * l.chunk_split > INT32_MAX ||
-                  static_cast<int64_t>(T) * nh > INT32_MAX;
-    l.bytes = 256 + (split > 1 ? static_cast<size_t>(T) * nh * split * part_stride(d) * 4 : 0);
-    return l;
-}
-
+// Adds the key ranges of a (row, head) where there are several: D / 4 lanes each.
 template <int D, bool BF16>
+__global__ void __launch_bounds__(256)
+chunk_combine_kernel(PagedAttnDev p, int T) {
+    constexpr int W = part_stride(D), LANES = D / 4;
+    const int pair = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, row = pair / p.nh;
+    if (row >= min(T, p.offs[p.B])) return;
+    const float* src = p.part + static_cast<size_t>(pair) * p.ranges * W;
+    const int ranges = min(static_cast<int>(src[D + 2]), p.ranges);
+    if (ranges <= 1) return;
+    RangeSum sum;
+    sum.add_all<D>(0, 1, ranges, threadIdx.x % LANES, [&](int z) { return src + static_cast<size_t>(z) * W; });
+    sum.put<BF16>(p.out + row * p.out_stride + (pair - row * p.nh) * D, threadIdx.x % LANES);
+}
+
+template <int D, bool BF16, int KG>
 static hipError_t chunk_form(const PagedAttnDev& a, hipStream_t stream) {
-    const bool split = a.n_split > 1;
+    const bool split = a.ranges > 1;
     const int64_t items = static_cast<int64_t>(a.items) * a.ranges;
-    const dim3 grid(static_cast<uint32_t>(items * a.nkv)), block(256);
-    if (split) hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, false>), grid, block, 0, stream, a);
+    const dim3 grid(static_cast<uint32_t>(items * a.nkv)), block(256 * KG);
+    if (split) hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, true, KG>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, false, KG>), grid, block, 0, stream, a);
     return hipGetLastError();
 }
 
-hipError_t launch_paged_chunk(const PagedAttnDev& a, int d, int bf16, hipStream_t stream) {
-    if (d == 128) return bf16 ? chunk_form<128, true>(a, stream) : chunk_form<128, false>(a, stream);
-    return bf16 ? chunk_form<64, true>(a, stream) : chunk_form<64, false>(a, stream);
+template <int D, bool BF16>
+static hipError_t chunk_groups(const PagedAttnDev& a, int groups, hipStream_t stream) {
+    return groups == 2 ? chunk_form<D, BF16, 2>(a, stream) : chunk_form<D, BF16, 1>(a, stream);
 }
 
-hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int bf16, int T, float* workspace, hipStream_t stream) {
-    // both kernels number their ranges in the same partial sums
-    a.n_split = std::max(plan.decode_split, plan.chunk_split);
-    a.items = plan.items;
-    a.take = plan.decode && plan.chunk;
-    a.part = workspace;
-    hipError_t e = hipSuccess;
-    a.ranges = plan.decode_split;
-    a.target = plan.decode_split > 1 ? plan.target : 0;
-    if (plan.decode && (e = launch_paged_decode(a, d, bf16, stream)) != hipSuccess) return e;
-    a.ranges = plan.chunk_split;
-    if (plan.chunk && (e = launch_paged_chunk(a, d, bf16, stream)) != hipSuccess) return e;
-    return a.n_split > 1 ? launch_paged_combine(a, d, bf16, T, stream) : e;
+hipError_t launch_paged_chunk(const PagedAttnDev& a, int groups, int d, int bf16, hipStream_t stream) {
+    if (d == 128) return bf16 ? chunk_groups<128, true>(a, groups, stream) : chunk_groups<128, false>(a, groups, stream);
+    return bf16 ? chunk_groups<64, true>(a, groups, stream) : chunk_groups<64, false>(a, groups, stream);
+}
+
+hipError_t launch_chunk_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream) {
+    const int per = 1024 / d;                                    // (row, head) pairs per workgroup
+    const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(T) * a.nh + per - 1) / per)), block(256);
+    if (d == 128) {
+        if (bf16) hipLaunchKernelGGL((chunk_combine_kernel<128, true>), grid, block, 0, stream, a, T);
+        else hipLaunchKernelGGL((chunk_combine_kernel<128, false>), grid, block, 0, stream, a, T);
+    } else {
+        if (bf16) hipLaunchKernelGGL((chunk_combine_kernel<64, true>), grid, block, 0, stream, a, T);
+        else hipLaunchKernelGGL((chunk_combine_kernel<64, false>), grid, block, 0, stream, a, T);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace qtale

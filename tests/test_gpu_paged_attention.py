@@ -88,6 +88,20 @@ def test_single_tokens_beside_chunks(qt, rep, d, hints):
     _case(qt, torch.bfloat16, rep, 8, d, 32, [1, 300] + [1] * 70, [90, 10] + [(11 * i) % 200 for i in range(70)], hints=hints, seed=rep)
 
 
+@pytest.mark.parametrize("dtype,d,rep,nkv", [(torch.float16, 64, 1, 1), (torch.bfloat16, 128, 4, 2), (torch.float16, 128, 2, 8), (torch.bfloat16, 64, 8, 3)])
+@pytest.mark.parametrize("B", [2, 7, 40, 170])
+def test_spans_that_end_one_sequence_and_begin_the_next(qt, dtype, d, rep, nkv, B):
+    # lengths of nothing, of a few keys and of thousands beside each other: pieces of every kind
+    if B * nkv >= 512:
+        pytest.skip("not cut")
+    old = [(0, 2500, 3, 130, 1, 900, 127, 64, 1400, 300)[i % 10] + i for i in range(B)]
+    new = [0 if i % 9 == 4 else 1 for i in range(B)]
+    _case(qt, dtype, rep, nkv, d, 64, new, old, seed=B)
+    if 2 * rep <= 16:
+        _case(qt, dtype, rep, nkv, d, 16, [min(2 * n, 1 + i % 2) for i, n in enumerate(new)], old, seed=B)
+    _case(qt, dtype, rep, nkv, d, 32, new, old, window=1500, sinks=20, seed=B, gone={(1, 0), (1, 3), (B - 1, 0)})
+
+
 @pytest.mark.parametrize("new,old", [(1, 5000), (2, 9000), (40, 6000), (300, 3000)])
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 def test_one_long_sequence_is_cut(qt, new, old, dtype):
