@@ -365,13 +365,29 @@ int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged
                           void* out, int64_t out_stride, int T, const int32_t* seq_offsets, const int32_t* slots, const int32_t* first,
                           int B, void* workspace, size_t workspace_bytes, void* stream);
 
+/* n_layers layers as in qtale_stack_forward, on a paged cache: layer l of the call uses the cache's layer first_layer + l.  In every layer the
+ * executed tokens get room in their sequences' slots (qtale_pages_reserve), their queries and keys are turned (positions are those of the
+ * tokens), keys and values go to the pages, and the queries attend to what their slot holds, which is executed tokens only.
+ *   kv      fp16, of cfg's kv heads and head size; slots [B] as everywhere (nullable: sequence b is slot b); B <= 2048
+ *   rope    replaces cfg->rope_base;  attn: window, sinks, scale and bounds (max_new: of a call's tokens per sequence; n_heads = cfg->n_heads)
+ *   missing nullable [n_layers] out: pages that the pool could not give in a layer.  Tokens without a place are dropped from that layer's
+ *           cache (their own queries see what is there), as the newest tokens are when a qtale_kv is full.
+ *   workspace >= qtale_paged_stack_workspace_bytes(cfg, kv, T, B) bytes, 256-byte aligned */
+size_t qtale_paged_stack_workspace_bytes(const qtale_layer_cfg* cfg, const qtale_paged_kv* kv, int max_tokens, int max_seqs);
+int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, int n_layers, int first_layer,
+                              void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_paged_kv* kv,
+                              const int32_t* slots /*nullable*/, const qtale_rope* rope, const qtale_paged_attn* attn,
+                              int32_t* missing /*nullable*/, int32_t* sel_idx /*nullable*/, int32_t* sel_count /*nullable*/,
+                              float* scores /*nullable*/, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing with HIP events recorded on the forward call's stream.  While enabled, every
  * layer/stack forward brackets its kernels with events; qtale_profile_read waits for them and
  * returns, per kernel class, accumulated milliseconds and launch counts since the last read.
  * Classes: 0 router, 1 select, 2 norm1, 3 qkv gemm, 4 rope+append, 5 attention, 6 o gemm, 7 norm2,
  * 8 gate/up gemm, 9 down gemm.  Small calls fuse some of them, and a fused step is counted in the class of the launch that
  * does it: up to 256 tokens class 2 is part of 1; with a cache and few new tokens per sequence (decode) class 4 is part
- * of 5, so that a bandwidth made from class 5 includes the rotation and the append (otherwise 4 also builds the work list of 5);
+ * of 5, so that a bandwidth made from class 5 includes the rotation and the append (otherwise 4 also builds the work list of 5;
+ * on a paged cache it is always 4, with the pages' room);
  * with at most four tokens 0 (unless the
  * router is an MLP), 1 and 2 are part of 3, and 7 is part of 8.  Inside a stack a decode-sized layer's class 9 also scores the
  * next layer's tokens (its class 0).  Profiling adds event overhead; leave it off when timing whole steps. */

@@ -28,7 +28,8 @@ EXPORTS = ["qtale_strerror", "qtale_create", "qtale_destroy", "qtale_set_exec_ra
            "qtale_static_scratch_bytes", "qtale_layer_forward_static",
            "qtale_pages_init", "qtale_pages_workspace_bytes", "qtale_pages_fork", "qtale_pages_reserve", "qtale_pages_release",
            "qtale_pages_trim", "qtale_pages_compact", "qtale_pages_copy", "qtale_rope_frequencies", "qtale_paged_rope_append",
-           "qtale_paged_attention_workspace_bytes", "qtale_paged_attention"]
+           "qtale_paged_attention_workspace_bytes", "qtale_paged_attention", "qtale_paged_stack_workspace_bytes",
+           "qtale_paged_stack_forward"]
 QTALE_THETA_GRID = 50
 QTALE_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 QTALE_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "parts": 4}
@@ -144,10 +145,15 @@ def load_library():
     lib.qtale_paged_attention_workspace_bytes.argtypes = [pk, C.POINTER(qtale_paged_attn), i, i]
     lib.qtale_paged_attention_workspace_bytes.restype = sz
     lib.qtale_paged_attention.argtypes = [pk, i, C.POINTER(qtale_paged_attn), vp, i64, vp, i64, i, vp, vp, vp, i, vp, sz, vp]
+    lib.qtale_paged_stack_workspace_bytes.argtypes = [C.POINTER(qtale_layer_cfg), pk, i, i]
+    lib.qtale_paged_stack_workspace_bytes.restype = sz
+    lib.qtale_paged_stack_forward.argtypes = [vp, C.POINTER(qtale_layer_cfg), C.POINTER(qtale_layer_weights), i, i, vp, i, vp, i, vp, pk, vp,
+                                              C.POINTER(qtale_rope), C.POINTER(qtale_paged_attn), vp, vp, vp, vp, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("qtale_strerror", "qtale_prepacked_bytes", "qtale_workspace_bytes",
                         "qtale_calibration_scratch_bytes", "qtale_graph_destroy", "qtale_static_scratch_bytes",
-                        "qtale_pages_workspace_bytes", "qtale_paged_attention_workspace_bytes"):
+                        "qtale_pages_workspace_bytes", "qtale_paged_attention_workspace_bytes",
+                        "qtale_paged_stack_workspace_bytes"):
             getattr(lib, name).restype = i
     _lib = lib
     return lib
@@ -664,6 +670,28 @@ def qtale_paged_attention(kv, layer, q, seq_offsets, first=None, slots=None, out
         kv._ref, layer, C.byref(attn), *_heads(q, kv, T, nh), *_heads(out, kv, T, nh), T, _ints(seq_offsets, kv, B + 1), _ints(slots, kv, B),
         _ints(first, kv, B), B, *_scratch(workspace, kv), _stream_of(kv)), "qtale_paged_attention")
     return out
+
+
+def alloc_paged_stack_workspace(cfg, kv, max_tokens, max_seqs):
+    n = load_library().qtale_paged_stack_workspace_bytes(C.byref(cfg), kv._ref, max_tokens, max_seqs)
+    if n == 0:
+        raise QtaleError(-1, "qtale_paged_stack_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=kv.device)
+
+
+def qtale_paged_stack_forward(ctx, stack, x, seq_offsets, positions, kv, rope, slots=None, window=0, sinks=0, scale=None, max_new=0, max_len=0,
+                              first_layer=0, missing=None, sel_idx=None, sel_count=None, scores=None, workspace=None):
+    """qtale_stack_forward on a paged cache (layer l of the stack is the cache's layer first_layer + l); the stack has no caches of its own."""
+    T = x.shape[0]
+    B = seq_offsets.numel() - 1
+    assert stack.kvs is None and rope.freqs.device == kv.device and x.device == kv.device and x.is_contiguous()
+    if workspace is None:
+        workspace = alloc_paged_stack_workspace(stack.cfg, kv, T, B)
+    attn = _paged_attn(kv, stack.cfg.n_heads, max_new, max_len, window, sinks, scale)
+    _check(load_library().qtale_paged_stack_forward(
+        ctx._h, C.byref(stack.cfg), stack._w, stack.n, first_layer, x.data_ptr(), T, _ints(seq_offsets, kv, B + 1), B, _ints(positions, kv, T),
+        kv._ref, _ints(slots, kv, B), rope._ref, C.byref(attn), _ints(missing, kv, stack.n), _ptr(sel_idx), _ptr(sel_count), _ptr(scores),
+        *_scratch(workspace, kv), _stream_of(kv)), "qtale_paged_stack_forward")
 
 
 def qtale_profile_enable(ctx, on):

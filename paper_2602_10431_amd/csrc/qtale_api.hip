@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/qtale.h"
+#include "paged_check.h"
 #include "qtale_kernels.h"
 
 using namespace qtale;
@@ -209,10 +210,51 @@ bool fits_cache(const qtale_layer_cfg* c, const qtale_layer_weights* layers, int
     return bytes <= (size_t{256} << 20);
 }
 
+// A layer call on a paged cache: one layer of it, and where its own scratch lies.
+struct PagedCall {
+    PagedDev cache;                             // all layers
+    int layer;
+    const qtale_paged_kv* kv;
+    const qtale_paged_attn* attn;
+    const qtale_rope* rope;
+    const int32_t* slots;
+    int32_t* missing;                           // nullable
+    void* pages_ws;
+    float* attn_ws;
+};
+
+// Room for the executed tokens, rotary embedding and append, attention: in place on the compact q|k|v rows.
+int paged_attention_block(qtale_ctx* ctx, const qtale_layer_cfg* c, const PagedCall& pc, const Workspace& ws, int M_max, int B,
+                          const int32_t* positions, hipStream_t stream) {
+    const int nh = c->n_heads, nkv = c->n_kv_heads, d = c->head_dim, width = (nh + 2 * nkv) * d;
+    uint16_t* qkv = reinterpret_cast<uint16_t*>(ws.qkv);
+    {
+        Prof pr(ctx, stream, 4);
+        HIP_TRY(launch_pages_reserve(pc.cache, pc.layer, ws.cu_exec, pc.slots, B, ws.kv_old, pc.missing, pc.pages_ws, stream));
+        PagedRopeArgs r{};
+        r.kv = paged_device(pc.kv, pc.layer);
+        r.layout = pc.rope->layout; r.rotary_dim = pc.rope->rotary_dim; r.freqs = pc.rope->freqs; r.magnitude = pc.rope->magnitude;
+        r.q = r.q_out = qkv; r.k = qkv + nh * d; r.v = qkv + (nh + nkv) * d;
+        r.q_stride = r.k_stride = r.v_stride = r.q_out_stride = width;
+        r.nh = nh; r.T = M_max; r.B = B; r.seq_offsets = ws.cu_exec; r.slots = pc.slots; r.first = ws.kv_old; r.positions = positions;
+        r.rows = ws.idx; r.count = ws.scalars;
+        HIP_TRY(launch_paged_rope(r, stream));
+    }
+    Prof pr(ctx, stream, 5);
+    const PagedAttnBounds m = attn_bounds(pc.attn, pc.kv, M_max);
+    const PagedAttnPlan plan = plan_paged_attention(nh, nkv, d, M_max, B, m.max_new, m.max_len, pc.attn->window, pc.attn->sinks);
+    if (plan.too_large) return QTALE_ERR_UNSUPPORTED;
+    PagedAttnDev a = attn_device(pc.kv, pc.layer, pc.attn, m);
+    a.q = qkv; a.q_stride = width; a.out = reinterpret_cast<uint16_t*>(ws.attn); a.out_stride = nh * d;
+    a.offs = ws.cu_exec; a.slots = pc.slots; a.first = ws.kv_old; a.B = B;
+    HIP_TRY(launch_paged_attention(a, plan, d, 0, M_max, pc.attn_ws, stream));
+    return QTALE_OK;
+}
+
 int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_layer_weights* w, void* x, int T,
                        const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_kv* kv,
                        int32_t* sel_idx, int32_t* sel_count, float* scores, const Workspace& ws,
-                       hipStream_t stream, LayerLink* link = nullptr) {
+                       hipStream_t stream, LayerLink* link = nullptr, const PagedCall* paged = nullptr) {
     const int bf16 = c->act_dtype == QTALE_ACT_BF16;
     const int H = c->hidden, nh = c->n_heads, nkv = c->n_kv_heads, d = c->head_dim, I = c->inter;
     const int ratio_mode = ctx->mode == QTALE_MODE_RATIO;
@@ -314,7 +356,10 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
     // the o-proj: the buffers from h to the parts of the GEMMs, which adjoin (the ranges' counters first)
     AttnList list{};
     float* a_part = ws.attn_part;
-    if (!decode_attn) {
+    if (paged) {
+        const int e = paged_attention_block(ctx, c, *paged, ws, M_max, B, positions, stream);
+        if (e) return e;
+    } else if (!decode_attn) {
         const size_t counters = align_up((static_cast<size_t>(M_max) / kAttnBQ + B + 1) * nh * 4, 256);
         const size_t room = static_cast<size_t>(reinterpret_cast<char*>(ws.inv) - reinterpret_cast<char*>(ws.h));
         list = attention_prefill_plan(M_max, B, nh, d, kv ? kv->cap : M_max, room > counters ? (room - counters) / 4 : 0);
@@ -323,7 +368,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
         list.arrive = reinterpret_cast<int32_t*>(ws.h);
         a_part = reinterpret_cast<float*>(reinterpret_cast<char*>(ws.h) + counters);
     }
-    if (!attn_rotates) {
+    if (!paged && !attn_rotates) {
         Prof pr(ctx, stream, 4);
         RopeArgs r{};
         r.qkv = ws.qkv; r.nh = nh; r.nkv = nkv; r.d = d; r.base = c->rope_base;
@@ -332,7 +377,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
         r.row_seq = ws.row_seq; r.cu_exec = ws.cu_exec; r.kv_old = ws.kv_old; r.list = list;
         HIP_TRY(launch_rope_append(r, stream));
     }
-    {
+    if (!paged) {
         Prof pr(ctx, stream, 5);
         AttnArgs a{};
         a.qkv = ws.qkv; a.out = ws.attn; a.nh = nh; a.nkv = nkv; a.d = d; a.count = count; a.max_rows = M_max;
@@ -640,6 +685,56 @@ int qtale_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_
                                sel_idx ? sel_idx + static_cast<size_t>(l) * T : nullptr,
                                sel_count ? sel_count + l : nullptr,
                                scores ? scores + static_cast<size_t>(l) * T : nullptr, ws, s, &link);
+        if (e) return e;
+        scores_ready = link.next_scored;
+    }
+    return QTALE_OK;
+}
+
+size_t qtale_paged_stack_workspace_bytes(const qtale_layer_cfg* cfg, const qtale_paged_kv* kv, int max_tokens, int max_seqs) {
+    if (check_cfg(cfg) || check_paged(kv, false) || max_tokens < 0 || max_seqs < 0 || max_seqs > kReserveItems) return 0;
+    return carve(cfg, max_tokens, max_seqs, nullptr).total + pages_workspace_bytes(paged_device(kv, -1), max_seqs) +
+           paged_attention_bytes(cfg->n_heads, cfg->n_kv_heads, cfg->head_dim, max_tokens, max_seqs);
+}
+
+int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, int n_layers, int first_layer,
+                              void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_paged_kv* kv,
+                              const int32_t* slots, const qtale_rope* rope, const qtale_paged_attn* attn, int32_t* missing,
+                              int32_t* sel_idx, int32_t* sel_count, float* scores, void* workspace, size_t workspace_bytes, void* stream) {
+    int e = check_forward_args(ctx, cfg, x, T, seq_offsets, B, positions, workspace, workspace_bytes);
+    if (e) return e;
+    if ((e = check_paged(kv, true)) || (e = check_rope(rope, cfg->head_dim)) || (e = check_paged_attn(attn, kv))) return e;
+    if (n_layers < 0 || first_layer < 0 || (n_layers > 0 && !layers)) return QTALE_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(first_layer) + n_layers > kv->n_layers) return QTALE_ERR_SHAPE;
+    if (kv->dtype != QTALE_ACT_FP16) return QTALE_ERR_UNSUPPORTED;   // q, k and v of a layer are fp16
+    if (kv->n_kv_heads != cfg->n_kv_heads || kv->head_dim != cfg->head_dim || attn->n_heads != cfg->n_heads) return QTALE_ERR_SHAPE;
+    if (B > kReserveItems) return QTALE_ERR_UNSUPPORTED;
+    if (!slots && B > kv->n_slots) return QTALE_ERR_SHAPE;
+    for (int l = 0; l < n_layers; ++l)
+        if ((e = check_weights(cfg, &layers[l]))) return e;
+    if (T == 0) return QTALE_OK;
+    if (workspace_bytes < qtale_paged_stack_workspace_bytes(cfg, kv, T, B)) return QTALE_ERR_WORKSPACE_TOO_SMALL;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const Workspace ws = carve(cfg, T, B, workspace);
+    PagedCall pc{};
+    pc.cache = paged_device(kv, -1);
+    pc.kv = kv; pc.attn = attn; pc.rope = rope; pc.slots = slots;
+    pc.pages_ws = reinterpret_cast<char*>(workspace) + ws.total;
+    pc.attn_ws = reinterpret_cast<float*>(reinterpret_cast<char*>(pc.pages_ws) + pages_workspace_bytes(pc.cache, B));
+    bool scores_ready = false;
+    const bool cached = fits_cache(cfg, layers, n_layers);
+    for (int l = 0; l < n_layers; ++l) {
+        LayerLink link;
+        link.scores_ready = scores_ready;
+        link.cached = cached;
+        if (l + 1 < n_layers) {
+            link.next = &layers[l + 1];
+            link.next_z = scores ? scores + static_cast<size_t>(l + 1) * T : ws.z;
+        }
+        pc.layer = first_layer + l;
+        pc.missing = missing ? missing + l : nullptr;
+        e = layer_forward_impl(ctx, cfg, &layers[l], x, T, seq_offsets, B, positions, nullptr, sel_idx ? sel_idx + static_cast<size_t>(l) * T : nullptr,
+                               sel_count ? sel_count + l : nullptr, scores ? scores + static_cast<size_t>(l) * T : nullptr, ws, s, &link, &pc);
         if (e) return e;
         scores_ready = link.next_scored;
     }

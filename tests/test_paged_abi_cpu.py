@@ -182,3 +182,30 @@ def test_frequencies_refuse(qt):
         assert call(how=how, factor=2.0, n=10, low=0.0, high=4.0) == -1
         assert call(how=how, factor=2.0, n=10, low=4.0, high=4.0) == -1
     assert call(how=4, base=1.0, factor=2.0, n=10, low=1.0, high=4.0) == -1
+
+
+def test_paged_stack_refuses(qt):
+    lib = qt.load_library()
+    ctx = qt.Context()
+    cfg = qt.make_cfg(256, 8, 4, 128, 512, group=32, act_dtype="fp16")
+    w = qt.qtale_layer_weights()
+    size = lib.qtale_paged_stack_workspace_bytes(C.byref(cfg), _kv(qt), 4, 2)
+    assert size > qt.qtale_workspace_bytes(cfg, 4, 2)
+    assert lib.qtale_paged_stack_workspace_bytes(C.byref(cfg), _kv(qt, page_size=8), 4, 2) == 0
+    assert lib.qtale_paged_stack_workspace_bytes(C.byref(cfg), _kv(qt), 4, 2049) == 0
+
+    def call(cfg_=cfg, kv=None, layers=True, n=1, first=0, x=FAKE, T=4, offs=FAKE, B=2, pos=FAKE, slots=FAKE, rope=(0, 64, 256, 1.0),
+             attn=(8, 0, 0, 0.1, 1, 0), work=FAKE, room=size):
+        return lib.qtale_paged_stack_forward(ctx._h, C.byref(cfg_), C.byref(w) if layers else None, n, first, x, T, offs, B, pos, kv or _kv(qt), slots,
+                                             None if rope is None else C.byref(qt.qtale_rope(*rope)), None if attn is None else C.byref(qt.qtale_paged_attn(*attn)),
+                                             None, None, None, None, work, room, None)
+
+    assert call() == -1                                          # weights without prepacked buffers
+    assert call(n=0) == 0 and call(T=0) == -1 and call(T=0, n=0) == 0
+    assert call(layers=False) == -1 and call(n=-1) == -1 and call(first=-1) == -1 and call(first=3) == -2 and call(first=2, n=2) == -2
+    for missing in ("x", "offs", "pos", "work"):
+        assert call(**{missing: None}) == -1
+    assert call(rope=None) == -1 and call(rope=(0, 200, 256, 1.0)) == -2 and call(attn=None) == -1 and call(attn=(8, 0, 0, 0.0, 1, 0)) == -1
+    assert call(attn=(4, 0, 0, 0.1, 1, 0)) == -2 and call(kv=_kv(qt, n_kv_heads=8)) == -2 and call(kv=_kv(qt, head_dim=64)) == -2
+    assert call(kv=_kv(qt, dtype=1)) == -3 and call(kv=_kv(qt, table=None)) == -1 and call(B=0) == -1 and call(slots=None, B=7, room=1 << 40) == -2
+    assert call(B=3000, room=1 << 40) == -3 and call(room=16) == -4
