@@ -75,12 +75,13 @@ struct PagedAttnDev {
 struct PagedAttnPlan {
     bool decode, chunk;          // which kernels run
     int spans;                   // decode
-    int ranges, target, groups, items;   // chunk; groups of waves per workgroup
+    int ranges, target, groups, items;   // chunk; groups of waves per workgroup that share its keys, 0: the wide form
     bool too_large;              // more workgroups than a grid has
     size_t decode_bytes, bytes;  // of workspace: the decode kernel's, all
 };
 constexpr int kDecodeCols = 16;                  // (query, head) pairs per kv head that the decode kernel holds
 constexpr int kChunkCols = 128;                  // ... and a workgroup of the chunk kernel
+constexpr int kWideCols = 256;                   // ... of its form with two halves that take turns
 constexpr int kChunkTileKeys = 64;
 constexpr int kSpanSeqs = 1024;                  // bound on the sequences of a call that is cut into spans
 constexpr int part_stride(int d) { return d + 4; }   // floats of a column's sums: numerators, reference point, denominator, (chunk) ranges, unused

@@ -38,19 +38,28 @@ PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max
     // 40 x 700 27.0 / 27.6, 40 x 2200 81 / 69, 60 x 2200 94.6 / 96.6, 60 x 12000 495 / 448; heads of 64 8 x 1500 13.2 / 13.6.
     const int64_t pairs = static_cast<int64_t>(B) * nkv, filled = (pairs + cus - 1) / cus * cus;
     if (l.decode && B <= kSpanSeqs && pairs < 2 * cus && seen * d / 128 * (10 * filled - 9 * pairs) > 8000 * filled) l.spans = decode_spans(nkv, d);
-    const int64_t items = (static_cast<int64_t>(T) * rep + static_cast<int64_t>(kChunkCols - 1) * std::min(B, T)) / kChunkCols;
+    int64_t items = (static_cast<int64_t>(T) * rep + static_cast<int64_t>(kChunkCols - 1) * std::min(B, T)) / kChunkCols;
     l.ranges = l.groups = 1;
     if (l.chunk) {
         // Few column tiles: where cutting their keys into ranges saves more than adding the ranges costs (about 24 tiles of time), ranges for
-        // two workgroups per CU; else two groups of waves per workgroup, which share a tile's keys.  us, ranges / groups / neither: heads of 128,
-        // 4 per kv head, 500 rows on 24000 keys 218 / 393 / -, 2 x 300 on 2000 59 / 61 / -, 1500 on 0 50 / 35 / 44; heads of 64 2 x 700 on 1400
-        // 52 / 45 / 58, 1500 on 0 30 / 24 / 34; one head per kv head, 200 on 3000 33 / 57 / -; 4 x 4096 - / 751 / 637.
+        // two workgroups per CU; else, where the tiles fill less than 7/8 of the CUs' places, two groups of waves per workgroup, which share a
+        // tile's keys.  us, ranges / groups / neither: heads of 128, 4 per kv head, 500 rows on 24000 keys 218 / 393 / -, 2 x 300 on 2000
+        // 59 / 61 / -, 1500 on 0 50 / 35 / 44, 1000 on 0 - / 23.6 / 27.3; heads of 64 2 x 700 on 1400 52 / 45 / 58, 1500 on 0 30 / 24 / 34; one
+        // head per kv head, 200 on 3000 33 / 57 / -, 40 heads 2 x 700 on 1000 - / 68 / 58; 4 x 4096 - / 704 / 603.
         const int64_t wgs = std::max<int64_t>(items * nkv, 1), tiles = (seen + kChunkTileKeys - 1) / kChunkTileKeys, two = 2 * cus;
+        // Many and long: the wide form, if its workgroups, one per CU at a time, end together.  us, it / chunk kernel: heads of 128, 4 per kv
+        // head, 4 x 4096 574 / 603, 1 x 4096 133 / 144, 2 x 2048 88 / 92, 3 x 750 to 2250 104 / 97, 8 x 512 52 / 48; one per kv head
+        // 4 x 1000 75 / 67; under a window of 1000 99 / 81; heads of 64 4 x 4096 411 / 326.
+        const int64_t wide = (static_cast<int64_t>(T) * rep + static_cast<int64_t>(kWideCols - 1) * std::min(B, T)) / kWideCols;
+        const int64_t rounds = (wide * nkv + cus - 1) / cus;
         if (tiles * (two - wgs) > 24 * two) {
             l.target = static_cast<int>(two);
             l.ranges = static_cast<int>(std::max<int64_t>(std::min<int64_t>({2 * ((two + wgs - 1) / wgs), tiles / 8, 32}), 1));
-        } else if (wgs < (d == 64 ? 4 : 2) * cus && tiles >= 8) {
+        } else if (8 * wgs < (d == 64 ? 28 : 14) * cus && tiles >= 8) {
             l.groups = 2;
+        } else if (d == 128 && tiles >= 32 && rounds >= 2 && (rounds >= 6 || 8 * wide * nkv >= 7 * cus * rounds)) {
+            l.groups = 0;
+            items = wide;
         }
     }
     l.items = static_cast<int>(std::min<int64_t>(items, INT32_MAX));

@@ -143,6 +143,33 @@ def test_missing_pages_anywhere(qt, new):
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_long_chunks(qt, dtype):
+    # enough column tiles and keys for the workgroups whose halves take turns: even and odd numbers of tiles, a last tile with few columns, missing
+    # pages, a window, a page per tile and several
+    _case(qt, dtype, 16, 8, 128, 64, [1400, 907, 300], [1000, 1201, 64], gone={(0, 5), (1, 30)}, seed=1)
+    _case(qt, dtype, 4, 8, 128, 16, [2048, 2048], [0, 0], seed=2)
+    _case(qt, dtype, 16, 8, 128, 128, [1333, 1300], [2100, 900], window=2300, sinks=5, seed=3)
+
+
+def test_a_long_chunk_with_a_value_that_is_not_finite(qt):
+    nkv, rep, d, page, new, old = 8, 16, 128, 64, [1400, 1200], [900, 10]
+    kv, slots = random_cache(qt, [o + n for o, n in zip(old, new)], page, nkv, d, torch.float16, 12)
+    q = torch.randn(sum(new), rep * nkv, d, device="cuda").half()
+    kw = dict(first=ints(old), slots=ints(slots), max_new=1400, max_len=2300)
+    clean = qt.qtale_paged_attention(kv, 0, q, offsets(new), **kw)
+    at = old[0] + 700                                            # a new token's value: rows before it do not see it
+    kv.v[int(kv.table[0, slots[0], at // page]), 2, at % page, 7] = float("nan")
+    got = qt.qtale_paged_attention(kv, 0, q, offsets(new), **kw)
+    hit = torch.zeros_like(got, dtype=torch.bool)
+    hit[700:1400, 2 * rep: 3 * rep, 7] = True
+    assert bool(torch.isnan(got[hit]).all())
+    # rows in a tile with it are done again key by key: equal within what two such results may differ
+    size = torch.ones_like(clean).double()
+    assert bool(((got.double() - clean.double()).abs() <= 2 * attention_bound(clean.double(), size, torch.float16, False))[~hit].all())
+    assert torch.equal(got[1400:], clean[1400:])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("new,old", [([3, 4, 2], [60, 5, 700]), ([60, 33, 40], [70, 0, 700]), ([3, 4, 2], [60, 5, 9000])])
 def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(qt, dtype, value, new, old):
