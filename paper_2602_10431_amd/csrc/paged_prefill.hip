@@ -432,6 +432,9 @@ paged_chunk_kernel(PagedAttnDev p) {
             turn(t + group, K0, V0, K1, V1);
             if (t + KG < t1) turn(t + KG + group, K1, V1, K0, V0);
         }
+        // the last turn's requests are past the range and bring zeros; they have to be in LDS before a sum takes their place or the
+        // workgroup's LDS goes to another
+        __builtin_amdgcn_s_waitcnt(0x0f70);
     }
 
     float l_tot = cw.l_run + __shfl_xor(cw.l_run, 32, 64);
