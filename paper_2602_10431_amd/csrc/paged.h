@@ -69,12 +69,13 @@ struct PagedAttnDev {
     // decode kernel: spans per kv head that the call's keys are cut into (0: a workgroup per sequence), the sums of a span's first and last
     // piece [nkv][spans][2][kDecodeCols][part_stride(d)], and where a sequence's pieces are: [B] (first span, pieces, place of the first, -)
     int spans, cols;             // cols: bound on a sequence's columns
+    int stream_keys;             // without spans: non-temporal keys
     float* span_part;
     int4* pieces;
 };
 struct PagedAttnPlan {
     bool decode, chunk;          // which kernels run
-    int spans;                   // decode
+    int spans, stream_keys;      // decode
     int ranges, target, groups, items;   // chunk; groups of waves per workgroup that share its keys, 0: the wide form
     bool too_large;              // more workgroups than a grid has
     size_t decode_bytes, bytes;  // of workspace: the decode kernel's, all

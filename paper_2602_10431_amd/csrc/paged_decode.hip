@@ -29,7 +29,10 @@ __device__ __forceinline__ int seq_units(const PagedAttnDev& p, int b) {
     return max((KeySteps<kStepKeys>(s.first, s.first + s.n - 1, s.len, p.window, p.sinks).steps + kUnitSteps - 1) / kUnitSteps, 1);
 }
 
-template <int D, bool BF16, bool SPANS>
+// STREAM: keys as non-temporal loads too, not only values.  Where the workgroups fill the chip evenly (spans, or many of them) the stream gains, us
+// without / with: 33 x 3000 keys of 8 kv heads 74 / 69, 20 x 6000 85 / 80, heads of 64 49 / 47; 64 x 2048 of 32 kv heads 324 / 313, 128 x 1000 of 8
+// 81.7 / 79.3; where some CUs are left with one workgroup more than others those have less of it each: 48 x 1028 37.6 / 40.8, 100 x 2000 139 / 142.
+template <int D, bool BF16, bool SPANS, bool STREAM>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : 3)
 paged_decode_kernel(PagedAttnDev p) {
     using A = Act16<BF16>;
@@ -118,7 +121,7 @@ again:                                                           // the pieces o
         for (int u = 0; u < 2; ++u) {
             const auto buf = buffer(p.k, u ? id.b : id.a, kb + 16 * u);
 #pragma unroll
-            for (int k = 0; k < S; ++k) kn[u][k] = __builtin_amdgcn_raw_buffer_load_b128(buf, k_off + 64 * k, 0, 0);
+            for (int k = 0; k < S; ++k) kn[u][k] = __builtin_amdgcn_raw_buffer_load_b128(buf, k_off + 64 * k, 0, STREAM ? 2 : 0);
         }
     };
     auto fetch_v = [&](int kb, Ids id) {
@@ -324,10 +327,12 @@ paged_pieces_kernel(PagedAttnDev p) {
 template <int D, bool BF16>
 static hipError_t decode_form(const PagedAttnDev& a, hipStream_t stream) {
     if (a.spans > 0) {
-        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true>), dim3(a.nkv, a.spans), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true, true>), dim3(a.nkv, a.spans), dim3(256), 0, stream, a);
         hipLaunchKernelGGL((paged_pieces_kernel<D, BF16>), dim3(a.nkv, a.B, a.cols), dim3(256), 0, stream, a);
+    } else if (D == 128 && a.stream_keys) {
+        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false, D == 128>), dim3(a.nkv, a.B), dim3(256), 0, stream, a);
     } else {
-        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false>), dim3(a.nkv, a.B), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false, false>), dim3(a.nkv, a.B), dim3(256), 0, stream, a);
     }
     return hipGetLastError();
 }

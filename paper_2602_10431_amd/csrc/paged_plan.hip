@@ -38,6 +38,7 @@ PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max
     // 40 x 700 27.0 / 27.6, 40 x 2200 81 / 69, 60 x 2200 94.6 / 96.6, 60 x 12000 495 / 448; heads of 64 8 x 1500 13.2 / 13.6.
     const int64_t pairs = static_cast<int64_t>(B) * nkv, filled = (pairs + cus - 1) / cus * cus;
     if (l.decode && B <= kSpanSeqs && pairs < 2 * cus && seen * d / 128 * (10 * filled - 9 * pairs) > 8000 * filled) l.spans = decode_spans(nkv, d);
+    l.stream_keys = pairs >= 4 * cus;
     int64_t items = (static_cast<int64_t>(T) * rep + static_cast<int64_t>(kChunkCols - 1) * std::min(B, T)) / kChunkCols;
     l.ranges = l.groups = 1;
     if (l.chunk) {
@@ -78,7 +79,7 @@ size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B) {
 hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int bf16, int T, float* workspace, hipStream_t stream) {
     a.take = plan.decode && plan.chunk;
     a.items = plan.items; a.ranges = plan.ranges; a.target = plan.target;
-    a.spans = plan.spans; a.cols = kDecodeCols < T * a.rep ? kDecodeCols : T * a.rep;
+    a.spans = plan.spans; a.stream_keys = plan.stream_keys; a.cols = kDecodeCols < T * a.rep ? kDecodeCols : T * a.rep;
     char* at = reinterpret_cast<char*>(workspace);
     a.pieces = reinterpret_cast<int4*>(at);
     a.span_part = reinterpret_cast<float*>(at + (static_cast<size_t>(std::min(a.B, kSpanSeqs)) * sizeof(int4) + 255) / 256 * 256);
