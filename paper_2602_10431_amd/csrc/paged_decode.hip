@@ -243,6 +243,11 @@ again:                                                           // the pieces o
         if (g == 0) { sm[wave][c][D] = m_run; sm[wave][c][D + 1] = l_run; }
     }
     __syncthreads();
+    // the launch that adds the chunk kernel's key ranges finds none in these rows
+    if (p.take != 0 && p.ranges > 1 && (!SPANS || cur == seq_begin) && tid < cols) {
+        const int i = tid / p.rep;
+        p.part[((static_cast<size_t>(s.row0 + i) * p.nh + hk * p.rep + tid - i * p.rep) * p.ranges) * part_stride(D) + D + 2] = 0.0f;
+    }
     // a piece that begins its span goes to the span's first place, another one (it reaches the span's end) to the second
     float* piece = SPANS ? p.span_part + ((static_cast<size_t>(hk) * p.spans + span) * 2 + (cur == begin ? 0 : 1)) * (kDecodeCols * part_stride(D)) : nullptr;
     if (SPANS && hk == 0 && tid == 0 && cur == seq_begin) {

@@ -88,6 +88,20 @@ def test_single_tokens_beside_chunks(qt, rep, d, hints):
     _case(qt, torch.bfloat16, rep, 8, d, 32, [1, 300] + [1] * 70, [90, 10] + [(11 * i) % 200 for i in range(70)], hints=hints, seed=rep)
 
 
+@pytest.mark.parametrize("left", [0.0, 2.0, 1e30, float("nan")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_a_workspace_held_does_not_show(qt, d, left):
+    # single tokens beside a chunk whose keys are cut: a workspace that other calls have used
+    rep, nkv, new, old = 4, 2, [1, 300, 1, 2, 0, 45] + [1] * 12, [900, 10, 0, 31, 5, 2600] + [70] * 12
+    nh, lens, T, B = rep * nkv, [o + n for o, n in zip(old, new)], sum(new), len(new)
+    kv, slots = random_cache(qt, lens, 64, nkv, d, torch.float16, 3)
+    q = torch.randn(T, nh, d, generator=torch.Generator().manual_seed(4)).half().cuda()
+    workspace = qt.alloc_paged_workspace(kv, nh, T, B, max(new))
+    workspace.view(torch.float32).fill_(left)
+    out = qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), max_new=max(new), max_len=4096, workspace=workspace)
+    _compare(kv, 0, q, out, new, old, slots, 0, 0, d ** -0.5, False)
+
+
 @pytest.mark.parametrize("dtype,d,rep,nkv", [(torch.float16, 64, 1, 1), (torch.bfloat16, 128, 4, 2), (torch.float16, 128, 2, 8), (torch.bfloat16, 64, 8, 3)])
 @pytest.mark.parametrize("B", [2, 7, 40, 170])
 def test_spans_that_end_one_sequence_and_begin_the_next(qt, dtype, d, rep, nkv, B):
