@@ -5,7 +5,9 @@
 
 namespace qtale {
 
-constexpr float kPagedNone = -1.0e30f;           // reference point of a row that has seen no key
+// Reference points of softmax sums are scores before their scale, so that the largest score less itself is zero whatever its size (scaled scores
+// would be rounded first, and at 10^10 by more than an exponent has room for).  This one is a row's that has seen no key.
+constexpr float kPagedNone = -3.0e38f;
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -108,10 +110,10 @@ __device__ void redo_column(const PagedAttnDev& p, const KeySteps<G>& walk, int 
                 sum = fmaf(Act16<BF16>::low(a), Act16<BF16>::low(b), sum);
                 sum = fmaf(Act16<BF16>::high(a), Act16<BF16>::high(b), sum);
             }
-            score = sum * p.scale_log2;
+            score = sum;
         }
-        const float m_new = fmaxf(m, wave_max(score)), alpha = __builtin_amdgcn_exp2f(m - m_new);
-        const float w = seen ? __builtin_amdgcn_exp2f(score - m_new) : 0.0f;
+        const float m_new = fmaxf(m, wave_max(score)), alpha = __builtin_amdgcn_exp2f((m - m_new) * p.scale_log2);
+        const float w = seen ? __builtin_amdgcn_exp2f((score - m_new) * p.scale_log2) : 0.0f;
         m = m_new;
         l = l * alpha + wave_sum(w);
 #pragma unroll
@@ -147,7 +149,7 @@ __device__ void put_column(const float* num, float m, float l, float* part, uint
 
 // Sums of key ranges, 16 bytes per lane: lane l of D / 4 has columns 4 l .. 4 l + 3.
 struct RangeSum {
-    float m = kPagedNone, den = 0.0f;
+    float sc, m = kPagedNone, den = 0.0f;        // sc: of scores, with log2(e)
     float4_t num = {0.f, 0.f, 0.f, 0.f};
     // adds N ranges at once (those with on[u]); the reference point of a range without keys lets it drop out
     template <int N>
@@ -155,7 +157,7 @@ struct RangeSum {
         float m_new = m;
 #pragma unroll
         for (int u = 0; u < N; ++u) m_new = on[u] ? fmaxf(m_new, s[u][0]) : m_new;
-        const float a = __builtin_amdgcn_exp2f(m - m_new);
+        const float a = __builtin_amdgcn_exp2f((m - m_new) * sc);
         m = m_new;
         den *= a;
 #pragma unroll
@@ -163,7 +165,7 @@ struct RangeSum {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             if (!on[u]) continue;                                // (what was loaded in its place may be anything)
-            const float f = __builtin_amdgcn_exp2f(s[u][0] - m);
+            const float f = __builtin_amdgcn_exp2f((s[u][0] - m) * sc);
             den += s[u][1] * f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) num[e] += x[u][e] * f;

@@ -144,19 +144,18 @@ again:                                                           // the pieces o
         }
         return S == 2 ? sum[0] : sum[0] + sum[S / 2 - 1];
     };
-    constexpr float kTop = 4.0f;                 // probabilities are 2^(score - m_run), at most 2^kTop
-    const float sc = p.scale_log2;
+    const float sc = p.scale_log2, top = 4.0f / sc;   // probabilities are 2^((score - m_run) sc), at most 2^4
     float m_run = kPagedNone, l_run = 0.0f;
     float4_t o[F];
 #pragma unroll
     for (int f = 0; f < F; ++f) o[f] = float4_t{0.f, 0.f, 0.f, 0.f};
     auto absorb = [&](const float4_t& st0, const float4_t& st1) {   // 32 keys; masked scores are -inf
-        float mx = fmaxf(fmaxf(fmaxf(st0[0], st0[1]), fmaxf(st0[2], st0[3])), fmaxf(fmaxf(st1[0], st1[1]), fmaxf(st1[2], st1[3]))) * sc;
-        if (__any(mx > m_run + kTop)) {
+        float mx = fmaxf(fmaxf(fmaxf(st0[0], st0[1]), fmaxf(st0[2], st0[3])), fmaxf(fmaxf(st1[0], st1[1]), fmaxf(st1[2], st1[3])));
+        if (__any(mx > m_run + top)) {
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));              // the column's largest score: all its lanes move together
-            const float m_new = mx > m_run + kTop ? mx : m_run;
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            const float m_new = mx > m_run + top ? mx : m_run;
+            const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
             l_run *= alpha;
 #pragma unroll
             for (int f = 0; f < F; ++f)
@@ -167,8 +166,8 @@ again:                                                           // the pieces o
         u32x4_t ph, pl;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(e < 4 ? st0[e & 3] : st1[e & 3], sc, -m_run));
-            const float p1 = __builtin_amdgcn_exp2f(fmaf(e < 4 ? st0[(e & 3) + 1] : st1[(e & 3) + 1], sc, -m_run));
+            const float p0 = __builtin_amdgcn_exp2f(((e < 4 ? st0[e & 3] : st1[e & 3]) - m_run) * sc);
+            const float p1 = __builtin_amdgcn_exp2f(((e < 4 ? st0[(e & 3) + 1] : st1[(e & 3) + 1]) - m_run) * sc);
             l_run += p0 + p1;
             const uint32_t h = A::pack(p0, p1);
             ph[e >> 1] = h;
@@ -263,7 +262,7 @@ again:                                                           // the pieces o
         float n0 = 0.0f, n1 = 0.0f, den = 0.0f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sm[w][r][D] - mn);
+            const float f = __builtin_amdgcn_exp2f((sm[w][r][D] - mn) * sc);
             n0 += sm[w][r][e] * f;
             n1 += sm[w][r][e + 1] * f;
             den += sm[w][r][D + 1] * f;
@@ -313,7 +312,7 @@ paged_pieces_kernel(PagedAttnDev p) {
     const int row0 = p.offs[b], n = p.offs[b + 1] - row0, cols = n * p.rep;
     if (n <= 0 || cols > kDecodeCols || r >= cols || at.y <= 1) return;
     const float* span0 = p.span_part + (static_cast<size_t>(hk) * p.spans + at.x) * (2 * kDecodeCols * W);
-    RangeSum sum;
+    RangeSum sum{p.scale_log2};
     sum.add_all<D>(group, GROUPS, at.y, lane, [&](int z) { return span0 + (static_cast<size_t>(2 * z + (z == 0 ? at.z : 0)) * kDecodeCols + r) * W; });
     nums[group][lane] = sum.num;
     if (lane == 0) stats[group] = float2_t{sum.m, sum.den};

@@ -206,7 +206,8 @@ struct ColumnWave {
                     st[kf][r] = seen ? st[kf][r] : -INFINITY;
                 }
         }
-        // Probabilities are 2^(score - m_run).  The reference point m_run need not be the maximum, only near it: it stays as long as the tile's
+        // Probabilities are 2^(score sc - scaled(m_run)), one fused operation each; where scores are so large that the rounding of scaled(m_run)
+        // shows, put() finds a sum that is not finite or too small for its own largest term.  The reference point m_run need not be the maximum, only near it: it stays as long as the tile's
         // probabilities add up to no more than kMost (then each fits fp16, and all have the bits of its normal numbers down to 2^-28 of the
         // largest), which is seen from the sum that is needed anyway.  Finding the maximum, meeting the other half of the column and rescaling
         // the sums are left to the tiles that break it: the first, and few after it.
@@ -219,7 +220,7 @@ struct ColumnWave {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kf][r]);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m_new = fmaxf(m_run, mx * sc), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            const float m_new = fmaxf(m_run, mx), alpha = __builtin_amdgcn_exp2f(scaled(m_run, sc) - scaled(m_new, sc));
             l_run *= alpha;
 #pragma unroll
             for (int f = 0; f < DF; ++f)
@@ -231,14 +232,17 @@ struct ColumnWave {
         l_run += sum;
     }
 
+    static __device__ __forceinline__ float scaled(float m, float sc) { return fmaxf(m * sc, -3.0e38f); }   // (finite also for a row that has seen no key)
+
     // Scores -> probabilities as operands; their sum, in 32 bits.
     __device__ __forceinline__ float weigh(float sc) {
+        const float ms = scaled(m_run, sc);
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int kf = 0; kf < 2; ++kf)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(st[kf][r], sc, -m_run)), p1 = __builtin_amdgcn_exp2f(fmaf(st[kf][r + 1], sc, -m_run));
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(st[kf][r], sc, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(st[kf][r + 1], sc, -ms));
                 sum[(r >> 1) & 3] += p0 + p1;
                 uint32_t w = A::pack(p0, p1);
                 asm("" : "+v"(w));                               // (packed here: carried past the caller's branch, 32 values would take 16 registers more)
@@ -293,8 +297,8 @@ struct ColumnWave {
     template <bool SPLIT>
     __device__ __forceinline__ void put(const PagedAttnDev& p, const SeqView& s, const KeySteps<kTileKeys>& walk, int hk, int t0, int t1, int z, int ranges, float l_tot) {
         const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
-        // columns whose sum is not finite (redo_column): both lanes of a column are left out below
-        float zero = l_tot * 0.0f;
+        // columns whose sum is not finite, or below the one that the largest term is (redo_column): both lanes of a column are left out below
+        float zero = m_run > kPagedNone && l_tot < 0.25f ? 1.0f : l_tot * 0.0f;
 #pragma unroll
         for (int f = 0; f < DF; ++f)
 #pragma unroll
@@ -317,12 +321,14 @@ struct ColumnWave {
             if (lhi == 0) dst[D + 2] = static_cast<float>(ranges);
             if (done) return;
             if (ranges > 1) {
+                // sums relative to scaled(m_run) -> to m_run times the scale: what the rounding left
+                const float to = m_run > kPagedNone ? __builtin_amdgcn_exp2f(-fmaf(m_run, p.scale_log2, -scaled(m_run, p.scale_log2))) : 1.0f;
 #pragma unroll
                 for (int f = 0; f < DF; ++f)
 #pragma unroll
                     for (int q4 = 0; q4 < 4; ++q4)
-                        *reinterpret_cast<float4_t*>(dst + f * 32 + 8 * q4 + 4 * lhi) = float4_t{o[f][4 * q4], o[f][4 * q4 + 1], o[f][4 * q4 + 2], o[f][4 * q4 + 3]};
-                if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{m_run, l_tot};
+                        *reinterpret_cast<float4_t*>(dst + f * 32 + 8 * q4 + 4 * lhi) = float4_t{o[f][4 * q4], o[f][4 * q4 + 1], o[f][4 * q4 + 2], o[f][4 * q4 + 3]} * to;
+                if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{m_run, l_tot * to};
                 return;
             }
         }
@@ -454,7 +460,8 @@ paged_chunk_kernel(PagedAttnDev p) {
         __syncthreads();
         if (group == 1) return;
         const float2_t other = *stats;
-        const float m = fmaxf(cw.m_run, other[0]), a0 = __builtin_amdgcn_exp2f(cw.m_run - m), a1 = __builtin_amdgcn_exp2f(other[0] - m);
+        const float m = fmaxf(cw.m_run, other[0]), ms = cw.scaled(m, p.scale_log2);
+        const float a0 = __builtin_amdgcn_exp2f(cw.scaled(cw.m_run, p.scale_log2) - ms), a1 = __builtin_amdgcn_exp2f(cw.scaled(other[0], p.scale_log2) - ms);
         cw.m_run = m;
         l_tot = l_tot * a0 + other[1] * a1;
 #pragma unroll
@@ -599,7 +606,7 @@ chunk_combine_kernel(PagedAttnDev p, int T) {
     const float* src = p.part + static_cast<size_t>(pair) * p.ranges * W;
     const int ranges = min(static_cast<int>(src[D + 2]), p.ranges);
     if (ranges <= 1) return;
-    RangeSum sum;
+    RangeSum sum{p.scale_log2};
     sum.add_all<D>(0, 1, ranges, threadIdx.x % LANES, [&](int z) { return src + static_cast<size_t>(z) * W; });
     sum.put<BF16>(p.out + row * p.out_stride + (pair - row * p.nh) * D, threadIdx.x % LANES);
 }

@@ -126,7 +126,7 @@ paged_rope_kernel(PagedRopeArgs a) {
             }
         } else {
             // The partners lie anywhere in the head; q may be turned in place: the lanes of a head are in one wave (8 or 16 of them), whose
-            // loads all come before its stores.
+            // loads all come before its stores (the barrier keeps the compiler to it).
             uint16_t own[8], other[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -134,6 +134,7 @@ paged_rope_kernel(PagedRopeArgs a) {
                 own[e] = e & 1 ? high(p[e >> 1]) : low(p[e >> 1]);
                 other[e] = col < r ? x.src[col < half ? col + half : col - half] : 0;
             }
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int col = 8 * x.chunk + e;

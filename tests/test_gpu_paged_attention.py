@@ -1,5 +1,7 @@
 """Attention over pages on the GPU (run with -m gpu) against 64 bits: head layouts, lengths around every tile and page edge, key ranges, windows with
 first tokens, missing pages, rows that see nothing, memory that holds NaN, large pools, graphs.  The bound on the error is derived in paged_helpers."""
+import random
+
 import pytest
 import torch
 
@@ -252,6 +254,55 @@ def test_scores_of_any_size(qt, new):
         for scale in (0.125, 8.0):
             got = qt.qtale_paged_attention(kv, 0, q, offsets(new), slots=ints(slots), scale=scale)
             _compare(kv, 0, q, got, new, [400 - new[0]], slots, 0, 0, scale, False)
+
+
+@pytest.mark.parametrize("new,old", [([1], [300]), ([60], [300]), ([1], [9000])])
+def test_scores_far_below_zero(qt, new, old):
+    # bf16 queries and keys of 10^17: every score is about -10^34, and what counts is how far they are from each other
+    nkv, rep, d = 2, 2, 64
+    kv, slots = random_cache(qt, [o + n for o, n in zip(old, new)], 32, nkv, d, torch.bfloat16, 8)
+    kv.k.fill_(-1e17)
+    kv.k[..., 1::2] = 0.0                                        # half of the columns: the scores are the same number
+    kv.v.copy_(torch.randn(kv.v.shape, generator=torch.Generator().manual_seed(9)))
+    q = torch.full((sum(new), nkv * rep, d), 1e17, dtype=torch.bfloat16, device="cuda")
+    out = qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), max_new=max(new), max_len=max(old) + max(new))
+    _compare(kv, 0, q, out, new, old, slots, 0, 0, d ** -0.5, max(new) == 1)
+
+
+@pytest.mark.parametrize("new,old", [([1], [300]), ([60], [300]), ([2, 60], [9000, 40]), ([400], [4000])])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_the_largest_scores_of_fp16(qt, new, old, sign):
+    # queries and keys of 60000: scores of 10^10, equal for every other key, half of that for the rest
+    nkv, rep, d = 2, 2, 64
+    kv, slots = random_cache(qt, [o + n for o, n in zip(old, new)], 32, nkv, d, torch.float16, 8)
+    kv.k.fill_(sign * 60000.0)
+    kv.k[:, :, 1::2] = sign * 30000.0
+    kv.v.copy_(torch.randn(kv.v.shape, generator=torch.Generator().manual_seed(9)))
+    q = torch.full((sum(new), nkv * rep, d), 60000.0, dtype=torch.float16, device="cuda")
+    out = qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), max_new=max(new), max_len=max(o + n for o, n in zip(old, new)))
+    _compare(kv, 0, q, out, new, old, slots, 0, 0, d ** -0.5, max(new) * rep <= 16)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_calls_of_any_kind(qt, seed):
+    rng = random.Random(seed)
+    d, dtype, page = rng.choice([64, 128]), rng.choice([torch.float16, torch.bfloat16]), rng.choice([16, 32, 64, 128, 256, 1024])
+    nkv, rep = rng.choice([1, 2, 3, 4, 8, 16]), rng.choice([1, 2, 3, 4, 5, 8, 12, 16, 17])
+    B = rng.choice([2, 5, 30])
+    longest = rng.choice([5, 50, 300, 1500] if B == 30 else [50, 1500, 6000])
+    most = rng.choice([1, 4, 100, 400])
+    new = [most] + [rng.choice([0, 1, 1, 2, rng.randint(1, most)]) if most > 1 else rng.choice([0, 1, 1]) for _ in range(B - 1)]
+    old = [rng.choice([0, longest, rng.randint(0, longest)]) for _ in range(B)]
+    lens = [o + n for o, n in zip(old, new)]
+    gone = {(b, rng.randrange(max(-(-lens[b] // page), 1))) for b in range(B) if rng.random() < 0.1}
+    window, sinks, hints = rng.choice([0, 0, 1, 17, 100, 700]), rng.choice([0, 4, 33]), rng.random() < 0.7
+    kv, slots = random_cache(qt, lens, page, nkv, d, dtype, seed, gone=gone)
+    q = torch.randn(sum(new), rep * nkv, d, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+    how = dict(max_new=most, max_len=max(lens) + rng.choice([0, 4000])) if hints else {}
+    workspace = qt.alloc_paged_workspace(kv, rep * nkv, sum(new), B, how.get("max_new", 0))
+    workspace.view(torch.float32).fill_(rng.choice([0.0, 2.0, 1e30, float("nan")]))
+    out = qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), window=window, sinks=sinks, workspace=workspace, **how)
+    _compare(kv, 0, q, out, new, old, slots, window, sinks, d ** -0.5, hints and most * rep <= 16)
 
 
 @pytest.mark.parametrize("new", [1, 50])
