@@ -26,12 +26,19 @@ hipError_t launch_pages_init(const PagedDev& p, hipStream_t stream);
 hipError_t launch_pages_fork(const PagedDev& p, const int32_t* src, const int32_t* dst, int n, hipStream_t stream);
 hipError_t launch_pages_drop(const PagedDev& p, const int32_t* slots, int n, bool release, int window, int sinks, hipStream_t stream);
 // layer < 0: every layer.  first/missing nullable; first [layers of the call][B]: the lengths before; then kv_len advances.
+// split: also the launch that copies shared pages; without it the next launch on the list has to.
 hipError_t launch_pages_reserve(const PagedDev& p, int layer, const int32_t* seq_offsets, const int32_t* slots, int B, int32_t* first,
-                                int32_t* missing, void* workspace, hipStream_t stream);
+                                int32_t* missing, bool split, void* workspace, hipStream_t stream);
 hipError_t launch_pages_compact(const PagedDev& p, int32_t* n_live, void* workspace, hipStream_t stream);
 hipError_t launch_pages_copy(const PagedDev& from, const PagedDev& to, const int32_t* src, const int32_t* dst, int n, hipStream_t stream);
 
 // ---- rotary embedding + append (paged_rope.hip) ---------------------------------------------------
+struct SplitList {               // pages to copy (pages_reserve_kernel's list)
+    const int32_t* n;
+    const int4* entries;         // from, to, tokens, -
+};
+SplitList pages_split_list(void* workspace);
+
 struct PagedRopeArgs {
     PagedDev kv;                 // table and len of the layer
     int layout, rotary_dim;      // 0 half, 1 interleaved
@@ -47,6 +54,7 @@ struct PagedRopeArgs {
     const int32_t* positions;
     const int32_t* rows;         // nullable: token of row i is rows[i]
     const int32_t* count;        // nullable: rows on the device (T is its bound)
+    SplitList copies;            // nullable: pages that the workgroups past the T rows copy
 };
 hipError_t launch_paged_rope(const PagedRopeArgs& a, hipStream_t stream);
 

@@ -77,7 +77,7 @@ int qtale_pages_reserve(const qtale_paged_kv* kv, int layer, const int32_t* seq_
     if (!seq_offsets) return QTALE_ERR_INVALID_ARG;
     const PagedDev p = paged_device(kv, -1);
     if ((e = check_workspace(workspace, workspace_bytes, pages_workspace_bytes(p, B)))) return e;
-    HIP_TRY(launch_pages_reserve(p, layer, seq_offsets, slots, B, first, missing, workspace, stream_of(stream)));
+    HIP_TRY(launch_pages_reserve(p, layer, seq_offsets, slots, B, first, missing, true, workspace, stream_of(stream)));
     return QTALE_OK;
 }
 

@@ -13,6 +13,8 @@
 // What bounds it is the stream of keys and values, and a CU takes in no more than about 50 GB/s (1 x 3000 keys, 32 workgroups: 33 us, whatever
 // the waves per workgroup).  So with few (sequence, kv head) pairs the keys of the call, laid end to end over its sequences, are cut into equally
 // long spans, one per workgroup that fits the chip; a span may end one sequence and begin the next, and a second launch adds the pieces.
+// Measured: 64 sequences of 2048 keys, 32 kv heads 312 us, 6.9 TB/s; 33 of 3000 (500 to 4500), 8 kv heads of 4 query heads 69 us, 5.9 TB/s, 4.6 us of it
+// the second launch; 1 of 700, 32 kv heads 10.8 us, where a launch alone takes 4 and the rest is the 350 KB per workgroup at a CU's rate.
 #include <algorithm>
 
 #include "paged_attn.h"

@@ -1,11 +1,15 @@
 // Pages of the paged K/V cache: who holds them, and moving their contents.
 //
 // Everything is decided on the device, because what a layer's cache needs is known there only: a layer holds the tokens that executed it.
+// What bounds these kernels is latency, chains of dependent loads, except where contents move.  us: room in one layer for a token of 1 / 64 / 256
+// sequences 5.8 / 7.4 / 8.3 (with the launch that copies); in 32 layers for 32 sequences, 24 of them with a page to copy, 13.9, and 34.6 for the copies
+// (190 MB read and written, 5.6 TB/s); fork, release, trim 4.6 to 7.4; compaction 6.8 to plan, 230 to move pages at 5.2 TB/s.
 // Every result is a function of the state before the call alone: pages are taken lowest free index first, in the order of layers, then of
 // the call's sequences, then of the pages' places; the counts are integers, so the order of their atomic updates does not show.
 #include <algorithm>
 
 #include "paged.h"
+#include "paged_split.h"
 #include "qtale_dev.h"
 
 namespace qtale {
@@ -101,37 +105,12 @@ hipError_t launch_pages_drop(const PagedDev& p, const int32_t* slots, int n, boo
 }
 
 // ---- moving pages ----------------------------------------------------------------------------------------
-// Work lists in the workspace: [0] number of entries, then (from, to) or (from, to, tokens) per entry from byte 256 on.
+// Work lists in the workspace: [0] number of entries, then (from, to) or (from, to, tokens, -) per entry from byte 256 on.
 constexpr int kMoveUnit = 16384;                 // bytes that a workgroup moves at a time: 256 threads x 4 x 16 bytes
 
-// Copies of shared last pages: the `tokens` first places of every head.  One workgroup per (entry, head) at a time.
 __global__ void __launch_bounds__(256)
-pages_split_kernel(PagedDev p, const int32_t* __restrict__ n_list, const int4* __restrict__ list) {
-    const int units = *n_list * p.nkv;
-    const int row_chunks = p.d >> 3;                             // 16-byte chunks of a token's head
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-        const int4 e = list[u / p.nkv];
-        const int chunks = e.z * row_chunks;
-        const size_t head = static_cast<size_t>(u % p.nkv) * row_chunks << p.shift, page = static_cast<size_t>(p.nkv) * row_chunks << p.shift;
-        const size_t from = e.x * page + head, to = e.y * page + head;
-        const u32x4_t *k0 = reinterpret_cast<const u32x4_t*>(p.k) + from, *v0 = reinterpret_cast<const u32x4_t*>(p.v) + from;
-        u32x4_t *k1 = reinterpret_cast<u32x4_t*>(p.k) + to, *v1 = reinterpret_cast<u32x4_t*>(p.v) + to;
-        // (chunks of keys, then of values: four of them in flight per thread)
-        for (int c = threadIdx.x; c < 2 * chunks; c += 4 * 256) {
-            u32x4_t x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = min(c + i * 256, 2 * chunks - 1);
-                x[i] = at < chunks ? k0[at] : v0[at - chunks];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = c + i * 256;
-                if (at < chunks) k1[at] = x[i];
-                else if (at < 2 * chunks) v1[at - chunks] = x[i];
-            }
-        }
-    }
+pages_split_kernel(PagedDev p, SplitList list) {
+    split_pages(p, list, blockIdx.x, gridDim.x);
 }
 
 // Whole pages, keys and values; workgroups past `movers` rewrite the page table instead (remap of the pages from n_live on).
@@ -367,13 +346,18 @@ size_t pages_workspace_bytes(const PagedDev& p, int B) {
     return 256 + (std::max(reserve, compact) + 255) / 256 * 256;
 }
 
+SplitList pages_split_list(void* workspace) {
+    return SplitList{reinterpret_cast<int32_t*>(workspace), reinterpret_cast<const int4*>(reinterpret_cast<char*>(workspace) + 256)};
+}
+
 hipError_t launch_pages_reserve(const PagedDev& p, int layer, const int32_t* seq_offsets, const int32_t* slots, int B, int32_t* first,
-                                int32_t* missing, void* workspace, hipStream_t stream) {
-    int32_t* n_copies = reinterpret_cast<int32_t*>(workspace);
-    int4* copies = reinterpret_cast<int4*>(reinterpret_cast<char*>(workspace) + 256);
-    hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kPlan), 0, stream, p, layer, seq_offsets, slots, B, first, missing, n_copies, copies);
+                                int32_t* missing, bool split, void* workspace, hipStream_t stream) {
+    const SplitList list = pages_split_list(workspace);
+    hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kPlan), 0, stream, p, layer, seq_offsets, slots, B, first, missing, const_cast<int32_t*>(list.n),
+                       const_cast<int4*>(list.entries));
+    if (!split) return hipGetLastError();
     const int64_t units = static_cast<int64_t>(layer < 0 ? p.n_layers : 1) * B * p.nkv;
-    hipLaunchKernelGGL(pages_split_kernel, dim3(static_cast<int>(std::min<int64_t>(units, kMovers))), dim3(256), 0, stream, p, n_copies, copies);
+    hipLaunchKernelGGL(pages_split_kernel, dim3(static_cast<int>(std::min<int64_t>(units, kMovers))), dim3(256), 0, stream, p, list);
     return hipGetLastError();
 }
 

@@ -230,14 +230,14 @@ int paged_attention_block(qtale_ctx* ctx, const qtale_layer_cfg* c, const PagedC
     uint16_t* qkv = reinterpret_cast<uint16_t*>(ws.qkv);
     {
         Prof pr(ctx, stream, 4);
-        HIP_TRY(launch_pages_reserve(pc.cache, pc.layer, ws.cu_exec, pc.slots, B, ws.kv_old, pc.missing, pc.pages_ws, stream));
+        HIP_TRY(launch_pages_reserve(pc.cache, pc.layer, ws.cu_exec, pc.slots, B, ws.kv_old, pc.missing, false, pc.pages_ws, stream));
         PagedRopeArgs r{};
         r.kv = paged_device(pc.kv, pc.layer);
         r.layout = pc.rope->layout; r.rotary_dim = pc.rope->rotary_dim; r.freqs = pc.rope->freqs; r.magnitude = pc.rope->magnitude;
         r.q = r.q_out = qkv; r.k = qkv + nh * d; r.v = qkv + (nh + nkv) * d;
         r.q_stride = r.k_stride = r.v_stride = r.q_out_stride = width;
         r.nh = nh; r.T = M_max; r.B = B; r.seq_offsets = ws.cu_exec; r.slots = pc.slots; r.first = ws.kv_old; r.positions = positions;
-        r.rows = ws.idx; r.count = ws.scalars;
+        r.rows = ws.idx; r.count = ws.scalars; r.copies = pages_split_list(pc.pages_ws);
         HIP_TRY(launch_paged_rope(r, stream));
     }
     Prof pr(ctx, stream, 5);
