@@ -76,19 +76,19 @@ struct PagedAttnDev {
     float* part;
     // decode kernel: spans per kv head that the call's keys are cut into (0: a workgroup per sequence), the sums of a span's first and last
     // piece [nkv][spans][2][kDecodeCols][part_stride(d)], and where a sequence's pieces are: [B] (first span, pieces, place of the first, -)
-    int spans, cols;             // cols: bound on a sequence's columns
+    int spans, cols;             // cols: bound on the columns of a sequence of this kernel
     int stream_keys;             // without spans: non-temporal keys
     float* span_part;
     int4* pieces;
 };
 struct PagedAttnPlan {
     bool decode, chunk;          // which kernels run
-    int spans, stream_keys;      // decode
+    int cols, spans, stream_keys;    // decode; cols: bound on those of a sequence of its
     int ranges, target, groups, items;   // chunk; groups of waves per workgroup that share its keys, 0: the wide form
     bool too_large;              // more workgroups than a grid has
     size_t decode_bytes, bytes;  // of workspace: the decode kernel's, all
 };
-constexpr int kDecodeCols = 16;                  // (query, head) pairs per kv head that the decode kernel holds
+constexpr int kDecodeCols = 16;                  // (query, head) pairs per kv head that a workgroup of the decode kernel holds
 constexpr int kChunkCols = 128;                  // ... and a workgroup of the chunk kernel
 constexpr int kWideCols = 256;                   // ... of its form with two halves that take turns
 constexpr int kChunkTileKeys = 64;

@@ -1,7 +1,7 @@
-// Attention over pages where few queries meet many keys: at most 16 (query, head) pairs per key/value head, so a single token of up to 16
-// heads per kv head, or a few tokens.
+// Attention over pages where few queries meet many keys: (query, head) pairs of a key/value head by sixteen, so a single token of up to 16 heads per
+// kv head, or a few tokens.
 //
-// One workgroup of four waves per (sequence, kv head[, key range]); the pairs are the 16 columns of both products.  A wave's step is 32 keys:
+// One workgroup of four waves per (sequence, kv head, 16 pairs), or per span of keys; the pairs are the 16 columns of both products.  A wave's step is 32 keys:
 //   S = K Q^T: two fragments of 16 keys; lane (c, g) = (lane % 16, lane / 16) holds 16 bytes of key c per instruction, an operand as loaded;
 //   O^T += V^T P^T: the scores of keys 4 g + r of both fragments are in lane (c, g), which is operand order if product index 8 g + e is key
 //   4 g + e (e < 4) or 16 + 4 g + e - 4.  Lane (c, g) loads columns F c .. F c + F - 1 of those eight keys; byte permutes make fragments.
@@ -10,6 +10,8 @@
 // maybe, would be NaN).  Probabilities are 32-bit sums; as operands they go in as two 16-bit terms, p = hi + lo, through two products into one
 // accumulator, which leaves 2^-16 (bf16) or 2^-22 of them: the matrix cores have time (about a tenth of the stream's), and a bf16 probability
 // alone would add as much error as the output's own rounding.
+// Calls of more than 16 pairs per sequence come here while their workgroups fit the chip about once: each reads the sequence's keys, from L2 but for
+// the first, and the longest is done sooner than a workgroup of the chunk kernel, whose waves take a tile after the other (plan_paged_attention).
 // What bounds it is the stream of keys and values, and a CU takes in no more than about 50 GB/s (1 x 3000 keys, 32 workgroups: 33 us, whatever
 // the waves per workgroup).  So with few (sequence, kv head) pairs the keys of the call, laid end to end over its sequences, are cut into equally
 // long spans, one per workgroup that fits the chip; a span may end one sequence and begin the next, and a second launch adds the pieces.
@@ -49,7 +51,7 @@ paged_decode_kernel(PagedAttnDev p) {
     __shared__ uint32_t s_redo;                                  // columns whose sum is not finite
     __shared__ int ends[SPANS ? kSpanSeqs : 1];                  // units up to and with sequence b
 
-    int b = blockIdx.y, cur = 0, end = 0, total = 0, spans = 1;
+    int b = blockIdx.z, cur = 0, end = 0, total = 0, spans = 1;
     uint32_t span = 0;
     if (SPANS) {
         for (int b0 = 0; b0 < p.B; b0 += 64) {
@@ -77,9 +79,12 @@ again:                                                           // the pieces o
     b = __builtin_amdgcn_readfirstlane(b);
     SeqView s(p, b);
     s.uniform();
-    const int cols = s.n * p.rep;
-    if (!SPANS && (s.n == 0 || (p.take != 0 && cols > kDecodeCols))) return;
-    const KeySteps<kStepKeys> walk(s.first, s.first + s.n - 1, s.len, p.window, p.sinks);
+    // this workgroup's columns c0 .. c0 + cols - 1 of the sequence's, of queries q_lo .. q_hi (with spans there are no more than sixteen)
+    const int c0 = SPANS ? 0 : static_cast<int>(blockIdx.y) * kDecodeCols, all_cols = s.n * p.rep;
+    if (!SPANS && (all_cols <= c0 || (p.take != 0 && all_cols > kDecodeCols))) return;
+    const int cols = min(all_cols - c0, kDecodeCols);
+    const int q_lo = SPANS ? 0 : __builtin_amdgcn_readfirstlane(c0 / p.rep), q_hi = SPANS ? s.n - 1 : __builtin_amdgcn_readfirstlane((c0 + cols - 1) / p.rep);
+    const KeySteps<kStepKeys> walk(s.first + q_lo, s.first + q_hi, s.len, p.window, p.sinks);
     int first_step = 0, last_step = walk.steps;
     bool whole = true;
     int seq_begin = 0, seq_end = 0;
@@ -90,7 +95,7 @@ again:                                                           // the pieces o
         if (end < seq_end) last_step = min(last_step, (end - seq_begin) * kUnitSteps);
         whole = cur == seq_begin && end >= seq_end;
     }
-    const int col = min(c, cols - 1);                            // this lane's column: query col / rep, head col % rep
+    const int col = c0 + min(c, cols - 1);                       // this lane's column: query col / rep, head col % rep
     const int qi = col / p.rep, head = hk * p.rep + col - qi * p.rep;
     const int place = s.first + qi;                              // the query's place in its slot
     const int reach = p.window > 0 ? place - p.window : INT32_MIN;   // keys after it are in its window
@@ -101,7 +106,7 @@ again:                                                           // the pieces o
 
     const int s0 = first_step + wave, s1 = last_step;            // this wave's steps: s0, s0 + 4, ...
     const PageRow pages(p, s.slot);
-    const int hi = walk.hi, lo = walk.lo, n_minus = s.n - 1;
+    const int hi = walk.hi, lo = walk.lo, n_minus = q_hi - q_lo;
     const size_t head_elems = static_cast<size_t>(D) << p.shift;
 
     // page ids of the two fragments of a step: read one step before the loads that use them
@@ -190,7 +195,7 @@ again:                                                           // the pieces o
         for (int u = 0; u < 2; ++u) st[u] = scores(kn[u]);
         next(0);
         // every key of the step is seen by every query, unless the step lies at an end of the keys or a page is gone
-        if (!(kb + kStepKeys <= min(s.first + 1, hi) && (kb >= lo + n_minus || kb + kStepKeys <= p.sinks) && (id.a | id.b) >= 0)) {
+        if (!(kb + kStepKeys <= min(s.first + q_lo + 1, hi) && (kb >= lo + n_minus || kb + kStepKeys <= p.sinks) && (id.a | id.b) >= 0)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -246,8 +251,8 @@ again:                                                           // the pieces o
     __syncthreads();
     // the launch that adds the chunk kernel's key ranges finds none in these rows
     if (p.take != 0 && p.ranges > 1 && (!SPANS || cur == seq_begin) && tid < cols) {
-        const int i = tid / p.rep;
-        p.part[((static_cast<size_t>(s.row0 + i) * p.nh + hk * p.rep + tid - i * p.rep) * p.ranges) * part_stride(D) + D + 2] = 0.0f;
+        const int i = (c0 + tid) / p.rep;
+        p.part[((static_cast<size_t>(s.row0 + i) * p.nh + hk * p.rep + c0 + tid - i * p.rep) * p.ranges) * part_stride(D) + D + 2] = 0.0f;
     }
     // a piece that begins its span goes to the span's first place, another one (it reaches the span's end) to the second
     float* piece = SPANS ? p.span_part + ((static_cast<size_t>(hk) * p.spans + span) * 2 + (cur == begin ? 0 : 1)) * (kDecodeCols * part_stride(D)) : nullptr;
@@ -256,7 +261,7 @@ again:                                                           // the pieces o
         const int last = whole ? static_cast<int>(span) : static_cast<int>((static_cast<uint64_t>(seq_end) * static_cast<uint32_t>(spans) - 1) / static_cast<uint32_t>(total));
         p.pieces[b] = int4{static_cast<int>(span), last - static_cast<int>(span) + 1, cur == begin ? 0 : 1, 0};
     }
-    for (int t = tid; t < min(cols, kDecodeCols) * (D / 2); t += 256) {
+    for (int t = tid; t < cols * (D / 2); t += 256) {
         const int r = t / (D / 2), e = 2 * (t % (D / 2));
         float mn = kPagedNone;
 #pragma unroll
@@ -275,7 +280,7 @@ again:                                                           // the pieces o
             *reinterpret_cast<float2_t*>(dst + e) = float2_t{n0, n1};
             if (e == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{mn, den};
         } else {
-            const int i = r / p.rep, h = hk * p.rep + r - i * p.rep;
+            const int i = (c0 + r) / p.rep, h = hk * p.rep + c0 + r - i * p.rep;
             const float inv = den != 0.0f ? 1.0f / den : 0.0f;   // a row that sees no key is zero
             *reinterpret_cast<uint32_t*>(p.out + (s.row0 + i) * p.out_stride + h * D + e) = A::pack(n0 * inv, n1 * inv);
         }
@@ -288,7 +293,7 @@ again:                                                           // the pieces o
 #pragma unroll 1
         for (int j = 0; redo != 0; ++j, redo &= redo - 1) {
             if ((j & 3) != wave) continue;
-            const int r = __ffs(static_cast<int>(redo)) - 1, i = r / p.rep, h = hk * p.rep + r - i * p.rep;
+            const int r = __ffs(static_cast<int>(redo)) - 1, i = (c0 + r) / p.rep, h = hk * p.rep + c0 + r - i * p.rep;
             float num[D / 64], m, l;
             redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + i) * p.q_stride + h * D, s.first + i, first_step, last_step, num, &m, &l);
             put_column<D, BF16>(num, m, l, whole ? nullptr : piece + r * part_stride(D), p.out + (s.row0 + i) * p.out_stride + h * D);
@@ -332,13 +337,15 @@ paged_pieces_kernel(PagedAttnDev p) {
 
 template <int D, bool BF16>
 static hipError_t decode_form(const PagedAttnDev& a, hipStream_t stream) {
+    // a sequence's columns next to each other: the workgroups that share its keys run together
+    const dim3 grid(a.nkv, (a.cols + kDecodeCols - 1) / kDecodeCols, a.B);
     if (a.spans > 0) {
         hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true, true>), dim3(a.nkv, a.spans), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL((paged_pieces_kernel<D, BF16>), dim3(a.nkv, a.B, a.cols), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_pieces_kernel<D, BF16>), dim3(a.nkv, a.B, a.cols), dim3(256), 0, stream, a);   // (a.cols <= 16)
     } else if (D == 128 && a.stream_keys) {
-        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false, D == 128>), dim3(a.nkv, a.B), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false, D == 128>), grid, dim3(256), 0, stream, a);
     } else {
-        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false, false>), dim3(a.nkv, a.B), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false, false>), grid, dim3(256), 0, stream, a);
     }
     return hipGetLastError();
 }

@@ -77,6 +77,54 @@ def test_chunks_around_the_tiles(qt, dtype, d, rep, nkv):
     _case(qt, dtype, rep, nkv, d, 16, new, [500, 0, 15, 17, 300, 31], seed=rep)
 
 
+# Calls that the kernel for chunks gets: its keys cut into ranges (a bound on long caches), many column tiles on short keys, and the same on longer
+# ones, which two groups of waves share.  (Few column tiles on short keys are the other kernel's, sixteen columns at a time.)
+FORMS = {"ranges": ([31, 33, 1, 65, 17], [0, 500, 64, 1, 300], 60000), "tiles": ([31, 33, 32, 65, 1, 64, 17, 40] * 3, [0, 1, 64, 63, 300, 128, 30, 200] * 3, 400),
+         "groups": ([31, 33, 32, 65, 1, 64, 17, 40] * 3, [0, 600, 64, 63, 900, 128, 30, 500] * 3, 1000)}
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("d,rep", [(64, 4), (128, 1), (128, 4), (64, 17)])
+@pytest.mark.parametrize("form", sorted(FORMS))
+def test_forms_of_the_kernel_for_chunks(qt, form, d, rep, dtype):
+    new, old, bound = FORMS[form]
+    nkv = 8 if rep < 17 else 2
+    _case(qt, dtype, rep, nkv, d, 64, new, old, max_len=bound, seed=rep)
+    _case(qt, dtype, rep, nkv, d, 16, new, old, window=70, sinks=20, max_len=bound, seed=rep, gone={(0, 0), (1, 2), (3, 1)})
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("form", sorted(FORMS))
+def test_values_that_are_not_finite_in_every_form(qt, form, d, dtype):
+    new, old, bound = FORMS[form]
+    nkv, rep, page = 8, 1, 32
+    kv, slots = random_cache(qt, [o + n for o, n in zip(old, new)], page, nkv, d, dtype, 12)
+    for b, h, e, pool, value in ((0, 0, 5, kv.v, "nan"), (1, 3, 9, kv.k, "inf"), (3, 7, 63, kv.v, "-inf")):
+        at = old[b] + new[b] // 2
+        pool[int(kv.table[0, slots[b], at // page]), h, at % page, e] = float(value)
+    q = torch.randn(sum(new), rep * nkv, d, generator=torch.Generator().manual_seed(5)).to(dtype).cuda()
+    got = qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), max_new=max(new), max_len=bound)
+    few = [0, 1, 3]                                              # the sequences that hold such values row by row, the others as ever
+    want, size = attend64(kv, 0, q, new, old, slots, 0, 0, d ** -0.5)
+    begin = offsets(new).tolist()
+    for b in few:
+        rows = slice(begin[b], begin[b + 1])
+        want[rows], size[rows] = attend64(kv, 0, q[rows], new[b: b + 1], old[b: b + 1], slots[b: b + 1], 0, 0, d ** -0.5, clean=True)
+    whole = torch.isfinite(want) & torch.isfinite(size)
+    assert not bool(whole.all()) and bool(whole.any())
+    assert bool(((got.double() - want).abs() <= attention_bound(want, size, dtype, False))[whole].all())
+    assert not bool(torch.isfinite(got[~whole]).any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rep,d,tokens", [(1, 128, 17), (3, 64, 11), (4, 128, 8), (16, 64, 3), (5, 64, 13), (24, 128, 2)])
+def test_columns_by_sixteen(qt, rep, d, tokens, dtype):
+    new = [tokens, 1, tokens - 1, 0, tokens]
+    _case(qt, dtype, rep, 2, d, 32, new, [0, 40, 33, 7, 300], seed=rep)
+    _case(qt, dtype, rep, 2, d, 16, new, [90, 40, 333, 7, 300], window=33, sinks=5, seed=rep, gone={(0, 1), (2, 3)})
+
+
 @pytest.mark.parametrize("rep", [17, 32, 40])
 def test_more_heads_per_kv_head_than_columns_of_the_decode_kernel(qt, rep):
     _case(qt, torch.float16, rep, 1, 64, 32, [1, 1, 4, 0, 9], [0, 100, 33, 5, 600])
