@@ -2,7 +2,7 @@
 //
 // Everything is decided on the device, because what a layer's cache needs is known there only: a layer holds the tokens that executed it.
 // What bounds these kernels is latency, chains of dependent loads, except where contents move.  us: room in one layer for a token of 1 / 64 / 256
-// sequences 5.8 / 7.4 / 8.3 (with the launch that copies); in 32 layers for 32 sequences, 24 of them with a page to copy, 13.9, and 34.6 for the copies
+// sequences 5.8 / 7.4 / 8.3 (with the launch that copies); in 32 layers for 32 sequences, 24 of them with a page to copy, 12.7, and 34.6 for the copies
 // (190 MB read and written, 5.6 TB/s); fork, release, trim 4.6 to 7.4; compaction 6.8 to plan, 230 to move pages at 5.2 TB/s.
 // Every result is a function of the state before the call alone: pages are taken lowest free index first, in the order of layers, then of
 // the call's sequences, then of the pages' places; the counts are integers, so the order of their atomic updates does not show.
@@ -220,6 +220,8 @@ pages_reserve_kernel(PagedDev p, int layer, const int32_t* __restrict__ offs, co
     const int words = (p.n_pages + 31) >> 5;
     if (tid == 0) s_copies = 0;
     int w0 = 0, short_by = 0;                                    // free pages lie from word w0 on
+    uint32_t ahead = tid < words ? p.bits[tid] : 0u;             // the first words, on their way beside the chain of loads below
+    bool have_ahead = true;
     for (int l0 = l_begin; l0 < l_end; l0 += per) {
         const int items = min(per, l_end - l0) * B;
         int len[2], cap[2], n[2], at[2], need[2], shared[2], extra[2];
@@ -256,6 +258,7 @@ pages_reserve_kernel(PagedDev p, int layer, const int32_t* __restrict__ offs, co
             const int i = 2 * tid + u;
             if (i < items && shared[u] > 1) {                    // holders of this page earlier in the layer's order take a copy each
                 int left = shared[u];
+#pragma unroll 4
                 for (int e = i - i % B; e < i; ++e) left -= last[e] == last[i];
                 copied[u] = left > 1;
             }
@@ -275,7 +278,8 @@ pages_reserve_kernel(PagedDev p, int layer, const int32_t* __restrict__ offs, co
         int got = 0;                                             // pages handed out in this chunk
         while (got < total && w0 < words) {
             const int w = w0 + tid;
-            const uint32_t bits = w < words ? p.bits[w] : 0u;
+            const uint32_t bits = have_ahead ? ahead : w < words ? p.bits[w] : 0u;
+            have_ahead = false;
             int found;
             const int rank = block_prefix(__popc(bits), sums, &found);
             const int room = min(total - got, kFreeList);
