@@ -18,9 +18,6 @@
 // What bounds it is the chip's power: the same call on zeros, at the clock that those leave, takes 455 us where random data takes 575 (4 x 4096 tokens, 32
 // heads on 8 kv heads of 128, the wide form: 950 TFLOP/s; a library product of 8192^3 reaches 1150).  500 tokens on 24000 take 206 us, 960 TFLOP/s;
 // heads of 64, where a score costs half the products and as much softmax, 2 x 700 on 1400 40 to 45 us, 560 to 630 TFLOP/s.
-#include <algorithm>
-#include <type_traits>
-
 #include "paged_attn.h"
 
 namespace qtale {
@@ -354,9 +351,13 @@ struct ColumnWave {
     }
 };
 
+// SPLIT: key ranges.  KG: groups of four waves that share the keys.  Waves per SIMD: two; for heads of 64 without ranges four, although a few
+// registers go to memory then (4 x 4096 tokens 324 us, with three 334), with ranges, which are two workgroups per CU, two (3 x 440 tokens on 12728
+// keys 199 us, with four 208).
 template <int D, bool BF16, bool SPLIT, int KG>
-__global__ void __launch_bounds__(256 * KG, D == 64 ? 4 : 2)
+__global__ void __launch_bounds__(256 * KG, D == 64 && !SPLIT ? 4 : 2)
 paged_chunk_kernel(PagedAttnDev p) {
+    static_assert(KG == 1 || !SPLIT, "ranges have one group");
     constexpr int DF = D / 32;                   // output fragments
     constexpr int CPR = D / 8;                   // 16-byte chunks of a row
     constexpr int RPF = 64 / CPR;                // rows per fetch instruction (1 KB)
@@ -387,7 +388,7 @@ paged_chunk_kernel(PagedAttnDev p) {
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) work += __shfl_xor(work, x, 64);
         const int wanted = max(p.target / p.nkv, 1);
-        const int per = __builtin_amdgcn_readfirstlane(max(max((work + wanted - 1) / wanted, (walk.steps + p.ranges - 1) / p.ranges), 4 * KG));
+        const int per = __builtin_amdgcn_readfirstlane(max(max((work + wanted - 1) / wanted, (walk.steps + p.ranges - 1) / p.ranges), 4));
         ranges = __builtin_amdgcn_readfirstlane(max((walk.steps + per - 1) / per, 1));
         if (z >= ranges) return;
         t0 = z * per;
@@ -618,28 +619,24 @@ chunk_combine_kernel(PagedAttnDev p, int T) {
     sum.put<BF16>(p.out + row * p.out_stride + (pair - row * p.nh) * D, threadIdx.x % LANES);
 }
 
-template <int D, bool BF16, int KG>
-static hipError_t chunk_form(const PagedAttnDev& a, hipStream_t stream) {
-    const bool split = a.ranges > 1;
-    const int64_t items = static_cast<int64_t>(a.items) * a.ranges;
-    const dim3 grid(static_cast<uint32_t>(items * a.nkv)), block(256 * KG);
-    if (split) hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, true, KG>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, false, KG>), grid, block, 0, stream, a);
+template <int D, bool BF16>
+static hipError_t chunk_form(const PagedAttnDev& a, int groups, hipStream_t stream) {
+    const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.items) * a.ranges * a.nkv));
+    if constexpr (D == 128) {                                    // (heads of 64 have no wide form: plan_paged_attention)
+        if (groups == 0) {
+            hipLaunchKernelGGL((paged_wide_kernel<D, BF16>), grid, dim3(512), 0, stream, a);
+            return hipGetLastError();
+        }
+    }
+    if (groups == 2) hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, false, 2>), grid, dim3(512), 0, stream, a);
+    else if (a.ranges > 1) hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, true, 1>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((paged_chunk_kernel<D, BF16, false, 1>), grid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
-template <int D, bool BF16>
-static hipError_t chunk_groups(const PagedAttnDev& a, int groups, hipStream_t stream) {
-    if (groups == 0) {
-        hipLaunchKernelGGL((paged_wide_kernel<D, BF16>), dim3(static_cast<uint32_t>(a.items * a.nkv)), dim3(512), 0, stream, a);
-        return hipGetLastError();
-    }
-    return groups == 2 ? chunk_form<D, BF16, 2>(a, stream) : chunk_form<D, BF16, 1>(a, stream);
-}
-
 hipError_t launch_paged_chunk(const PagedAttnDev& a, int groups, int d, int bf16, hipStream_t stream) {
-    if (d == 128) return bf16 ? chunk_groups<128, true>(a, groups, stream) : chunk_groups<128, false>(a, groups, stream);
-    return bf16 ? chunk_groups<64, true>(a, groups, stream) : chunk_groups<64, false>(a, groups, stream);
+    if (d == 128) return bf16 ? chunk_form<128, true>(a, groups, stream) : chunk_form<128, false>(a, groups, stream);
+    return bf16 ? chunk_form<64, true>(a, groups, stream) : chunk_form<64, false>(a, groups, stream);
 }
 
 hipError_t launch_chunk_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream) {
