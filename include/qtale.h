@@ -357,7 +357,7 @@ typedef struct {
     int window;               /* entries that a token sees, itself included; 0 = all before it */
     int sinks;                /* first entries of the slot that stay visible with a window */
     float scale;              /* > 0, e.g. 1 / sqrt(head_dim) */
-    int max_new;              /* bound on the new tokens of a sequence; 0 = T.  The launches follow from it: a bound near the truth pays */
+    int max_new;              /* bound on the new tokens of a sequence (rows past it are undefined); 0 = T.  A bound near the truth pays */
     int max_len;              /* bound on kv_len; 0 = max_pages * page_size.  Entries from max_len on are not seen */
 } qtale_paged_attn;
 size_t qtale_paged_attention_workspace_bytes(const qtale_paged_kv* kv, const qtale_paged_attn* attn, int T, int B);

@@ -622,10 +622,11 @@ class Rope:
 
 
 def _heads(t, kv, T, n):
-    """(address, elements between tokens) of [T, n, head_dim] of the cache's type, the heads of a token contiguous."""
-    step = t.stride()
-    assert t.shape == (T, n, kv.head_dim) and step[1:] == (kv.head_dim, 1) and t.dtype is kv.dtype and t.device == kv.device, (t.shape, step)
-    return t.data_ptr(), step[0]
+    """(address, elements between tokens) of [T, n, head_dim] of the cache's type, the heads of a token contiguous.  (What a tensor says of the
+    stride of a single token or head means nothing.)"""
+    step, d = t.stride(), kv.head_dim
+    assert (t.shape == (T, n, d) and step[2] == 1 and (step[1] == d or n == 1) and t.dtype is kv.dtype and t.device == kv.device), (t.shape, step)
+    return t.data_ptr(), step[0] if T > 1 else n * d
 
 
 def qtale_paged_rope_append(kv, layer, rope, q, k, v, seq_offsets, positions, first=None, slots=None, q_out=None):

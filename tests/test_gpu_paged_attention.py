@@ -280,6 +280,25 @@ def test_entries_past_the_bound_are_not_seen(qt):
         _compare(kv, 1, q, got, new, [200, 90], slots, 0, 0, 64 ** -0.5, False)
 
 
+def test_strides_of_a_single_token_or_head(qt):
+    # [heads, 1, d] and [1, T, d] seen from the other side: contiguous, whatever the strides say
+    d = 64
+    for T, rep, nkv in ((1, 4, 2), (5, 1, 1)):
+        kv, slots = random_cache(qt, [70], 16, nkv, d, torch.float16, 2, max_extra=4)
+        q = torch.randn(rep * nkv, T, d, generator=torch.Generator().manual_seed(3)).half().cuda().transpose(0, 1)
+        assert q.is_contiguous() and q.stride() != (rep * nkv * d, d, 1)
+        kv_len = kv.kv_len.clone()
+        out = qt.qtale_paged_attention(kv, 0, q, offsets([T]), slots=ints(slots), max_new=T, out=torch.empty_like(q))
+        _compare(kv, 0, q, out, [T], [70 - T], slots, 0, 0, d ** -0.5, True)
+        k, v = (torch.randn(nkv, T, d, generator=torch.Generator().manual_seed(i)).half().cuda().transpose(0, 1) for i in (4, 5))
+        rope, pos = qt.Rope(d), ints(list(range(70 - T, 70)))
+        a = qt.qtale_paged_rope_append(kv, 0, rope, q, k, v, offsets([T]), pos, slots=ints(slots))
+        kept = kv.k.clone(), kv.v.clone()
+        b = qt.qtale_paged_rope_append(kv, 0, rope, *(t.clone(memory_format=torch.contiguous_format) for t in (q, k, v)), offsets([T]), pos, slots=ints(slots))
+        assert torch.equal(a, b) and torch.equal(kept[0].nan_to_num(), kv.k.nan_to_num()) and torch.equal(kept[1].nan_to_num(), kv.v.nan_to_num())
+        assert torch.equal(kv_len, kv.kv_len)
+
+
 def test_no_slots_no_first(qt):
     # sequence b is slot b, its tokens are the slot's last ones
     kv, slots = random_cache(qt, [70, 33, 5], 16, 2, 64, torch.float16, 8, extra_slots=0)
