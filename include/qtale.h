@@ -293,12 +293,13 @@ int qtale_pages_fork(const qtale_paged_kv* kv, const int32_t* src, const int32_t
 
 /* Makes room for the new tokens of a call: seq_offsets[b+1] - seq_offsets[b] for sequence b (seq_offsets [B+1] int32 device), in one layer or
  * in all (layer = -1).  Pages are taken lowest number first, in the order of layers, then sequences, then places.  A slot that will write into
- * a page it shares (its last, partly filled) first gets a copy of it, unless it is the page's last holder by then: of several in one call the
- * earlier ones take copies.
+ * a page it shares (its last, partly filled) first gets a copy of it.  Only where all holders of the page write in this call, the one with the
+ * most tokens, of several the last in order, keeps the page itself.
  *   first     nullable: only make room.  Otherwise the slots' lengths are advanced as well and first [layers of the call][B] receives the
  *             lengths before: token i of sequence b is entry first[b] + i of its slot, for qtale_paged_rope_append and qtale_paged_attention
  *   missing   nullable [1] out: pages that the pool could not give.  A slot that got fewer than it needs holds as many of the new tokens as
- *             fit (the first ones); the others are dropped by the append, and its length stops there.  Likewise at max_pages * page_size.
+ *             fit (the first ones); the others are dropped by the append, and its length stops there.  Likewise at max_pages * page_size.  One that
+ *             got no page for its copy takes none of its tokens and keeps sharing the old one
  *   workspace qtale_pages_workspace_bytes(kv, B) bytes, 256-byte aligned; B <= 2048 */
 int qtale_pages_reserve(const qtale_paged_kv* kv, int layer, const int32_t* seq_offsets, const int32_t* slots, int B, int32_t* first,
                         int32_t* missing, void* workspace, size_t workspace_bytes, void* stream);

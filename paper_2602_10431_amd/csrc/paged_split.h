@@ -1,5 +1,5 @@
 // Copies of shared, partly filled pages, by the launch after the one that lists them (pages.hip): a launch of its own, or beside the rotation and
-// the append of the same tokens, which write other places of these pages.
+// the append of the same tokens, which writes other places of these pages: nobody stores below the length of a holder (pages_reserve_kernel).
 #pragma once
 #include "paged.h"
 #include "qtale_dev.h"

@@ -200,8 +200,11 @@ __device__ __forceinline__ int block_prefix(int v, int* sums, int* total) {
 }
 
 // ---- room for new tokens ---------------------------------------------------------------------------------
-// Per (layer, sequence): a page for the copy of a shared, partly filled last page (every holder in the call but the last one, in order, when
-// nobody else holds it), and the pages of tokens beyond its room.  Thread t owns items 2 t and 2 t + 1 of a chunk of whole layers.
+// Per (layer, sequence): a page for the copy of a shared, partly filled last page, and the pages of tokens beyond its room.  Where all holders of such
+// a page are in the call, the one with the most tokens (of several the last in order) writes into it and only the others take copies.  The
+// most tokens, because holders need not have equally many: one whose copy the pool could not give stays behind with the page, and its next token
+// would lie where the others have one already.  So no call writes below the length of any holder, nor where a copy of the same call reads.
+// Thread t owns items 2 t and 2 t + 1 of a chunk of whole layers.
 //   1. what each item needs, and its place in the order (prefix sum);
 //   2. the free pages in ascending order, up to kFreeList at a time, into LDS; 32768 pages are looked at per round;
 //   3. list entry k goes to the item whose span of the order holds it (binary search in LDS);
@@ -211,8 +214,11 @@ constexpr int kFreeList = 4096;
 __global__ void __launch_bounds__(kPlan)
 pages_reserve_kernel(PagedDev p, int layer, const int32_t* __restrict__ offs, const int32_t* __restrict__ slots, int B, int32_t* __restrict__ first,
                      int32_t* __restrict__ missing, int32_t* __restrict__ n_copies, int4* __restrict__ copies) {
-    __shared__ int start[kReserveItems + 1], row[kReserveItems], place[kReserveItems], last[kReserveItems];
-    __shared__ int list[kFreeList];
+    __shared__ int start[kReserveItems + 1], row[kReserveItems], place[kReserveItems];
+    __shared__ __attribute__((aligned(16))) int list[kFreeList];
+    // until the list is made: the page that an item would go on in (-1: none), and its next place there with its place in the order, which decide
+    int2* writers = reinterpret_cast<int2*>(list);
+    static_assert(kFreeList >= 2 * kReserveItems, "the items fit the list");
     __shared__ int sums[kPlan / 64], s_copies;
     const int tid = threadIdx.x;
     const int l_begin = layer < 0 ? 0 : layer, l_end = layer < 0 ? p.n_layers : layer + 1;
@@ -224,20 +230,19 @@ pages_reserve_kernel(PagedDev p, int layer, const int32_t* __restrict__ offs, co
     bool have_ahead = true;
     for (int l0 = l_begin; l0 < l_end; l0 += per) {
         const int items = min(per, l_end - l0) * B;
-        int len[2], cap[2], n[2], at[2], need[2], shared[2], extra[2];
+        int len[2], cap[2], n[2], at[2], need[2], shared[2], extra[2], old[2];
         bool copied[2];
         __syncthreads();                                         // the chunk before is done with LDS
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int i = 2 * tid + u;
             n[u] = len[u] = cap[u] = need[u] = extra[u] = shared[u] = 0;
-            at[u] = -1;
+            at[u] = old[u] = -1;
             copied[u] = false;
             if (i >= items) continue;
             const int b = i % B, l = l0 + i / B;
             const int slot = slots ? slots[b] : b;
             n[u] = max(offs[b + 1] - offs[b], 0);
-            int candidate = -1;
             if (slot_ok(p, slot)) {
                 at[u] = l * p.n_slots + slot;
                 len[u] = p.len[at[u]];
@@ -245,22 +250,27 @@ pages_reserve_kernel(PagedDev p, int layer, const int32_t* __restrict__ offs, co
                 const int j = len[u] >> p.shift;
                 if (n[u] > 0 && (len[u] & ((1 << p.shift) - 1)) != 0 && j < p.max_pages) {
                     const int page = p.table[static_cast<size_t>(at[u]) * p.max_pages + j];
-                    if (page_ok(p, page)) { candidate = page; shared[u] = p.refs[page]; }
+                    if (page_ok(p, page)) { old[u] = page; shared[u] = p.refs[page]; }
                 }
                 const int64_t want = min((static_cast<int64_t>(len[u]) + n[u] + (1 << p.shift) - 1) >> p.shift, static_cast<int64_t>(p.max_pages));
                 if (n[u] > 0) extra[u] = max(static_cast<int>(want) - (cap[u] >> p.shift), 0);
             }
-            last[i] = candidate;
+            writers[i] = int2{old[u], (len[u] & ((1 << p.shift) - 1)) * kReserveItems + i % B};
         }
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int i = 2 * tid + u;
-            if (i < items && shared[u] > 1) {                    // holders of this page earlier in the layer's order take a copy each
-                int left = shared[u];
-#pragma unroll 4
-                for (int e = i - i % B; e < i; ++e) left -= last[e] == last[i];
-                copied[u] = left > 1;
+            if (i < items && shared[u] > 1) {
+                int holders = 0, keeps = -1;
+                const int e0 = i - i % B;
+#pragma unroll 8
+                for (int e = e0; e < e0 + B; ++e) {
+                    const int2 w = writers[e];
+                    holders += w.x == old[u];
+                    keeps = max(keeps, w.x == old[u] ? w.y : -1);
+                }
+                copied[u] = holders < shared[u] || keeps != writers[i].y;
             }
             need[u] = extra[u] + copied[u];
         }
@@ -312,10 +322,9 @@ pages_reserve_kernel(PagedDev p, int layer, const int32_t* __restrict__ offs, co
                 if (i >= items || !copied[u]) continue;
                 const int k = start[i] - got;
                 if (k < 0 || k >= taken) continue;
-                const int old = last[i];
                 p.table[static_cast<size_t>(at[u]) * p.max_pages + (len[u] >> p.shift)] = list[k];
-                atomicSub(&p.refs[old], 1);                      // (at least one holder is left: no page becomes free here)
-                copies[atomicAdd(&s_copies, 1)] = int4{old, list[k], len[u] & ((1 << p.shift) - 1), 0};
+                atomicSub(&p.refs[old[u]], 1);                   // (at least one holder is left: no page becomes free here)
+                copies[atomicAdd(&s_copies, 1)] = int4{old[u], list[k], len[u] & ((1 << p.shift) - 1), 0};
             }
             got += taken;
             if (found <= room) w0 += kPlan;                      // else the same words again, less what was taken
