@@ -9,6 +9,17 @@ namespace qtale {
 // would be rounded first, and at 10^10 by more than an exponent has room for).  This one is a row's that has seen no key.
 constexpr float kPagedNone = -3.0e38f;
 
+// Probabilities are 2^(score - reference point + lift).  fp16 ends at 2^16 and has all its bits down to 2^-14 only: with the largest probability at 2^0
+// those 15 nats below it, all of the output where its value is about zero, would keep a few bits or none, while the 32-bit denominator has them.
+// So the largest is 2^lift when the reference point moves.  In the kernel for few columns that is free, and a score passes the reference point by
+// kDecodeHead at most.  In chunks, where the sum of a lane's 32 probabilities has to stay below fp16's end, each power of two is room less for later
+// scores, and more tiles move the reference point: us at lift 0 / 8 / 9 / 10 / 11, 4 x 4096 tokens, heads of 128, 576 / 585 / 582 / 591 / 606; 2 x 700 on
+// 1400, heads of 64, 44.4 / 44.7 / 45.1 / 46.8 / 48.1.  A probability is then off by 2^-11 of itself (two terms: 2^-22), or by 2^-34 (2^-37) of the
+// largest one if that is more.  bf16 has the exponents of 32 bits and no use for it.
+template <bool BF16> constexpr float kDecodeLift = BF16 ? 0.0f : 12.0f;
+template <bool BF16> constexpr float kChunkLift = BF16 ? 0.0f : 9.0f;
+constexpr float kDecodeHead = 3.5f;
+
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
@@ -83,8 +94,8 @@ struct SeqView {
 // that do not, and a masked key's probability of zero times an infinity or a NaN is NaN.  A finite sum has met neither, so it stands; one that
 // is not is done again here.  (About 45 cycles per key.)
 template <int D, bool BF16, int G>
-__device__ void redo_column(const PagedAttnDev& p, const KeySteps<G>& walk, int slot, int hk, const uint16_t* q, int place, int s0, int s1, float* num,
-                            float* m_out, float* l_out) {
+__device__ void redo_column(const PagedAttnDev& p, const KeySteps<G>& walk, int slot, int hk, const uint16_t* q, int place, int s0, int s1, float lift,
+                            float* num, float* m_out, float* l_out) {
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
     const int32_t* row = p.table + static_cast<size_t>(slot) * p.max_pages;
@@ -113,7 +124,7 @@ __device__ void redo_column(const PagedAttnDev& p, const KeySteps<G>& walk, int 
             score = sum;
         }
         const float m_new = fmaxf(m, wave_max(score)), alpha = __builtin_amdgcn_exp2f((m - m_new) * p.scale_log2);
-        const float w = seen ? __builtin_amdgcn_exp2f((score - m_new) * p.scale_log2) : 0.0f;
+        const float w = seen ? __builtin_amdgcn_exp2f(fmaf(score - m_new, p.scale_log2, lift)) : 0.0f;
         m = m_new;
         l = l * alpha + wave_sum(w);
 #pragma unroll

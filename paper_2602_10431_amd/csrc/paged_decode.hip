@@ -8,8 +8,8 @@
 // 16 consecutive keys lie in one page whatever its size, so a fragment has one base address, kept in scalar registers as a buffer whose length
 // ends at the last key: loads past it, and of pages that are gone, return zeros (a zero probability times what lies in unused memory, NaN
 // maybe, would be NaN).  Probabilities are 32-bit sums; as operands they go in as two 16-bit terms, p = hi + lo, through two products into one
-// accumulator, which leaves 2^-16 (bf16) or 2^-22 of them: the matrix cores have time (about a tenth of the stream's), and a bf16 probability
-// alone would add as much error as the output's own rounding.
+// accumulator, which leaves 2^-16 (bf16) or 2^-22 of them (fp16; or 2^-37 of the largest, kDecodeLift): the matrix cores have time (about a tenth of
+// the stream's), and a bf16 probability alone would add as much error as the output's own rounding.
 // Calls of more than 16 pairs per sequence come here while their workgroups fit the chip about once: each reads the sequence's keys, from L2 but for
 // the first, and the longest is done sooner than a workgroup of the chunk kernel, whose waves take a tile after the other (plan_paged_attention).
 // What bounds it is the stream of keys and values, and a CU takes in no more than about 50 GB/s (1 x 3000 keys, 32 workgroups: 33 us, whatever
@@ -151,17 +151,18 @@ again:                                                           // the pieces o
         }
         return S == 2 ? sum[0] : sum[0] + sum[S / 2 - 1];
     };
-    const float sc = p.scale_log2, top = 4.0f / sc;   // probabilities are 2^((score - m_run) sc), at most 2^4
+    const float sc = p.scale_log2;               // probabilities are 2^((score - m_run) sc + lift)
+    constexpr float LIFT = kDecodeLift<BF16>;
     float m_run = kPagedNone, l_run = 0.0f;
     float4_t o[F];
 #pragma unroll
     for (int f = 0; f < F; ++f) o[f] = float4_t{0.f, 0.f, 0.f, 0.f};
     auto absorb = [&](const float4_t& st0, const float4_t& st1) {   // 32 keys; masked scores are -inf
         float mx = fmaxf(fmaxf(fmaxf(st0[0], st0[1]), fmaxf(st0[2], st0[3])), fmaxf(fmaxf(st1[0], st1[1]), fmaxf(st1[2], st1[3])));
-        if (__any(mx > m_run + top)) {
+        if (__any((mx - m_run) * sc > kDecodeHead)) {
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));              // the column's largest score: all its lanes move together
-            const float m_new = mx > m_run + top ? mx : m_run;
+            const float m_new = (mx - m_run) * sc > kDecodeHead ? mx : m_run;
             const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
             l_run *= alpha;
 #pragma unroll
@@ -173,8 +174,8 @@ again:                                                           // the pieces o
         u32x4_t ph, pl;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(((e < 4 ? st0[e & 3] : st1[e & 3]) - m_run) * sc);
-            const float p1 = __builtin_amdgcn_exp2f(((e < 4 ? st0[(e & 3) + 1] : st1[(e & 3) + 1]) - m_run) * sc);
+            const float p0 = __builtin_amdgcn_exp2f(fmaf((e < 4 ? st0[e & 3] : st1[e & 3]) - m_run, sc, LIFT));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf((e < 4 ? st0[(e & 3) + 1] : st1[(e & 3) + 1]) - m_run, sc, LIFT));
             l_run += p0 + p1;
             const uint32_t h = A::pack(p0, p1);
             ph[e >> 1] = h;
@@ -295,7 +296,7 @@ again:                                                           // the pieces o
             if ((j & 3) != wave) continue;
             const int r = __ffs(static_cast<int>(redo)) - 1, i = (c0 + r) / p.rep, h = hk * p.rep + c0 + r - i * p.rep;
             float num[D / 64], m, l;
-            redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + i) * p.q_stride + h * D, s.first + i, first_step, last_step, num, &m, &l);
+            redo_column<D, BF16>(p, walk, s.slot, hk, p.q + (s.row0 + i) * p.q_stride + h * D, s.first + i, first_step, last_step, LIFT, num, &m, &l);
             put_column<D, BF16>(num, m, l, whole ? nullptr : piece + r * part_stride(D), p.out + (s.row0 + i) * p.out_stride + h * D);
         }
     }

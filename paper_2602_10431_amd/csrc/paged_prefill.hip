@@ -210,12 +210,12 @@ struct ColumnWave {
                     st[kf][r] = seen ? st[kf][r] : -INFINITY;
                 }
         }
-        // Probabilities are 2^(score sc - scaled(m_run)), one fused operation each; where scores are so large that the rounding of scaled(m_run)
+        // Probabilities are 2^(score sc - scaled(m_run) + lift), one fused operation each; where scores are so large that the rounding of scaled(m_run)
         // shows, put() finds a sum that is not finite or too small for its own largest term.  The reference point m_run need not be the maximum,
-        // only near it: it stays as long as the tile's probabilities add up to no more than kMost (then each fits fp16, and all have the bits
-        // of its normal numbers down to 2^-28 of the largest), which is seen from the sum that is needed anyway.  Finding the maximum, meeting
-        // the other half of the column and rescaling the sums are left to the tiles that break it: the first, and few after it.
-        constexpr float kMost = 16384.0f;
+        // only near it: it stays as long as the lane's probabilities of the tile add up to no more than kMost (for fp16 its largest number, so each
+        // fits), which is seen from the sum that is needed anyway.  Finding the maximum, meeting the other half of the column and rescaling the
+        // sums are left to the tiles that break it: the first, and few after it.
+        constexpr float kMost = BF16 ? 16384.0f : 65504.0f;
         float sum = weigh(sc);
         if (__any(!(sum <= kMost))) {
             float mx = -INFINITY;
@@ -240,7 +240,7 @@ struct ColumnWave {
 
     // Scores -> probabilities as operands; their sum, in 32 bits.
     __device__ __forceinline__ float weigh(float sc) {
-        const float ms = scaled(m_run, sc);
+        const float ms = scaled(m_run, sc) - kChunkLift<BF16>;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int kf = 0; kf < 2; ++kf)
@@ -302,7 +302,8 @@ struct ColumnWave {
     __device__ __forceinline__ void put(const PagedAttnDev& p, const SeqView& s, const KeySteps<kTileKeys>& walk, int hk, int t0, int t1, int z, int ranges, float l_tot) {
         const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
         // columns whose sum is not finite, or below the one that the largest term is (redo_column): both lanes of a column are left out below
-        float zero = m_run > kPagedNone && l_tot < 0.25f ? 1.0f : l_tot * 0.0f;
+        constexpr float LEAST = BF16 ? 0.25f : 128.0f;           // a quarter of 2^lift
+        float zero = m_run > kPagedNone && l_tot < LEAST ? 1.0f : l_tot * 0.0f;
 #pragma unroll
         for (int f = 0; f < DF; ++f)
 #pragma unroll
@@ -315,7 +316,7 @@ struct ColumnWave {
             const int qj = __shfl(qi, j, 64), hj = __shfl(head, j, 64);
             const size_t row = s.row0 + qj;
             float num[D / 64], m, l;
-            redo_column<D, BF16>(p, walk, s.slot, hk, p.q + row * p.q_stride + hj * D, s.first + qj, t0, t1, num, &m, &l);
+            redo_column<D, BF16>(p, walk, s.slot, hk, p.q + row * p.q_stride + hj * D, s.first + qj, t0, t1, kChunkLift<BF16>, num, &m, &l);
             put_column<D, BF16>(num, m, l, SPLIT && ranges > 1 ? p.part + ((row * p.nh + hj) * p.ranges + z) * part_stride(D) : nullptr, p.out + row * p.out_stride + hj * D);
         }
         if (!mine) return;
