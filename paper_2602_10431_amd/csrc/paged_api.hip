@@ -181,7 +181,7 @@ int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged
     const PagedAttnPlan plan = plan_paged_attention(attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B, m.max_new, m.max_len, attn->window, attn->sinks);
     if (plan.too_large) return QTALE_ERR_UNSUPPORTED;
     if ((e = check_workspace(workspace, workspace_bytes, plan.bytes))) return e;
-    PagedAttnDev a = attn_device(kv, layer, attn, m);
+    PagedAttnDev a = attn_device(kv, layer, attn, m, T);
     a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.offs = seq_offsets; a.slots = slots; a.first = first; a.B = B;
     HIP_TRY(launch_paged_attention(a, plan, kv->head_dim, kv->dtype == QTALE_ACT_BF16, T, static_cast<float*>(workspace), stream_of(stream)));

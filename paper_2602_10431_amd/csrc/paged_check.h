@@ -68,12 +68,14 @@ inline PagedAttnBounds attn_bounds(const qtale_paged_attn* a, const qtale_paged_
     return {a->max_new > 0 ? std::min(a->max_new, T) : T, a->max_len > 0 ? std::min(a->max_len, most) : most};
 }
 
-inline PagedAttnDev attn_device(const qtale_paged_kv* kv, int layer, const qtale_paged_attn* attn, const PagedAttnBounds& m) {
+inline PagedAttnDev attn_device(const qtale_paged_kv* kv, int layer, const qtale_paged_attn* attn, const PagedAttnBounds& m, int T) {
     const PagedDev p = paged_device(kv, layer);
     PagedAttnDev a{};
     a.k = p.k; a.v = p.v; a.table = p.table; a.len = p.len;
     a.nh = attn->n_heads; a.nkv = p.nkv; a.rep = attn->n_heads / p.nkv; a.shift = p.shift; a.max_pages = p.max_pages; a.n_slots = p.n_slots;
-    a.n_pages = p.n_pages; a.window = attn->window; a.sinks = attn->window > 0 ? attn->sinks : 0; a.max_len = m.max_len;
+    a.n_pages = p.n_pages; a.sinks = attn->window > 0 ? attn->sinks : 0; a.max_len = m.max_len;
+    // places begin at -T (rows before their slot's begin), so that place - window stays in 32 bits; windows beyond the cache are all the same
+    a.window = std::min(attn->window, INT32_MAX - T);
     a.scale_log2 = 1.4426950408889634f * attn->scale;
     return a;
 }

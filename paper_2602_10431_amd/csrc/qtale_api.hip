@@ -244,7 +244,7 @@ int paged_attention_block(qtale_ctx* ctx, const qtale_layer_cfg* c, const PagedC
     const PagedAttnBounds m = attn_bounds(pc.attn, pc.kv, M_max);
     const PagedAttnPlan plan = plan_paged_attention(nh, nkv, d, M_max, B, m.max_new, m.max_len, pc.attn->window, pc.attn->sinks);
     if (plan.too_large) return QTALE_ERR_UNSUPPORTED;
-    PagedAttnDev a = attn_device(pc.kv, pc.layer, pc.attn, m);
+    PagedAttnDev a = attn_device(pc.kv, pc.layer, pc.attn, m, M_max);
     a.q = qkv; a.q_stride = width; a.out = reinterpret_cast<uint16_t*>(ws.attn); a.out_stride = nh * d;
     a.offs = ws.cu_exec; a.slots = pc.slots; a.first = ws.kv_old; a.B = B;
     HIP_TRY(launch_paged_attention(a, plan, d, 0, M_max, pc.attn_ws, stream));
