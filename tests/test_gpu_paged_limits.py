@@ -1,5 +1,5 @@
 """Attention over pages at the ends of its arguments' ranges (run with -m gpu): windows up to the largest 32-bit number, with queries whose places lie
-before their slot's begin."""
+before their slot's begin; the same call again and again."""
 import pytest
 import torch
 
@@ -32,3 +32,18 @@ def test_a_window_without_end(qt, new, d, nkv, rep, max_len, window, sinks):
     assert bool(((got.double() - want).abs() <= attention_bound(want, size, q.dtype, False)).all())
     assert bool(((plain.double() - want).abs() <= attention_bound(want, size, q.dtype, False)).all())
     assert bool((want.abs().amax((1, 2)) > 0).any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("new,old,rep,nkv,d,bound", [([1, 1, 1], [3000, 50, 700], 4, 2, 128, 0), ([1] * 5, [30, 900, 0, 64, 500], 1, 60, 64, 0),
+                                                     ([70, 1, 200], [3000, 50, 700], 4, 2, 128, 30000), ([64] * 16, [1000] * 16, 4, 8, 64, 0),
+                                                     ([1400, 1300], [2000, 900], 16, 8, 128, 0)])
+def test_repeated_calls_give_the_bits_of_the_first(qt, new, old, rep, nkv, d, bound, dtype):
+    lens = [o + n for o, n in zip(old, new)]
+    kv, slots = random_cache(qt, lens, 32, nkv, d, dtype, 5)
+    q = torch.randn(sum(new), rep * nkv, d, generator=torch.Generator().manual_seed(6)).to(dtype).cuda()
+    call = lambda: qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), max_new=max(new), max_len=bound or max(lens))
+    one = call()
+    assert bool(torch.isfinite(one).all())
+    for _ in range(4):
+        assert torch.equal(one, call())
