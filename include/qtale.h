@@ -343,7 +343,8 @@ int qtale_rope_frequencies(int rotary_dim, float base, int scaling, float factor
 /* Turns the queries and the new keys of T tokens and stores keys and values into the pages of one layer.  q [T][n_heads * head_dim],
  * k, v [T][n_kv_heads * head_dim], q_out like q (may be q itself): kv->dtype, *_stride elements between tokens (a multiple of 8), 16-byte aligned.
  *   seq_offsets [B+1], positions [T] (absolute, for the angles); first [B]: entry of each sequence's first new token in its slot (nullable:
- *   kv_len minus its new tokens).  Entries at or past kv_len, and those without a page, are not stored. */
+ *   kv_len minus its new tokens, which is that entry only where qtale_pages_reserve has dropped none of them: after a call that may find
+ *   the pool empty pass the `first` that it gave, or kept entries are overwritten).  Entries at or past kv_len, and those without a page, are not stored. */
 int qtale_paged_rope_append(const qtale_paged_kv* kv, int layer, const qtale_rope* rope, const void* q, int64_t q_stride,
                             const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
                             int n_heads, int T, const int32_t* seq_offsets, const int32_t* slots, const int32_t* first, int B,
@@ -351,7 +352,7 @@ int qtale_paged_rope_append(const qtale_paged_kv* kv, int layer, const qtale_rop
 
 /* Causal attention of T new tokens over the pages of one layer, from one token per sequence to whole prompts:
  *   out_p = sum_j softmax_j(scale q_p . k_j) v_j,  j <= p, j < kv_len, page of j present, and (window == 0 or j > p - window or j < sinks),
- * p = first[b] + i for token i of sequence b.  A token that sees no entry gets zeros.  Head h reads kv head h / (n_heads / n_kv_heads).
+ * p = first[b] + i for token i of sequence b (first as in qtale_paged_rope_append).  A token that sees no entry gets zeros.  Head h reads kv head h / (n_heads / n_kv_heads).
  * q and out [T][n_heads * head_dim], *_stride elements between tokens (q: a multiple of 8, 16-byte aligned; out: of 4, 8-byte aligned). */
 typedef struct {
     int n_heads;
@@ -372,7 +373,8 @@ int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged
  *   kv      fp16, of cfg's kv heads and head size; slots [B] as everywhere (nullable: sequence b is slot b); B <= 2048
  *   rope    replaces cfg->rope_base;  attn: window, sinks, scale and bounds (max_new: of a call's tokens per sequence; n_heads = cfg->n_heads)
  *   missing nullable [n_layers] out: pages that the pool could not give in a layer.  Tokens without a place are dropped from that layer's
- *           cache (their own queries see what is there), as the newest tokens are when a qtale_kv is full.
+ *           cache (their own queries see what is there), as the newest tokens are when a qtale_kv is full.  Left as it is by calls that ask
+ *           for no pages, because T is 0 or the ratio rounds to no token: set it to 0 before such a call.
  *   workspace >= qtale_paged_stack_workspace_bytes(cfg, kv, T, B) bytes, 256-byte aligned */
 size_t qtale_paged_stack_workspace_bytes(const qtale_layer_cfg* cfg, const qtale_paged_kv* kv, int max_tokens, int max_seqs);
 int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, int n_layers, int first_layer,
