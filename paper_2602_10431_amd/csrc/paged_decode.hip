@@ -36,6 +36,8 @@ __device__ __forceinline__ int seq_units(const PagedAttnDev& p, int b) {
 // STREAM: keys as non-temporal loads too, not only values.  Where the workgroups fill the chip evenly (spans, or many of them) the stream gains, us
 // without / with: 33 x 3000 keys of 8 kv heads 74 / 69, 20 x 6000 85 / 80, heads of 64 49 / 47; 64 x 2048 of 32 kv heads 324 / 313, 128 x 1000 of 8
 // 81.7 / 79.3; where some CUs are left with one workgroup more than others those have less of it each: 48 x 1028 37.6 / 40.8, 100 x 2000 139 / 142.
+// Heads of 64 gain it with spans only, however many workgroups: 128 x 1000 keys of 8 kv heads 43.0 / 42.6, 128 x 2000 81.1 / 81.7, 150 x 1500 73.2 / 74.7,
+// 256 x 1000 81.9 / 82.7, 200 x 2000 of 1000 to 3000 137 / 143.
 template <int D, bool BF16, bool SPANS, bool STREAM>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : 3)
 paged_decode_kernel(PagedAttnDev p) {
