@@ -34,6 +34,7 @@ PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max
     // adding the ranges costs, about 24 tiles of time)
     const int64_t wgs = std::max<int64_t>(items * nkv, 1), tiles = (seen + kChunkTileKeys - 1) / kChunkTileKeys, two = 2 * cus;
     const bool cut = tiles * (two - wgs) > 24 * two;
+    // (Figures of chunks in fp16, here and below, are from before kChunkLift, which adds 1 to 2 % to every form.)
     // The decode kernel takes sequences of up to sixteen columns, for which a chunk's workgroup would run mostly empty, and larger ones while its
     // workgroups, each walking all keys, fill the chip about once.  us, it / chunk kernel, heads of 128, 4 per kv head (8): 1 x 32 tokens on 700
     // keys 12 / 19, on 1500 18 / 28, on 4000 (cut) 40 / 24; 4 x 64 on 300 13 / 17, on 700 20 / 22, on 1500 35 / 31; 16 x 8 on 1500 23 / 32, on 4000

@@ -15,9 +15,10 @@
 // Probabilities go into the second product rounded to 16 bits, which adds about as much error as the output's own rounding (fp16 2.7e-4 where the
 // output's alone is 2.1e-4, bf16 2.3e-3 / 1.7e-3); the second term that the kernel for few columns spends on it would be half as many products again.
 //
-// What bounds it is the chip's power: the same call on zeros, at the clock that those leave, takes 455 us where random data takes 575 (4 x 4096 tokens, 32
-// heads on 8 kv heads of 128, the wide form: 950 TFLOP/s; a library product of 8192^3 reaches 1150).  500 tokens on 24000 take 206 us, 960 TFLOP/s;
-// heads of 64, where a score costs half the products and as much softmax, 2 x 700 on 1400 40 to 45 us, 560 to 630 TFLOP/s.
+// What bounds it is the chip's power: the same call on zeros, at the clock that those leave, takes 457 us where random data takes 570 to 597, card by card
+// (4 x 4096 tokens, 32 heads on 8 kv heads of 128, the wide form: 920 to 960 TFLOP/s; a library product of 8192^3 reaches 1150).  500 tokens on 24000 take
+// 204 to 214 us, 930 to 970 TFLOP/s.  Heads of 64, where a score costs half the products and as much softmax: 4 x 4096 325 us, 850 TFLOP/s; 350 and 1050
+// tokens on 700 and 2100 44 us, 390 TFLOP/s, with the long prompt on the long cache 58 us, 440: one uneven round of workgroups.
 #include "paged_attn.h"
 
 namespace qtale {

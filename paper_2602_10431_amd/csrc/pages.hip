@@ -2,7 +2,7 @@
 //
 // Everything is decided on the device, because what a layer's cache needs is known there only: a layer holds the tokens that executed it.
 // What bounds these kernels is latency, chains of dependent loads, except where contents move.  us: room in one layer for a token of 1 / 64 / 256
-// sequences 5.8 / 7.4 / 8.3 (with the launch that copies); in 32 layers for 32 sequences, 24 of them with a page to copy, 12.7, and 34.6 for the copies
+// sequences 5.8 / 7.4 / 8.3 (with the launch that copies); in 32 layers for 32 sequences, 24 of them with a page to copy, 12.8, and 34.6 for the copies
 // (190 MB read and written, 5.6 TB/s); fork, release, trim 4.6 to 7.4; compaction 6.8 to plan, 230 to move pages at 5.2 TB/s.
 // Every result is a function of the state before the call alone: pages are taken lowest free index first, in the order of layers, then of
 // the call's sequences, then of the pages' places; the counts are integers, so the order of their atomic updates does not show.
