@@ -235,6 +235,33 @@ int qtale_linear_w4a16(const qtale_qlinear* w, int bits, int group, const void* 
 int qtale_swiglu_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, int bits, int group,
                        const void* A, int M, void* out, void* stream);
 
+/* ---- low-rank adapters of many requests beside a shared projection -----------------------------------------
+ * Row i of a call has adapter a = adapter[i] (int32 device [M]; a number outside 0 .. n_adapters - 1: none):
+ *   y_i = W A_i + scale[a] * up_a (down_a A_i),   W the quantized linear, sums in 32 bits.
+ * The inner values down_a A_i are held in 32 bits between the two products; they enter the second one as fp16 of their row's power of two.
+ * The shared product is rounded to fp16 where it leaves its kernel, and the sum once more. */
+typedef struct {
+    const void* down;          /* [n_adapters][max_rank][K] fp16, 16-byte aligned */
+    const void* up;            /* [n_adapters][N][max_rank] fp16, 16-byte aligned */
+    const int32_t* rank;       /* device [n_adapters], 0 .. max_rank each (nullable: max_rank): what lies past an adapter's rank is not used */
+    const float* scale;        /* device [n_adapters] (nullable: 1) */
+    int n_adapters, max_rank;  /* max_rank a multiple of 8, at most 128 */
+    int N, K;                  /* of the linear */
+} qtale_lora;
+
+/* Scratch of the two calls below with M rows: of a linear with `a` (b null), or of a gate/up pair with `a` and `b` (a pair with one of them alone
+ * needs no more than with that one twice). */
+size_t qtale_lora_workspace_bytes(const qtale_lora* a, const qtale_lora* b, int M);
+
+/* qtale_linear_w4a16 with adapters. */
+int qtale_linear_lora_w4a16(const qtale_qlinear* w, int bits, int group, const qtale_lora* lora, const int32_t* adapter, const void* A, int M,
+                            void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* qtale_swiglu_w4a16 with adapters on gate and up (either nullable): silu(gate_i) * up_i of the y above. */
+int qtale_swiglu_lora_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, int bits, int group, const qtale_lora* lora_gate,
+                            const qtale_lora* lora_up, const int32_t* adapter, const void* A, int M, void* out, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* ---- HIP graph of one stack forward (launch-overhead removal, App. B.2 future work) -------------------
  * qtale_graph_capture_stack records the kernels of ONE qtale_stack_forward call with exactly these
  * arguments (no dbg_hidden) into a HIP graph and instantiates it; nothing executes during capture.
@@ -258,7 +285,7 @@ void qtale_graph_destroy(qtale_graph* graph);
  * A layer's cache holds the tokens that executed it, so its length differs from layer to layer and only the device knows it.  Instead of
  * `cap` entries per layer and sequence, a paged cache takes pages of page_size tokens from one pool as they are needed; sequences that begin
  * alike share them.
- *   page    keys and values of page_size consecutive tokens of one slot: [n_kv_heads][page_size][head_dim] each, fp16 or bf16
+ *   page    keys and values of page_size consecutive tokens of one slot: [n_kv_heads][page_size][head_dim] each, fp16 or bf16, or in 4 bits
  *   slot    the cache of one sequence; 0 .. n_slots - 1, the same number in every layer
  *   table   page of every page_size tokens of a slot, per layer; -1 = none: its tokens are not seen by attention, and not stored by an append
  * The caller allocates all arrays; qtale_pages_init makes an empty cache of them.  Invariants that the calls keep: page_refs[p] is the number
@@ -267,7 +294,7 @@ void qtale_graph_destroy(qtale_graph* graph);
  * out of range is skipped.  The calls only enqueue kernels (no synchronisation, no allocation; they can be captured into a graph), and
  * every result, page numbers included, depends on the state and the arguments alone. */
 typedef struct {
-    void* k_pages;          /* [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned */
+    void* k_pages;          /* [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned (4 bits: see QTALE_KV_INT4) */
     void* v_pages;
     int32_t* page_refs;     /* [n_pages] table entries that name the page */
     uint32_t* free_bits;    /* [ceil(n_pages / 32)] bit p % 32 of word p / 32: page p is free */
@@ -278,8 +305,21 @@ typedef struct {
     int page_size;          /* 16, 32, 64, ..., 1024 */
     int n_kv_heads, head_dim;   /* head_dim 64 or 128 */
     int n_layers, n_slots, max_pages;
-    int dtype;              /* QTALE_ACT_FP16 | QTALE_ACT_BF16, of keys and values (and of the queries and outputs of the calls on them) */
+    int dtype;              /* QTALE_ACT_FP16 | QTALE_ACT_BF16, of keys and values (and of the queries and outputs of the calls on them);
+                             * plus QTALE_KV_INT4: that is the type of what goes in and comes out, the pages hold 4 bits */
 } qtale_paged_kv;
+
+/* Pages in 4 bits.  The d values x of a token's key or value at one kv head share a scale s, of the cache's 16-bit type T, and a zero point z, as
+ * the weights' groups do: lo = min(0, min x), hi = max(0, max x), s = T((hi - lo) / 15) (1 if that is 0), z = min(rint(-lo / s), 15),
+ * code = clamp(rint(x / s) + z, 0, 15), half to even; a code stands for (code - z) * s.  A row with a value that is not finite has s = NaN: it
+ * reads as NaN.  Keys are turned in 64 bits and rounded to T (what a 16-bit page would hold) before that.
+ * A page is [n_kv_heads] blocks of page_size * (head_dim / 2 + 4) bytes: the codes, then per token a 32-bit word s | z << 16.
+ * (64 to 16 bits, here and in s, by way of 32.)
+ *   key codes    [page_size][head_dim / 8] words: column 8 w + 2 i of a token at bits 4 i of its word w, column 8 w + 2 i + 1 at bits 16 + 4 i
+ *   value codes  [page_size / 4][head_dim / 4][2] words, tokens by fours: column 4 Q + i of token 2 p of the four at bits 4 i of word (Q, p),
+ *                of token 2 p + 1 at bits 16 + 4 i
+ * All calls on a qtale_paged_kv take either form; a fork's copy of a shared page copies what its tokens hold bit by bit. */
+enum { QTALE_KV_INT4 = 4 };
 
 /* All pages free, all slots empty. */
 int qtale_pages_init(const qtale_paged_kv* kv, void* stream);
@@ -350,6 +390,12 @@ int qtale_paged_rope_append(const qtale_paged_kv* kv, int layer, const qtale_rop
                             int n_heads, int T, const int32_t* seq_offsets, const int32_t* slots, const int32_t* first, int B,
                             const int32_t* positions, void* stream);
 
+/* The values that entries of one layer's slots stand for, in kv->dtype's 16-bit type: row i of sequence b is entry first[b] + i (first [B]; nullable: its
+ * slot's last entries) of its slot.  k, v [T][n_kv_heads * head_dim], strides as above.  Entries outside 0 .. kv_len - 1, without a page or
+ * of a slot that does not exist are zeros; rows past the last sequence are left as they are. */
+int qtale_paged_read(const qtale_paged_kv* kv, int layer, void* k, int64_t k_stride, void* v, int64_t v_stride, int T,
+                     const int32_t* seq_offsets, const int32_t* slots, const int32_t* first, int B, void* stream);
+
 /* Causal attention of T new tokens over the pages of one layer, from one token per sequence to whole prompts:
  *   out_p = sum_j softmax_j(scale q_p . k_j) v_j,  j <= p, j < kv_len, page of j present, and (window == 0 or j > p - window or j < sinks),
  * p = first[b] + i for token i of sequence b (first as in qtale_paged_rope_append).  A token that sees no entry gets zeros.  Head h reads kv head h / (n_heads / n_kv_heads).
@@ -370,7 +416,7 @@ int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged
 /* n_layers layers as in qtale_stack_forward, on a paged cache: layer l of the call uses the cache's layer first_layer + l.  In every layer the
  * executed tokens get room in their sequences' slots (qtale_pages_reserve), their queries and keys are turned (positions are those of the
  * tokens), keys and values go to the pages, and the queries attend to what their slot holds, which is executed tokens only.
- *   kv      fp16, of cfg's kv heads and head size; slots [B] as everywhere (nullable: sequence b is slot b); B <= 2048
+ *   kv      fp16 (or fp16 in 4 bits), of cfg's kv heads and head size; slots [B] as everywhere (nullable: sequence b is slot b); B <= 2048
  *   rope    replaces cfg->rope_base;  attn: window, sinks, scale and bounds (max_new: of a call's tokens per sequence; n_heads = cfg->n_heads)
  *   missing nullable [n_layers] out: pages that the pool could not give in a layer.  Tokens without a place are dropped from that layer's
  *           cache (their own queries see what is there), as the newest tokens are when a qtale_kv is full.  Left as it is by calls that ask

@@ -13,6 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libqtale.so")
 
 QTALE_ACT_FP16, QTALE_ACT_BF16 = 0, 1
+QTALE_KV_INT4 = 4
 QTALE_MODE_RATIO, QTALE_MODE_THRESHOLD = 0, 1
 QTALE_PROF_CLASSES = 10
 PROF_NAMES = ["router", "select", "norm1", "qkv_gemm", "rope_append", "attention", "o_gemm", "norm2",
@@ -29,7 +30,7 @@ EXPORTS = ["qtale_strerror", "qtale_create", "qtale_destroy", "qtale_set_exec_ra
            "qtale_pages_init", "qtale_pages_workspace_bytes", "qtale_pages_fork", "qtale_pages_reserve", "qtale_pages_release",
            "qtale_pages_trim", "qtale_pages_compact", "qtale_pages_copy", "qtale_rope_frequencies", "qtale_paged_rope_append",
            "qtale_paged_attention_workspace_bytes", "qtale_paged_attention", "qtale_paged_stack_workspace_bytes",
-           "qtale_paged_stack_forward"]
+           "qtale_paged_stack_forward", "qtale_paged_read", "qtale_lora_workspace_bytes", "qtale_linear_lora_w4a16", "qtale_swiglu_lora_w4a16"]
 QTALE_THETA_GRID = 50
 QTALE_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 QTALE_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "parts": 4}
@@ -69,6 +70,11 @@ class qtale_paged_kv(C.Structure):
                 ("table", C.c_void_p), ("kv_len", C.c_void_p), ("kv_cap", C.c_void_p), ("n_pages", C.c_int),
                 ("page_size", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("n_layers", C.c_int),
                 ("n_slots", C.c_int), ("max_pages", C.c_int), ("dtype", C.c_int)]
+
+
+class qtale_lora(C.Structure):
+    _fields_ = [("down", C.c_void_p), ("up", C.c_void_p), ("rank", C.c_void_p), ("scale", C.c_void_p), ("n_adapters", C.c_int),
+                ("max_rank", C.c_int), ("N", C.c_int), ("K", C.c_int)]
 
 
 class qtale_rope(C.Structure):
@@ -149,8 +155,14 @@ def load_library():
     lib.qtale_paged_stack_workspace_bytes.restype = sz
     lib.qtale_paged_stack_forward.argtypes = [vp, C.POINTER(qtale_layer_cfg), C.POINTER(qtale_layer_weights), i, i, vp, i, vp, i, vp, pk, vp,
                                               C.POINTER(qtale_rope), C.POINTER(qtale_paged_attn), vp, vp, vp, vp, vp, sz, vp]
+    lib.qtale_paged_read.argtypes = [pk, i, vp, i64, vp, i64, i, vp, vp, vp, i, vp]
+    lo, ql = C.POINTER(qtale_lora), C.POINTER(qtale_qlinear)
+    lib.qtale_lora_workspace_bytes.argtypes = [lo, lo, i]
+    lib.qtale_lora_workspace_bytes.restype = sz
+    lib.qtale_linear_lora_w4a16.argtypes = [ql, i, i, lo, vp, vp, i, vp, vp, sz, vp]
+    lib.qtale_swiglu_lora_w4a16.argtypes = [ql, ql, i, i, lo, lo, vp, vp, i, vp, vp, sz, vp]
     for name in EXPORTS:
-        if name not in ("qtale_strerror", "qtale_prepacked_bytes", "qtale_workspace_bytes",
+        if name not in ("qtale_lora_workspace_bytes", "qtale_strerror", "qtale_prepacked_bytes", "qtale_workspace_bytes",
                         "qtale_calibration_scratch_bytes", "qtale_graph_destroy", "qtale_static_scratch_bytes",
                         "qtale_pages_workspace_bytes", "qtale_paged_attention_workspace_bytes",
                         "qtale_paged_stack_workspace_bytes"):
@@ -484,6 +496,81 @@ def qtale_swiglu_w4a16(gate, up, A, out=None):
     return out
 
 
+# ---- low-rank adapters ------------------------------------------------------------------------------------------
+class Lora:
+    """Adapters of one linear: down [n, r, K] and up [n, N, r] fp16 CUDA tensors; rank int32 [n] and scale fp32 [n] (None: r and 1 for all).
+    A largest rank r that is no multiple of 8 is padded once, here."""
+
+    def __init__(self, down, up, rank=None, scale=None):
+        n, r, K = down.shape
+        assert up.shape[0] == n and up.shape[2] == r and down.dtype == up.dtype == torch.float16 and down.device == up.device
+        if r % 8:
+            if rank is None:
+                rank = torch.full((n,), r, dtype=torch.int32, device=down.device)
+            down, up = torch.nn.functional.pad(down, (0, 0, 0, -r % 8)), torch.nn.functional.pad(up, (0, -r % 8))
+        assert rank is None or (rank.dtype == torch.int32 and rank.shape == (n,) and rank.is_contiguous() and rank.device == down.device)
+        assert scale is None or (scale.dtype == torch.float32 and scale.shape == (n,) and scale.is_contiguous() and scale.device == down.device)
+        self.down, self.up, self.rank, self.scale = down.contiguous(), up.contiguous(), rank, scale
+        self.n, self.max_rank, self.N, self.K, self.device = n, self.down.shape[1], self.up.shape[1], K, down.device
+        at = lambda t: None if t is None else t.data_ptr()
+        self._c = qtale_lora(self.down.data_ptr(), self.up.data_ptr(), at(rank), at(scale), n, self.max_rank, self.N, K)
+        self._ref = C.byref(self._c)
+
+    def c_struct(self):
+        return self._c
+
+
+def alloc_lora_workspace(loras, M):
+    """Scratch of qtale_linear_lora_w4a16 ([lora]) or qtale_swiglu_lora_w4a16 ([gate's, up's]; None for one that has none) with up to M rows."""
+    pair = [l for l in loras if l is not None]
+    a, b = pair[0], None if len(loras) == 1 else pair[-1]
+    n = load_library().qtale_lora_workspace_bytes(a._ref, None if b is None else b._ref, M)
+    if n == 0:
+        raise QtaleError(-1, "qtale_lora_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=a.device)
+
+
+def _lora_rows(adapter, A, lora, K):
+    """(address of the rows' adapters, of the rows)"""
+    assert A.dtype == torch.float16 and A.is_contiguous() and A.shape[1] == K and A.device == lora.device
+    return _ints(adapter, lora, A.shape[0]), A.data_ptr()
+
+
+def _lora_out(out, M, N, A):
+    if out is None:
+        return torch.empty((M, N), dtype=torch.float16, device=A.device)
+    assert out.shape == (M, N) and out.dtype == torch.float16 and out.is_contiguous() and out.device == A.device
+    return out
+
+
+def qtale_linear_lora_w4a16(qlin, lora, A, adapter, out=None, workspace=None):
+    """qtale_linear_w4a16 with row i's adapter adapter[i] of `lora` beside it (int32 [M]; a number that names none: no adapter)."""
+    M = A.shape[0]
+    out = _lora_out(out, M, qlin.N, A)
+    if workspace is None:
+        workspace = alloc_lora_workspace([lora], M)
+    s = qlin.c_struct()
+    ids, rows = _lora_rows(adapter, A, lora, qlin.K)
+    _check(load_library().qtale_linear_lora_w4a16(C.byref(s), qlin.bits, qlin.group, lora._ref, ids, rows, M, out.data_ptr(),
+                                                  *_scratch(workspace, lora), _stream_of(lora)), "qtale_linear_lora_w4a16")
+    return out
+
+
+def qtale_swiglu_lora_w4a16(gate, up, lora_gate, lora_up, A, adapter, out=None, workspace=None):
+    """qtale_swiglu_w4a16 with adapters on gate and up (either may be None)."""
+    M, lora = A.shape[0], lora_gate or lora_up
+    out = _lora_out(out, M, gate.N, A)
+    if workspace is None:
+        workspace = alloc_lora_workspace([lora_gate, lora_up], M)
+    g, u = gate.c_struct(), up.c_struct()
+    ids, rows = _lora_rows(adapter, A, lora, gate.K)
+    assert up.bits == gate.bits and up.group == gate.group
+    _check(load_library().qtale_swiglu_lora_w4a16(
+        C.byref(g), C.byref(u), gate.bits, gate.group, lora_gate._ref if lora_gate else None, lora_up._ref if lora_up else None, ids, rows, M,
+        out.data_ptr(), *_scratch(workspace, lora), _stream_of(lora)), "qtale_swiglu_lora_w4a16")
+    return out
+
+
 # ---- paged K/V cache ------------------------------------------------------------------------------------------
 # A decode step calls these once per layer with little work behind each call, so the checks are the few attribute reads that are enough, and the
 # stream's address is asked for without making a Stream object (2.7 us of about 10).
@@ -506,10 +593,18 @@ def _scratch(t, kv):
 
 class PagedKV:
     """Device arrays of a paged K/V cache (see qtale_paged_kv).  k, v: [n_pages, n_kv_heads, page_size, head_dim] fp16 or bf16; page_refs
-    [n_pages], free_bits [ceil(n_pages / 32)], table [n_layers, n_slots, max_pages], kv_len and kv_cap [n_layers, n_slots]: int32."""
+    [n_pages], free_bits [ceil(n_pages / 32)], table [n_layers, n_slots, max_pages], kv_len and kv_cap [n_layers, n_slots]: int32.
+    In 4 bits: k, v [n_pages, n_kv_heads, page_size * (head_dim / 2 + 4)] uint8, with head_dim and dtype (of what goes in and comes out) given."""
 
-    def __init__(self, k, v, page_refs, free_bits, table, kv_len, kv_cap):
-        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous()
+    def __init__(self, k, v, page_refs, free_bits, table, kv_len, kv_cap, dtype=None, head_dim=None):
+        assert k.shape == v.shape and k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous()
+        self.bits = 4 if k.dtype is torch.uint8 else 16
+        if self.bits == 4:
+            assert k.dim() == 3 and dtype in (torch.float16, torch.bfloat16) and head_dim and k.shape[2] % (head_dim // 2 + 4) == 0
+            self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = *k.shape[:2], k.shape[2] // (head_dim // 2 + 4), head_dim
+        else:
+            assert k.dim() == 4 and dtype in (None, k.dtype) and head_dim in (None, k.shape[3])
+            self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         assert table.dim() == 3 and kv_len.shape == kv_cap.shape == table.shape[:2]
         assert page_refs.shape == (k.shape[0],) and free_bits.shape == ((k.shape[0] + 31) // 32,)
         for t in (page_refs, free_bits, table, kv_len, kv_cap):
@@ -518,21 +613,24 @@ class PagedKV:
             assert t.device == k.device
         self.k, self.v, self.page_refs, self.free_bits = k, v, page_refs, free_bits
         self.table, self.kv_len, self.kv_cap = table, kv_len, kv_cap
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.n_layers, self.n_slots, self.max_pages = table.shape
-        self.device, self.dtype = k.device, k.dtype
+        self.device, self.dtype = k.device, k.dtype if dtype is None else dtype
         self._c = qtale_paged_kv(k.data_ptr(), v.data_ptr(), page_refs.data_ptr(), free_bits.data_ptr(), table.data_ptr(),
                                  kv_len.data_ptr(), kv_cap.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
-                                 self.n_layers, self.n_slots, self.max_pages, _act_code(k.dtype))
+                                 self.n_layers, self.n_slots, self.max_pages, _act_code(self.dtype) + (QTALE_KV_INT4 if self.bits == 4 else 0))
         self._ref = C.byref(self._c)
 
     @classmethod
-    def empty(cls, n_pages, page_size, n_kv_heads, head_dim, n_slots, max_pages, n_layers=1, dtype=torch.float16, device="cuda"):
-        """Allocates an empty cache."""
+    def empty(cls, n_pages, page_size, n_kv_heads, head_dim, n_slots, max_pages, n_layers=1, dtype=torch.float16, device="cuda", bits=16):
+        """Allocates an empty cache; bits: 16 or 4, of what the pages hold."""
+        assert bits in (16, 4), bits
         ints = lambda *size: torch.empty(size, dtype=torch.int32, device=device)
-        k, v = (torch.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype, device=device) for _ in range(2))
+        if bits == 4:
+            k, v = (torch.empty(n_pages, n_kv_heads, page_size * (head_dim // 2 + 4), dtype=torch.uint8, device=device) for _ in range(2))
+        else:
+            k, v = (torch.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype, device=device) for _ in range(2))
         kv = cls(k, v, ints(n_pages), ints((n_pages + 31) // 32), ints(n_layers, n_slots, max_pages), ints(n_layers, n_slots),
-                 ints(n_layers, n_slots))
+                 ints(n_layers, n_slots), dtype, head_dim)
         qtale_pages_init(kv)
         return kv
 
@@ -643,6 +741,18 @@ def qtale_paged_rope_append(kv, layer, rope, q, k, v, seq_offsets, positions, fi
         _ints(seq_offsets, kv, B + 1), _ints(slots, kv, B), _ints(first, kv, B), B, _ints(positions, kv, T), _stream_of(kv)),
         "qtale_paged_rope_append")
     return q_out
+
+
+def qtale_paged_read(kv, layer, seq_offsets, first=None, slots=None, k_out=None, v_out=None, T=None):
+    """The values that entries first[b] .. of the slots stand for: (k_out, v_out), [T, n_kv_heads, head_dim] in kv.dtype (None: new tensors for T rows)."""
+    B = seq_offsets.numel() - 1
+    if k_out is None or v_out is None:
+        T = next(t.shape[0] for t in (k_out, v_out) if t is not None) if T is None else T
+        k_out, v_out = (torch.empty((T, kv.n_kv_heads, kv.head_dim), dtype=kv.dtype, device=kv.device) if t is None else t for t in (k_out, v_out))
+    T, nkv = k_out.shape[0], kv.n_kv_heads
+    _check(load_library().qtale_paged_read(kv._ref, layer, *_heads(k_out, kv, T, nkv), *_heads(v_out, kv, T, nkv), T, _ints(seq_offsets, kv, B + 1),
+                                           _ints(slots, kv, B), _ints(first, kv, B), B, _stream_of(kv)), "qtale_paged_read")
+    return k_out, v_out
 
 
 def _paged_attn(kv, n_heads, max_new, max_len, window=0, sinks=0, scale=None):

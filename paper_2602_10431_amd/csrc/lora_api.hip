@@ -1,0 +1,100 @@
+// Host side of the adapters' C ABI (include/qtale.h): argument validation before any HIP call, then the launches.
+#include <algorithm>
+
+#include "lora_check.h"
+#include "qtale_kernels.h"
+
+using namespace qtale;
+
+namespace {
+
+#define HIP_TRY(expr)                                   \
+    do {                                                \
+        hipError_t e__ = (expr);                        \
+        if (e__ != hipSuccess) return QTALE_ERR_HIP;    \
+    } while (0)
+
+int check_base(const qtale_qlinear* w, int bits, int group) {
+    if (!w || w->N <= 0 || w->K <= 0) return QTALE_ERR_INVALID_ARG;
+    if (bits != 4 && bits != 3 && bits != 2) return QTALE_ERR_UNSUPPORTED;
+    if (group != 32 && group != 64 && group != 128) return QTALE_ERR_UNSUPPORTED;
+    return w->K % 8 != 0 || w->N % 8 != 0 ? QTALE_ERR_SHAPE : QTALE_OK;
+}
+
+int check_lora_call(const int32_t* adapter, const void* A, const void* out, const void* ws, size_t have, size_t need) {
+    if (!adapter || !A || !out || !ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0) return QTALE_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(out)) % 16 != 0) return QTALE_ERR_INVALID_ARG;
+    return have < need ? QTALE_ERR_WORKSPACE_TOO_SMALL : QTALE_OK;
+}
+
+// The shared product alone.
+hipError_t base_linear(const qtale_qlinear* w, int bits, int group, const void* A, int M, void* out, hipStream_t stream) {
+    GemmArgs g{};
+    g.A = A; g.M_max = M; g.rows_exact = 1; g.K = w->K; g.group = group; g.bits = bits; g.n_w = 1;
+    g.w[0] = {w->prepacked, w->N, w->K};
+    g.epilogue = EPI_STORE_F16; g.out = out; g.ldo = w->N;
+    return launch_gemm_w4a16(g, stream);
+}
+
+size_t rows_bytes(int M, int N) { return (static_cast<size_t>(M) * N * 2 + 255) / 256 * 256; }
+size_t inner_bytes(const qtale_lora* l, int M) { return l ? lora_inner_bytes(l->max_rank, M) : 0; }
+
+}  // namespace
+
+extern "C" {
+
+size_t qtale_lora_workspace_bytes(const qtale_lora* a, const qtale_lora* b, int M) {
+    if (!a || check_lora(a, a->N, a->K, false) || (b && check_lora(b, a->N, a->K, false)) || M < 0 || a->N <= 0 || a->K <= 0) return 0;
+    return 256 + inner_bytes(a, M) + inner_bytes(b, M) + (b ? 2 * rows_bytes(M, a->N) : 0);
+}
+
+int qtale_linear_lora_w4a16(const qtale_qlinear* w, int bits, int group, const qtale_lora* lora, const int32_t* adapter, const void* A, int M,
+                            void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    int e = check_base(w, bits, group);
+    if (e || (e = check_lora(lora, w->N, w->K, M > 0))) return e;
+    if (M < 0) return QTALE_ERR_INVALID_ARG;
+    if (M == 0) return QTALE_OK;
+    if (!w->prepacked) return QTALE_ERR_INVALID_ARG;
+    if ((e = check_lora_call(adapter, A, out, workspace, workspace_bytes, qtale_lora_workspace_bytes(lora, nullptr, M)))) return e;
+    const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const LoraDev l = lora_device(lora);
+    const LoraRows rows{adapter, nullptr, nullptr, M, 0};
+    float* inner = static_cast<float*>(workspace);
+    HIP_TRY(launch_lora_inner(l, rows, A, inner, s));
+    HIP_TRY(base_linear(w, bits, group, A, M, out, s));
+    HIP_TRY(launch_lora_add(l, rows, inner, out, w->N, 0, s));
+    return QTALE_OK;
+}
+
+int qtale_swiglu_lora_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, int bits, int group, const qtale_lora* lora_gate,
+                            const qtale_lora* lora_up, const int32_t* adapter, const void* A, int M, void* out, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    int e = check_base(gate, bits, group);
+    if (e || (e = check_base(up, bits, group))) return e;
+    if (gate->N != up->N || gate->K != up->K) return QTALE_ERR_SHAPE;
+    if (!lora_gate && !lora_up) return QTALE_ERR_INVALID_ARG;
+    if (lora_gate && (e = check_lora(lora_gate, gate->N, gate->K, M > 0))) return e;
+    if (lora_up && (e = check_lora(lora_up, up->N, up->K, M > 0))) return e;
+    if (M < 0) return QTALE_ERR_INVALID_ARG;
+    if (M == 0) return QTALE_OK;
+    if (!gate->prepacked || !up->prepacked) return QTALE_ERR_INVALID_ARG;
+    // (a size for one of them counts the rows' buffers too: the pair's size with the larger rank twice is enough for either)
+    const size_t need = 256 + inner_bytes(lora_gate, M) + inner_bytes(lora_up, M) + 2 * rows_bytes(M, gate->N);
+    if ((e = check_lora_call(adapter, A, out, workspace, workspace_bytes, need))) return e;
+    const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const LoraDev lg = lora_device(lora_gate), lu = lora_device(lora_up);
+    const LoraRows rows{adapter, nullptr, nullptr, M, 0};
+    char* at = static_cast<char*>(workspace);
+    float* inner_g = reinterpret_cast<float*>(at);
+    float* inner_u = reinterpret_cast<float*>(at += inner_bytes(lora_gate, M));
+    void* g = at += inner_bytes(lora_up, M);
+    void* u = at += rows_bytes(M, gate->N);
+    if (lg.n) HIP_TRY(launch_lora_inner(lg, rows, A, inner_g, s));
+    if (lu.n) HIP_TRY(launch_lora_inner(lu, rows, A, inner_u, s));
+    HIP_TRY(base_linear(gate, bits, group, A, M, g, s));
+    HIP_TRY(base_linear(up, bits, group, A, M, u, s));
+    HIP_TRY(launch_lora_swiglu(lg, lu, rows, inner_g, inner_u, g, u, out, gate->N, s));
+    return QTALE_OK;
+}
+
+}  // extern "C"

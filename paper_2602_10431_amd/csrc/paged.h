@@ -11,13 +11,16 @@
 namespace qtale {
 
 struct PagedDev {
-    uint16_t *k, *v;             // [n_pages][nkv][P][d] fp16 or bf16
+    uint16_t *k, *v;             // [n_pages][nkv][P][d] fp16 or bf16; q4: blocks of head_bytes (paged4.h)
     int32_t* refs;               // [n_pages]
     uint32_t* bits;              // [ceil(n_pages / 32)]
     int32_t* table;              // [n_layers][n_slots][max_pages]
     int32_t *len, *cap;          // [n_layers][n_slots]
     int n_pages, shift, nkv, d, n_layers, n_slots, max_pages, bf16;   // P = 1 << shift
+    int q4;                      // pages in 4 bits; bf16 is then the type of their scales and of what goes in and out
 };
+// bytes of a head in a page
+__host__ __device__ inline size_t head_bytes(const PagedDev& p) { return static_cast<size_t>(p.q4 ? p.d / 2 + 4 : 2 * p.d) << p.shift; }
 
 // ---- pages (pages.hip) ----------------------------------------------------------------------------
 constexpr int kReserveItems = 2048;              // (layer, sequence) pairs that a reserving workgroup holds at once; bound on B
@@ -57,6 +60,16 @@ struct PagedRopeArgs {
     SplitList copies;            // nullable: pages that the workgroups past the T rows copy
 };
 hipError_t launch_paged_rope(const PagedRopeArgs& a, hipStream_t stream);
+hipError_t launch_paged4_rope(const PagedRopeArgs& a, hipStream_t stream);   // pages in 4 bits (paged4_store.hip)
+
+struct PagedReadArgs {
+    PagedDev kv;                 // table and len of the layer
+    uint16_t *k, *v;
+    int64_t k_stride, v_stride;
+    int T, B;
+    const int32_t *seq_offsets, *slots, *first;
+};
+hipError_t launch_paged_read(const PagedReadArgs& a, hipStream_t stream);
 
 // ---- attention (paged_decode.hip, paged_prefill.hip) ----------------------------------------------
 struct PagedAttnDev {
@@ -69,6 +82,7 @@ struct PagedAttnDev {
     int B, nh, nkv, rep, shift, max_pages, n_slots, n_pages;
     int window, sinks, max_len;
     float scale_log2;
+    int bf16, q4;                // of the pages
     int take;                    // 0: every sequence; 1: only those of this kernel (the other one is launched too)
     // chunk kernel: column tiles (bound), key ranges that one may be cut into (1: none), workgroups that the call's ranges are to be, and the
     // ranges' sums [T * nh][ranges][part_stride(d)]
@@ -97,7 +111,8 @@ constexpr int part_stride(int d) { return d + 4; }   // floats of a column's sum
 PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks);
 size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B);   // of workspace, for any call of at most T tokens and B sequences
 // All launches of a call; a: everything but `take` and what follows it, which the plan says.
-hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int bf16, int T, float* workspace, hipStream_t stream);
+hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int T, float* workspace, hipStream_t stream);
+hipError_t launch_paged4_simple(const PagedAttnDev& a, int d, int T, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);
 hipError_t launch_paged_chunk(const PagedAttnDev& a, int groups, int d, int bf16, hipStream_t stream);
 hipError_t launch_chunk_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream);

@@ -159,6 +159,24 @@ int qtale_paged_rope_append(const qtale_paged_kv* kv, int layer, const qtale_rop
     return QTALE_OK;
 }
 
+int qtale_paged_read(const qtale_paged_kv* kv, int layer, void* k, int64_t k_stride, void* v, int64_t v_stride, int T, const int32_t* seq_offsets,
+                     const int32_t* slots, const int32_t* first, int B, void* stream) {
+    int e = check_paged(kv, true);
+    if (e) return e;
+    if (layer < 0 || layer >= kv->n_layers || T < 0 || B < 0) return QTALE_ERR_INVALID_ARG;
+    if (!slots && B > kv->n_slots) return QTALE_ERR_SHAPE;
+    if (T == 0) return QTALE_OK;
+    if (B == 0 || !k || !v || !seq_offsets) return QTALE_ERR_INVALID_ARG;
+    const int64_t row = static_cast<int64_t>(kv->n_kv_heads) * kv->head_dim;
+    if ((e = check_rows(k, k_stride, row, 8)) || (e = check_rows(v, v_stride, row, 8))) return e;
+    PagedReadArgs a{};
+    a.kv = paged_device(kv, layer);
+    a.k = static_cast<uint16_t*>(k); a.v = static_cast<uint16_t*>(v); a.k_stride = k_stride; a.v_stride = v_stride;
+    a.T = T; a.B = B; a.seq_offsets = seq_offsets; a.slots = slots; a.first = first;
+    HIP_TRY(launch_paged_read(a, stream_of(stream)));
+    return QTALE_OK;
+}
+
 size_t qtale_paged_attention_workspace_bytes(const qtale_paged_kv* kv, const qtale_paged_attn* attn, int T, int B) {
     if (check_paged(kv, false) || check_paged_attn(attn, kv) || T < 0 || B < 0) return 0;
     return T == 0 || B == 0 ? 256 : paged_attention_bytes(attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B);
@@ -184,7 +202,7 @@ int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged
     PagedAttnDev a = attn_device(kv, layer, attn, m, T);
     a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.offs = seq_offsets; a.slots = slots; a.first = first; a.B = B;
-    HIP_TRY(launch_paged_attention(a, plan, kv->head_dim, kv->dtype == QTALE_ACT_BF16, T, static_cast<float*>(workspace), stream_of(stream)));
+    HIP_TRY(launch_paged_attention(a, plan, kv->head_dim, T, static_cast<float*>(workspace), stream_of(stream)));
     return QTALE_OK;
 }
 

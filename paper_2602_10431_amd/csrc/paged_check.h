@@ -15,7 +15,7 @@ inline int check_paged(const qtale_paged_kv* kv, bool buffers) {
         return QTALE_ERR_INVALID_ARG;
     if (kv->head_dim != 64 && kv->head_dim != 128) return QTALE_ERR_UNSUPPORTED;
     if (kv->page_size < 16 || kv->page_size > 1024 || (kv->page_size & (kv->page_size - 1)) != 0) return QTALE_ERR_UNSUPPORTED;
-    if (kv->dtype != QTALE_ACT_FP16 && kv->dtype != QTALE_ACT_BF16) return QTALE_ERR_UNSUPPORTED;
+    if ((kv->dtype & ~QTALE_KV_INT4) != QTALE_ACT_FP16 && (kv->dtype & ~QTALE_KV_INT4) != QTALE_ACT_BF16) return QTALE_ERR_UNSUPPORTED;
     if (kv->n_layers > 65535) return QTALE_ERR_UNSUPPORTED;
     // places in a slot and slots of all layers are counted in 32 bits
     if (static_cast<int64_t>(kv->max_pages) * kv->page_size > (int64_t{1} << 30)) return QTALE_ERR_UNSUPPORTED;
@@ -37,7 +37,7 @@ inline PagedDev paged_device(const qtale_paged_kv* kv, int layer) {
     p.len = kv->kv_len ? kv->kv_len + skip : nullptr;
     p.cap = kv->kv_cap ? kv->kv_cap + skip : nullptr;
     p.n_pages = kv->n_pages; p.nkv = kv->n_kv_heads; p.d = kv->head_dim; p.n_layers = kv->n_layers; p.n_slots = kv->n_slots;
-    p.max_pages = kv->max_pages; p.bf16 = kv->dtype == QTALE_ACT_BF16;
+    p.max_pages = kv->max_pages; p.bf16 = (kv->dtype & ~QTALE_KV_INT4) == QTALE_ACT_BF16; p.q4 = (kv->dtype & QTALE_KV_INT4) != 0;
     while ((1 << p.shift) < kv->page_size) ++p.shift;
     return p;
 }
@@ -71,7 +71,7 @@ inline PagedAttnBounds attn_bounds(const qtale_paged_attn* a, const qtale_paged_
 inline PagedAttnDev attn_device(const qtale_paged_kv* kv, int layer, const qtale_paged_attn* attn, const PagedAttnBounds& m, int T) {
     const PagedDev p = paged_device(kv, layer);
     PagedAttnDev a{};
-    a.k = p.k; a.v = p.v; a.table = p.table; a.len = p.len;
+    a.k = p.k; a.v = p.v; a.table = p.table; a.len = p.len; a.bf16 = p.bf16; a.q4 = p.q4;
     a.nh = attn->n_heads; a.nkv = p.nkv; a.rep = attn->n_heads / p.nkv; a.shift = p.shift; a.max_pages = p.max_pages; a.n_slots = p.n_slots;
     a.n_pages = p.n_pages; a.sinks = attn->window > 0 ? attn->sinks : 0; a.max_len = m.max_len;
     // places begin at -T (rows before their slot's begin), so that place - window stays in 32 bits; windows beyond the cache are all the same

@@ -87,7 +87,9 @@ size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B) {
     return (256 + decode_bytes(nkv, d, B) + sums * part_stride(d) * 4 + 255) / 256 * 256;
 }
 
-hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int bf16, int T, float* workspace, hipStream_t stream) {
+hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int T, float* workspace, hipStream_t stream) {
+    if (a.q4) return launch_paged4_simple(a, d, T, stream);
+    const int bf16 = a.bf16;
     a.take = plan.decode && plan.chunk;
     a.items = plan.items; a.ranges = plan.ranges; a.target = plan.target;
     a.spans = plan.spans; a.stream_keys = plan.stream_keys; a.cols = plan.cols;

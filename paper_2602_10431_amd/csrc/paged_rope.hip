@@ -175,6 +175,7 @@ static void launch_rope_form(const PagedRopeArgs& a, dim3 grid, hipStream_t stre
 
 hipError_t launch_paged_rope(const PagedRopeArgs& a, hipStream_t stream) {
     if (a.T == 0) return hipSuccess;
+    if (a.kv.q4) return launch_paged4_rope(a, stream);
     // few tokens: a row's units go to several workgroups, about one unit per thread
     const int chunks = (a.nh + 2 * a.kv.nkv) * (a.kv.d >> 3);
     const int parts = a.T >= 512 ? 1 : std::min((chunks + 511) / 512, 16);

@@ -110,7 +110,8 @@ constexpr int kMoveUnit = 16384;                 // bytes that a workgroup moves
 
 __global__ void __launch_bounds__(256)
 pages_split_kernel(PagedDev p, SplitList list) {
-    split_pages(p, list, blockIdx.x, gridDim.x);
+    if (p.q4) split_pages4(p, list, blockIdx.x, gridDim.x);
+    else split_pages(p, list, blockIdx.x, gridDim.x);
 }
 
 // Whole pages, keys and values; workgroups past `movers` rewrite the page table instead (remap of the pages from n_live on).
@@ -166,7 +167,7 @@ hipError_t launch_pages_copy(const PagedDev& from, const PagedDev& to, const int
     MoveArgs a{};
     a.k0 = from.k; a.v0 = from.v; a.k1 = to.k; a.v1 = to.v;
     a.n = n; a.n_from = from.n_pages; a.n_to = to.n_pages; a.src = src; a.dst = dst;
-    a.page_bytes = (static_cast<size_t>(from.nkv) * from.d * 2) << from.shift;
+    a.page_bytes = from.nkv * head_bytes(from);
     const size_t units = static_cast<size_t>(n) * 2 * ((a.page_bytes + kMoveUnit - 1) / kMoveUnit);
     a.movers = static_cast<int>(std::min<size_t>(units, kMovers));
     hipLaunchKernelGGL(pages_move_kernel, dim3(a.movers), dim3(256), 0, stream, a);
@@ -433,7 +434,7 @@ hipError_t launch_pages_compact(const PagedDev& p, int32_t* n_live, void* worksp
     MoveArgs a{};
     a.k0 = a.k1 = p.k; a.v0 = a.v1 = p.v;
     a.n_list = n_moves; a.n_from = a.n_to = p.n_pages; a.src = src; a.dst = dst;
-    a.page_bytes = (static_cast<size_t>(p.nkv) * p.d * 2) << p.shift;
+    a.page_bytes = p.nkv * head_bytes(p);
     a.movers = kMovers;
     a.table = p.table; a.entries = static_cast<size_t>(p.n_layers) * p.n_slots * p.max_pages; a.remap = remap; a.n_live = n_moves + 1;
     const int writers = static_cast<int>(std::min<size_t>((a.entries + 1023) / 1024, 256));

@@ -247,7 +247,7 @@ int paged_attention_block(qtale_ctx* ctx, const qtale_layer_cfg* c, const PagedC
     PagedAttnDev a = attn_device(pc.kv, pc.layer, pc.attn, m, M_max);
     a.q = qkv; a.q_stride = width; a.out = reinterpret_cast<uint16_t*>(ws.attn); a.out_stride = nh * d;
     a.offs = ws.cu_exec; a.slots = pc.slots; a.first = ws.kv_old; a.B = B;
-    HIP_TRY(launch_paged_attention(a, plan, d, 0, M_max, pc.attn_ws, stream));
+    HIP_TRY(launch_paged_attention(a, plan, d, M_max, pc.attn_ws, stream));
     return QTALE_OK;
 }
 
@@ -706,7 +706,7 @@ int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const 
     if ((e = check_paged(kv, true)) || (e = check_rope(rope, cfg->head_dim)) || (e = check_paged_attn(attn, kv))) return e;
     if (n_layers < 0 || first_layer < 0 || (n_layers > 0 && !layers)) return QTALE_ERR_INVALID_ARG;
     if (static_cast<int64_t>(first_layer) + n_layers > kv->n_layers) return QTALE_ERR_SHAPE;
-    if (kv->dtype != QTALE_ACT_FP16) return QTALE_ERR_UNSUPPORTED;   // q, k and v of a layer are fp16
+    if ((kv->dtype & ~QTALE_KV_INT4) != QTALE_ACT_FP16) return QTALE_ERR_UNSUPPORTED;   // q, k and v of a layer are fp16
     if (kv->n_kv_heads != cfg->n_kv_heads || kv->head_dim != cfg->head_dim || attn->n_heads != cfg->n_heads) return QTALE_ERR_SHAPE;
     if (B > kReserveItems) return QTALE_ERR_UNSUPPORTED;
     if (!slots && B > kv->n_slots) return QTALE_ERR_SHAPE;

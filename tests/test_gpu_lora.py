@@ -1,0 +1,218 @@
+"""Low-rank adapters beside a shared projection on the GPU (run with -m gpu) against 64 bits: adapters in any order, ranks from 0 to 128, rows without one,
+odd sizes, one row to many, values of all sizes, what lies past an adapter's rank, streams and graphs."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def qt():
+    import paper_2602_10431_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def _base(qt, N, K, bits, group, seed):
+    """(QuantLinear, its weights in float64)"""
+    w = torch.randn(N, K, generator=torch.Generator().manual_seed(seed)) / K ** 0.5
+    q = qt.qtale_quantize(w.cuda(), bits, group)
+    words = q.codes.cpu().long() & 0xffffffff
+    stream = (words[..., None] >> torch.arange(32) & 1).reshape(N, -1)[:, : K * bits].reshape(N, K, bits)
+    codes = (stream << torch.arange(bits)).sum(2).double()
+    at = torch.arange(K) // group
+    return q, ((codes - q.zeros.cpu().double()[:, at]) * q.scales.cpu().double()[:, at]).cuda()
+
+
+def _adapters(qt, n, r, N, K, seed, ranks=None, scales=True, fill=None):
+    g = torch.Generator().manual_seed(seed)
+    down, up = (torch.randn(n, r, K, generator=g) / K ** 0.5).half().cuda(), (torch.randn(n, N, r, generator=g) / r ** 0.5).half().cuda()
+    rank = None if ranks is None else torch.tensor(ranks, dtype=torch.int32).cuda()
+    if fill is not None:
+        for a, x in enumerate(ranks):
+            down[a, x:], up[a, :, x:] = fill, fill
+    scale = (0.25 + 2 * torch.rand(n, generator=g)).cuda() if scales else None
+    return qt.Lora(down, up, rank, scale), down, up
+
+
+# Errors: the shared product in 32 bits and rounded to fp16, 2^-11 of it; the inner values in 32 bits (K products, their magnitudes' sum times 2^-24 (K
+# / 64 + 8), as 64 or more lanes add side by side) and as operands 2^-11 of each; the sum of up to 128 products 2^-24 * 130 of its magnitudes; the sum once
+# more to fp16, 2^-11 of it.  Weights of the shared product go into the matrix cores as fp16 (code - zero) * scale, 2^-11 each, its sums of K in 32 bits.
+def _expect(base, lora, down, up, x, ids):
+    """(y, bound) in float64"""
+    U = 2.0 ** -11
+    xd, n = x.double(), down.shape[0]
+    y = xd @ base.t()
+    size = xd.abs() @ base.abs().t()
+    K = x.shape[1]
+    bound = U * y.abs() + (U + 2.0 ** -24 * (K / 64 + 8)) * size
+    for a in range(n):
+        rows = (ids == a).nonzero()[:, 0]
+        if rows.numel() == 0:
+            continue
+        r = down.shape[1] if lora.rank is None else int(lora.rank[a])
+        s = 1.0 if lora.scale is None else float(lora.scale[a])
+        dn, u = down[a, :r].double(), up[a, :, :r].double()
+        inner, big = xd[rows] @ dn.t(), xd[rows].abs() @ dn.abs().t()
+        y[rows] += s * inner @ u.t()
+        bound[rows] += s * ((U + 2.0 ** -24 * 132) * inner.abs() + 2.0 ** -24 * (K / 64 + 8) * big) @ u.abs().t()
+        # (as fp16 of their row's power of two, inner values far below the row's largest keep 2^-25 of it)
+        bound[rows] += s * 2.0 ** -24 * (inner.abs().amax(1, keepdim=True) if r else 0.0) * u.abs().sum(1)
+    return y, bound + U * y.abs() + 2.0 ** -24
+
+
+def _ids(pattern, M, n, seed):
+    g = torch.Generator().manual_seed(seed)
+    if pattern == "mixed":
+        return torch.randint(-1, n, (M,), generator=g).int().cuda()
+    if pattern == "runs":                                         # requests of several rows; a number out of range is none
+        ids = torch.randint(-1, n + 1, (M // 7 + 1,), generator=g).repeat_interleave(7)[:M]
+        return ids.int().cuda()
+    return torch.full((M,), {"one": n - 1, "none": -1}[pattern], dtype=torch.int32).cuda()
+
+
+SIZES = [(64, 64, 32), (8, 512, 64), (264, 136, 64), (1376, 512, 128), (520, 1384, 128), (4096, 1024, 128)]
+
+
+@pytest.mark.parametrize("N,K,group", SIZES)
+@pytest.mark.parametrize("M", [1, 2, 5, 16, 17, 33, 64, 130, 300])
+def test_linear(qt, N, K, group, M):
+    q, base = _base(qt, N, K, 4, group, N + K)
+    for pattern, n, r in (("mixed", 7, 16), ("runs", 3, 40), ("one", 2, 8), ("none", 2, 8)):
+        ranks = [(r * (a + 1)) // n for a in range(n)]
+        lora, down, up = _adapters(qt, n, r, N, K, M, ranks, pattern != "one")
+        x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).half().cuda()
+        ids = _ids(pattern, M, n, M + n)
+        y, bound = _expect(base, lora, down, up, x, ids)
+        out = torch.full((M + 1, N), 7.0, dtype=torch.float16, device="cuda")
+        got = qt.qtale_linear_lora_w4a16(q, lora, x, ids, out=out[:M])
+        assert bool(((got.double() - y).abs() <= bound).all()) and bool((out[M:] == 7.0).all())
+        if pattern == "none":
+            assert torch.equal(got, qt.qtale_linear_w4a16(q, x))
+
+
+@pytest.mark.parametrize("r", [1, 2, 7, 8, 15, 16, 17, 24, 32, 33, 61, 64, 100, 128])
+def test_ranks(qt, r):
+    N, K = 328, 200
+    q, base = _base(qt, N, K, 4, 64, r)
+    for M in (3, 70):
+        ranks = [0, r, max(r // 2, 1), min(r, 9)]
+        lora, down, up = _adapters(qt, 4, r, N, K, r, ranks, fill=float("nan"))                       # what lies past a rank is not used
+        x = torch.randn(M, K, generator=torch.Generator().manual_seed(r)).half().cuda()
+        ids = _ids("mixed", M, 4, r)
+        y, bound = _expect(base, lora, down, up, x, ids)
+        got = qt.qtale_linear_lora_w4a16(q, lora, x, ids)
+        assert bool(((got.double() - y).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4])
+@pytest.mark.parametrize("M", [1, 6, 40, 200, 513])
+def test_gated(qt, bits, M):
+    N, K = 712, 512
+    pairs = [_base(qt, N, K, bits, 128, s) for s in (1, 2)]
+    lg, dg, ug = _adapters(qt, 5, 16, N, K, 3)
+    lu, du, uu = _adapters(qt, 9, 24, N, K, 4)                    # another pool, more adapters, another rank
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).half().cuda()
+    ids = _ids("mixed", M, 9, M)
+    (g, bg), (u, bu) = _expect(pairs[0][1], lg, dg, ug, x, ids), _expect(pairs[1][1], lu, du, uu, x, ids)
+    only = torch.full_like(ids, -1)
+    for a, b in ((lg, lu), (lg, None), (None, lu)):
+        if a is None:
+            g, bg = _expect(pairs[0][1], lg, dg, ug, x, only)
+        if b is None:
+            (u1, bu1) = _expect(pairs[1][1], lu, du, uu, x, only)
+        else:
+            u1, bu1 = u, bu
+        got = qt.qtale_swiglu_lora_w4a16(pairs[0][0], pairs[1][0], a, b, x, ids)
+        s = torch.sigmoid(g)
+        # silu's slope is at most 1.1; the product's rounding, and silu in 32 bits
+        bound = 1.1 * bg * (u1.abs() + bu1) + (g * s).abs() * bu1 + (2.0 ** -11 + 2.0 ** -20) * (g * s * u1).abs() + 2.0 ** -24
+        assert bool(((got.double() - g * s * u1).abs() <= bound).all()), (a is None, b is None)
+
+
+def test_many_rows_of_few_adapters(qt):
+    N, K, M = 1032, 2048, 3000
+    q, base = _base(qt, N, K, 4, 128, 9)
+    lora, down, up = _adapters(qt, 3, 32, N, K, 9, [32, 5, 20])
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(1)).half().cuda()
+    ids = torch.tensor([0] * 1000 + [1] * 3 + [-1] * 497 + [2] * 1500, dtype=torch.int32).cuda()
+    y, bound = _expect(base, lora, down, up, x, ids)
+    assert bool(((qt.qtale_linear_lora_w4a16(q, lora, x, ids).double() - y).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("M", [2, 90])
+@pytest.mark.parametrize("size,back", [(2.0 ** 12, 2.0 ** -12), (2.0 ** -13, 2.0 ** 10)])
+def test_inner_values_of_all_sizes(qt, M, size, back):
+    # inner values past fp16's end, or far below one: they are operands relative to their row's largest
+    N, K = 256, 512
+    q, base = _base(qt, N, K, 4, 128, 2)
+    lora, down, up = _adapters(qt, 3, 16, N, K, 5)
+    down.mul_(size)
+    lora.scale.mul_(back)
+    x = (64 * torch.randn(M, K, generator=torch.Generator().manual_seed(3))).half().cuda()
+    ids = _ids("mixed", M, 3, 4)
+    y, bound = _expect(base, lora, down, up, x, ids)
+    assert bool(((qt.qtale_linear_lora_w4a16(q, lora, x, ids).double() - y).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("M", [5, 64, 300])
+def test_a_row_that_is_not_finite_stays_alone(qt, M):
+    N, K = 256, 512
+    q, base = _base(qt, N, K, 4, 128, 2)
+    lora, down, up = _adapters(qt, 3, 16, N, K, 5)
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(3)).half().cuda()
+    ids = _ids("mixed", M, 3, 4)
+    ids[1] = ids[2] = ids[3] = 1
+    want = qt.qtale_linear_lora_w4a16(q, lora, x, ids)
+    x[2, 77] = float("nan")
+    got = qt.qtale_linear_lora_w4a16(q, lora, x, ids)
+    assert bool(got[2].isnan().all())
+    keep = torch.arange(M, device="cuda") != 2
+    assert torch.equal(got[keep], want[keep])
+    # an adapter with a NaN reaches its own rows alone
+    x[2, 77] = 0.0
+    lora.down[1, 3, 9] = float("nan")
+    got, want = qt.qtale_linear_lora_w4a16(q, lora, x, ids), qt.qtale_linear_lora_w4a16(q, lora, x, torch.where(ids == 1, -1, ids))
+    assert bool(got[ids == 1].isnan().all()) and torch.equal(got[ids != 1], want[ids != 1])
+
+
+@pytest.mark.parametrize("M", [3, 64, 500])
+def test_repeats_streams_and_graphs(qt, M):
+    N, K = 1024, 1024
+    (g, _), (u, _) = _base(qt, N, K, 4, 128, 1), _base(qt, N, K, 4, 128, 2)
+    lora, _, _ = _adapters(qt, 8, 16, N, K, 5)
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(3)).half().cuda()
+    ids = _ids("mixed", M, 8, 4)
+    ws = qt.alloc_lora_workspace([lora, lora], M)
+    out1, out2 = torch.empty(M, N, dtype=torch.float16, device="cuda"), torch.empty(M, N, dtype=torch.float16, device="cuda")
+
+    def call():
+        qt.qtale_linear_lora_w4a16(g, lora, x, ids, out=out1, workspace=ws)
+        qt.qtale_swiglu_lora_w4a16(g, u, lora, lora, x, ids, out=out2, workspace=ws)
+
+    call()
+    want = out1.clone(), out2.clone()
+    for _ in range(10):
+        ws.fill_(255)
+        call()
+        assert torch.equal(out1, want[0]) and torch.equal(out2, want[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out1, want[0]) and torch.equal(out2, want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        out1.zero_(), out2.zero_(), ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out1, want[0]) and torch.equal(out2, want[1])
+    x.mul_(0.5)                                                   # other inputs, other adapters, in place
+    ids.copy_(_ids("mixed", M, 8, 5))
+    graph.replay()
+    replayed = out1.clone(), out2.clone()
+    call()
+    assert torch.equal(out1, replayed[0]) and torch.equal(out2, replayed[1])
