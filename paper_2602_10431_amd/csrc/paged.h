@@ -114,6 +114,8 @@ size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B);   // of work
 hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int T, float* workspace, hipStream_t stream);
 hipError_t launch_paged4_simple(const PagedAttnDev& a, int d, int T, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);
+hipError_t launch_paged_pieces(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);   // adds the spans' sums
+hipError_t launch_paged4_decode(const PagedAttnDev& a, int d, hipStream_t stream);
 hipError_t launch_paged_chunk(const PagedAttnDev& a, int groups, int d, int bf16, hipStream_t stream);
 hipError_t launch_chunk_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream);
 

@@ -338,13 +338,26 @@ paged_pieces_kernel(PagedAttnDev p) {
     sum.put<BF16>(p.out + (row0 + i) * p.out_stride + h * D, lane);
 }
 
+// (a.cols <= 16)
+hipError_t launch_paged_pieces(const PagedAttnDev& a, int d, int bf16, hipStream_t stream) {
+    const dim3 grid(a.nkv, a.B, a.cols), block(256);
+    if (d == 128) {
+        if (bf16) hipLaunchKernelGGL((paged_pieces_kernel<128, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((paged_pieces_kernel<128, false>), grid, block, 0, stream, a);
+    } else {
+        if (bf16) hipLaunchKernelGGL((paged_pieces_kernel<64, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((paged_pieces_kernel<64, false>), grid, block, 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
 template <int D, bool BF16>
 static hipError_t decode_form(const PagedAttnDev& a, hipStream_t stream) {
     // a sequence's columns next to each other: the workgroups that share its keys run together
     const dim3 grid(a.nkv, (a.cols + kDecodeCols - 1) / kDecodeCols, a.B);
     if (a.spans > 0) {
         hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true, true>), dim3(a.nkv, a.spans), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL((paged_pieces_kernel<D, BF16>), dim3(a.nkv, a.B, a.cols), dim3(256), 0, stream, a);   // (a.cols <= 16)
+        return launch_paged_pieces(a, D, BF16, stream);
     } else if (D == 128 && a.stream_keys) {
         hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false, D == 128>), grid, dim3(256), 0, stream, a);
     } else {

@@ -88,7 +88,6 @@ size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B) {
 }
 
 hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int T, float* workspace, hipStream_t stream) {
-    if (a.q4) return launch_paged4_simple(a, d, T, stream);
     const int bf16 = a.bf16;
     a.take = plan.decode && plan.chunk;
     a.items = plan.items; a.ranges = plan.ranges; a.target = plan.target;
@@ -98,6 +97,10 @@ hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int
     a.span_part = reinterpret_cast<float*>(at + (static_cast<size_t>(std::min(a.B, kSpanSeqs)) * sizeof(int4) + 255) / 256 * 256);
     a.part = reinterpret_cast<float*>(at + plan.decode_bytes);
     hipError_t e = hipSuccess;
+    if (a.q4) {
+        if (plan.chunk) return launch_paged4_simple(a, d, T, stream);
+        return launch_paged4_decode(a, d, stream);
+    }
     if (plan.decode && (e = launch_paged_decode(a, d, bf16, stream)) != hipSuccess) return e;
     if (plan.chunk && (e = launch_paged_chunk(a, plan.groups, d, bf16, stream)) != hipSuccess) return e;
     return plan.ranges > 1 ? launch_chunk_combine(a, d, bf16, T, stream) : e;
