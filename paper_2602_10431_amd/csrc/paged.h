@@ -112,10 +112,10 @@ PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max
 size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B);   // of workspace, for any call of at most T tokens and B sequences
 // All launches of a call; a: everything but `take` and what follows it, which the plan says.
 hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int T, float* workspace, hipStream_t stream);
-hipError_t launch_paged4_simple(const PagedAttnDev& a, int d, int T, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);
 hipError_t launch_paged_pieces(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);   // adds the spans' sums
 hipError_t launch_paged4_decode(const PagedAttnDev& a, int d, hipStream_t stream);
+hipError_t launch_paged4_chunk(const PagedAttnDev& a, int groups, int d, hipStream_t stream);
 hipError_t launch_paged_chunk(const PagedAttnDev& a, int groups, int d, int bf16, hipStream_t stream);
 hipError_t launch_chunk_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream);
 

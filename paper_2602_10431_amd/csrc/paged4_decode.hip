@@ -214,7 +214,7 @@ again:                                                           // the pieces o
             const float p0 = __builtin_amdgcn_exp2f(sc[e] - m_run), p1 = __builtin_amdgcn_exp2f(sc[e + 1] - m_run);
             l_run += p0 + p1;
             ph[e >> 1] = Act16<false>::pack(p0 * (t[e] * t_inv), p1 * (t[e + 1] * t_inv));
-            zv[e >> 1] = __builtin_amdgcn_perm(vp[e >> 2][(e & 3) + 1], vp[e >> 2][e & 3], 0x07060302u);
+            zv[e >> 1] = __builtin_amdgcn_perm(vp[e >> 2][(e & 3) + 1], vp[e >> 2][e & 3], 0x07060302u) & 0x000f000fu;   // (in unused places it may be anything)
         }
         o[F] = Act16<false>::mfma16(zv, ph, o[F]);
         // words 2 h, 2 h + 1 of a lane: columns F c + 4 h .. + 3 of its keys 4 g + {0, 1} and {2, 3}

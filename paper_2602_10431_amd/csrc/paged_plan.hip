@@ -98,8 +98,10 @@ hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int
     a.part = reinterpret_cast<float*>(at + plan.decode_bytes);
     hipError_t e = hipSuccess;
     if (a.q4) {
-        if (plan.chunk) return launch_paged4_simple(a, d, T, stream);
-        return launch_paged4_decode(a, d, stream);
+        if (plan.decode && (e = launch_paged4_decode(a, d, stream)) != hipSuccess) return e;
+        if (plan.chunk && (e = launch_paged4_chunk(a, plan.groups, d, stream)) != hipSuccess) return e;
+        a.scale_log2 = 1.0f;                                     // (reference points of these kernels are scaled scores)
+        return plan.ranges > 1 ? launch_chunk_combine(a, d, bf16, T, stream) : e;
     }
     if (plan.decode && (e = launch_paged_decode(a, d, bf16, stream)) != hipSuccess) return e;
     if (plan.chunk && (e = launch_paged_chunk(a, plan.groups, d, bf16, stream)) != hipSuccess) return e;

@@ -63,7 +63,8 @@ def shadow(kv, k, v):
 
 
 def random_cache4(qt, lens, page, nkv, d, dtype, seed, spare=3, n_layers=1, layer=0, gone=(), extra_slots=2, max_extra=1, std=1.0):
-    """(cache, slots, shadow): slots of `layer` hold `lens` random tokens on shuffled pages; every other place has a NaN scale and codes of 15."""
+    """(cache, slots, shadow): slots of `layer` hold `lens` random tokens on shuffled pages; every other place has a NaN for its scale and
+    zero point, and codes of 15."""
     g = torch.Generator().manual_seed(seed)
     held = [-(-n // page) for n in lens]
     n_pages, n_slots = sum(held) + spare, len(lens) + extra_slots
@@ -87,7 +88,7 @@ def random_cache4(qt, lens, page, nkv, d, dtype, seed, spare=3, n_layers=1, laye
         hole = ~used[:, None].expand(n_pages, nkv, page)
         codes = torch.where(hole[..., None], torch.full_like(codes, 15), codes)
         scale = torch.where(hole, torch.full_like(scale, float("nan")), scale)
-        (kv.k if keys else kv.v).copy_(pack(codes, scale, zero, keys))
+        (kv.k if keys else kv.v).copy_(pack(codes, scale, torch.where(hole, torch.full_like(zero, 0x7e01), zero), keys))
         dense.append(values64(codes, scale, zero))
     free = [int(r == 0) for r in refs.tolist()] + [0] * (-n_pages % 32)
     words = [sum(bit << i for i, bit in enumerate(free[w: w + 32])) for w in range(0, len(free), 32)]
