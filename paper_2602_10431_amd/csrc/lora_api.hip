@@ -27,12 +27,13 @@ int check_lora_call(const int32_t* adapter, const void* A, const void* out, cons
     return have < need ? QTALE_ERR_WORKSPACE_TOO_SMALL : QTALE_OK;
 }
 
-// The shared product alone.
-hipError_t base_linear(const qtale_qlinear* w, int bits, int group, const void* A, int M, void* out, hipStream_t stream) {
+// The shared product alone, of one linear or of two side by side ([M][2 N]).
+hipError_t base_linear(const qtale_qlinear* w, const qtale_qlinear* w2, int bits, int group, const void* A, int M, void* out, hipStream_t stream) {
     GemmArgs g{};
-    g.A = A; g.M_max = M; g.rows_exact = 1; g.K = w->K; g.group = group; g.bits = bits; g.n_w = 1;
+    g.A = A; g.M_max = M; g.rows_exact = 1; g.K = w->K; g.group = group; g.bits = bits; g.n_w = w2 ? 2 : 1;
     g.w[0] = {w->prepacked, w->N, w->K};
-    g.epilogue = EPI_STORE_F16; g.out = out; g.ldo = w->N;
+    if (w2) g.w[1] = {w2->prepacked, w2->N, w2->K};
+    g.epilogue = EPI_STORE_F16; g.out = out; g.ldo = w->N * g.n_w;
     return launch_gemm_w4a16(g, stream);
 }
 
@@ -60,9 +61,10 @@ int qtale_linear_lora_w4a16(const qtale_qlinear* w, int bits, int group, const q
     const LoraDev l = lora_device(lora);
     const LoraRows rows{adapter, nullptr, nullptr, M, 0};
     float* inner = static_cast<float*>(workspace);
-    HIP_TRY(launch_lora_inner(l, rows, A, inner, s));
-    HIP_TRY(base_linear(w, bits, group, A, M, out, s));
-    HIP_TRY(launch_lora_add(l, rows, inner, out, w->N, 0, s));
+    int parts = 0;
+    HIP_TRY(launch_lora_inner(&l, 1, rows, A, &inner, &parts, s));
+    HIP_TRY(base_linear(w, nullptr, bits, group, A, M, out, s));
+    HIP_TRY(launch_lora_add(l, rows, inner, parts, out, w->N, 0, s));
     return QTALE_OK;
 }
 
@@ -87,13 +89,15 @@ int qtale_swiglu_lora_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, 
     char* at = static_cast<char*>(workspace);
     float* inner_g = reinterpret_cast<float*>(at);
     float* inner_u = reinterpret_cast<float*>(at += inner_bytes(lora_gate, M));
-    void* g = at += inner_bytes(lora_up, M);
-    void* u = at += rows_bytes(M, gate->N);
-    if (lg.n) HIP_TRY(launch_lora_inner(lg, rows, A, inner_g, s));
-    if (lu.n) HIP_TRY(launch_lora_inner(lu, rows, A, inner_u, s));
-    HIP_TRY(base_linear(gate, bits, group, A, M, g, s));
-    HIP_TRY(base_linear(up, bits, group, A, M, u, s));
-    HIP_TRY(launch_lora_swiglu(lg, lu, rows, inner_g, inner_u, g, u, out, gate->N, s));
+    void* base = at += inner_bytes(lora_up, M);
+    LoraDev l[2];
+    float* inner[2];
+    int parts[2] = {0, 0}, n = 0;
+    if (lg.n) { l[n] = lg; inner[n++] = inner_g; }
+    if (lu.n) { l[n] = lu; inner[n++] = inner_u; }
+    HIP_TRY(launch_lora_inner(l, n, rows, A, inner, parts, s));
+    HIP_TRY(base_linear(gate, up, bits, group, A, M, base, s));
+    HIP_TRY(launch_lora_swiglu(lg, lu, rows, inner_g, inner_u, parts[0], parts[n - 1], base, out, gate->N, s));
     return QTALE_OK;
 }
 
