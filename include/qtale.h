@@ -429,6 +429,17 @@ int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const 
                               int32_t* missing /*nullable*/, int32_t* sel_idx /*nullable*/, int32_t* sel_count /*nullable*/,
                               float* scores /*nullable*/, void* workspace, size_t workspace_bytes, void* stream);
 
+/* qtale_paged_stack_forward with adapters: loras host [n_layers], whose linears without an adapter have n_adapters = 0 (the rest is then not read);
+ * adapter [B] int32 device: that of each sequence of the call, one number for all linears and layers (outside a linear's adapters: none).
+ * workspace >= qtale_paged_stack_lora_workspace_bytes(cfg, kv, max_rank, T, B) with the largest max_rank. */
+typedef struct { qtale_lora q, k, v, o, gate, up, down; } qtale_layer_lora;
+size_t qtale_paged_stack_lora_workspace_bytes(const qtale_layer_cfg* cfg, const qtale_paged_kv* kv, int max_rank, int max_tokens, int max_seqs);
+int qtale_paged_stack_lora_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, const qtale_layer_lora* loras,
+                                   int n_layers, int first_layer, void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions,
+                                   const qtale_paged_kv* kv, const int32_t* slots /*nullable*/, const int32_t* adapter, const qtale_rope* rope,
+                                   const qtale_paged_attn* attn, int32_t* missing /*nullable*/, int32_t* sel_idx /*nullable*/,
+                                   int32_t* sel_count /*nullable*/, float* scores /*nullable*/, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing with HIP events recorded on the forward call's stream.  While enabled, every
  * layer/stack forward brackets its kernels with events; qtale_profile_read waits for them and
  * returns, per kernel class, accumulated milliseconds and launch counts since the last read.
@@ -437,6 +448,7 @@ int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const 
  * does it: up to 256 tokens class 2 is part of 1; with a cache and few new tokens per sequence (decode) class 4 is part
  * of 5, so that a bandwidth made from class 5 includes the rotation and the append (otherwise 4 also builds the work list of 5;
  * on a paged cache it is always 4, with the pages' room);
+ * adapters are counted in the class of their linear;
  * with at most four tokens 0 (unless the
  * router is an MLP), 1 and 2 are part of 3, and 7 is part of 8.  Inside a stack a decode-sized layer's class 9 also scores the
  * next layer's tokens (its class 0).  Profiling adds event overhead; leave it off when timing whole steps. */

@@ -30,7 +30,8 @@ EXPORTS = ["qtale_strerror", "qtale_create", "qtale_destroy", "qtale_set_exec_ra
            "qtale_pages_init", "qtale_pages_workspace_bytes", "qtale_pages_fork", "qtale_pages_reserve", "qtale_pages_release",
            "qtale_pages_trim", "qtale_pages_compact", "qtale_pages_copy", "qtale_rope_frequencies", "qtale_paged_rope_append",
            "qtale_paged_attention_workspace_bytes", "qtale_paged_attention", "qtale_paged_stack_workspace_bytes",
-           "qtale_paged_stack_forward", "qtale_paged_read", "qtale_lora_workspace_bytes", "qtale_linear_lora_w4a16", "qtale_swiglu_lora_w4a16"]
+           "qtale_paged_stack_forward", "qtale_paged_read", "qtale_lora_workspace_bytes", "qtale_linear_lora_w4a16", "qtale_swiglu_lora_w4a16",
+           "qtale_paged_stack_lora_workspace_bytes", "qtale_paged_stack_lora_forward"]
 QTALE_THETA_GRID = 50
 QTALE_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 QTALE_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "parts": 4}
@@ -75,6 +76,10 @@ class qtale_paged_kv(C.Structure):
 class qtale_lora(C.Structure):
     _fields_ = [("down", C.c_void_p), ("up", C.c_void_p), ("rank", C.c_void_p), ("scale", C.c_void_p), ("n_adapters", C.c_int),
                 ("max_rank", C.c_int), ("N", C.c_int), ("K", C.c_int)]
+
+
+class qtale_layer_lora(C.Structure):
+    _fields_ = [(n, qtale_lora) for n in ("q", "k", "v", "o", "gate", "up", "down")]
 
 
 class qtale_rope(C.Structure):
@@ -161,8 +166,12 @@ def load_library():
     lib.qtale_lora_workspace_bytes.restype = sz
     lib.qtale_linear_lora_w4a16.argtypes = [ql, i, i, lo, vp, vp, i, vp, vp, sz, vp]
     lib.qtale_swiglu_lora_w4a16.argtypes = [ql, ql, i, i, lo, lo, vp, vp, i, vp, vp, sz, vp]
+    lib.qtale_paged_stack_lora_workspace_bytes.argtypes = [C.POINTER(qtale_layer_cfg), pk, i, i, i]
+    lib.qtale_paged_stack_lora_workspace_bytes.restype = sz
+    lib.qtale_paged_stack_lora_forward.argtypes = [vp, C.POINTER(qtale_layer_cfg), C.POINTER(qtale_layer_weights), C.POINTER(qtale_layer_lora), i, i, vp,
+                                                   i, vp, i, vp, pk, vp, vp, C.POINTER(qtale_rope), C.POINTER(qtale_paged_attn), vp, vp, vp, vp, vp, sz, vp]
     for name in EXPORTS:
-        if name not in ("qtale_lora_workspace_bytes", "qtale_strerror", "qtale_prepacked_bytes", "qtale_workspace_bytes",
+        if name not in ("qtale_paged_stack_lora_workspace_bytes", "qtale_lora_workspace_bytes", "qtale_strerror", "qtale_prepacked_bytes", "qtale_workspace_bytes",
                         "qtale_calibration_scratch_bytes", "qtale_graph_destroy", "qtale_static_scratch_bytes",
                         "qtale_pages_workspace_bytes", "qtale_paged_attention_workspace_bytes",
                         "qtale_paged_stack_workspace_bytes"):
@@ -783,26 +792,50 @@ def qtale_paged_attention(kv, layer, q, seq_offsets, first=None, slots=None, out
     return out
 
 
-def alloc_paged_stack_workspace(cfg, kv, max_tokens, max_seqs):
-    n = load_library().qtale_paged_stack_workspace_bytes(C.byref(cfg), kv._ref, max_tokens, max_seqs)
+class StackLora:
+    """Adapters of a stack's linears: one dict per layer from any of "q", "k", "v", "o", "gate", "up", "down" to a Lora.  A sequence's number chooses its
+    adapter in all of them."""
+
+    def __init__(self, layers):
+        names = [n for n, _ in qtale_layer_lora._fields_]
+        for l in layers:
+            assert set(l) <= set(names), sorted(l)
+        self.layers, self.n = layers, len(layers)
+        self.max_rank = max([x.max_rank for l in layers for x in l.values()] + [0])
+        none = qtale_lora(None, None, None, None, 0, 0, 0, 0)
+        self._c = (qtale_layer_lora * self.n)(*[qtale_layer_lora(*[l[n].c_struct() if n in l else none for n in names]) for l in layers])
+
+
+def alloc_paged_stack_workspace(cfg, kv, max_tokens, max_seqs, loras=None):
+    """loras: the StackLora of the calls, if they have one."""
+    if loras is None:
+        n = load_library().qtale_paged_stack_workspace_bytes(C.byref(cfg), kv._ref, max_tokens, max_seqs)
+    else:
+        n = load_library().qtale_paged_stack_lora_workspace_bytes(C.byref(cfg), kv._ref, loras.max_rank, max_tokens, max_seqs)
     if n == 0:
         raise QtaleError(-1, "qtale_paged_stack_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=kv.device)
 
 
 def qtale_paged_stack_forward(ctx, stack, x, seq_offsets, positions, kv, rope, slots=None, window=0, sinks=0, scale=None, max_new=0, max_len=0,
-                              first_layer=0, missing=None, sel_idx=None, sel_count=None, scores=None, workspace=None):
-    """qtale_stack_forward on a paged cache (layer l of the stack is the cache's layer first_layer + l); the stack has no caches of its own."""
+                              first_layer=0, missing=None, sel_idx=None, sel_count=None, scores=None, workspace=None, loras=None, adapter=None):
+    """qtale_stack_forward on a paged cache (layer l of the stack is the cache's layer first_layer + l); the stack has no caches of its own.
+    loras (a StackLora) with adapter (int32 [B], the number of each sequence's adapter): qtale_paged_stack_lora_forward."""
     T = x.shape[0]
     B = seq_offsets.numel() - 1
     assert stack.kvs is None and rope.freqs.device == kv.device and x.device == kv.device and x.is_contiguous()
+    assert (loras is None) == (adapter is None) and (loras is None or loras.n == stack.n)
     if workspace is None:
-        workspace = alloc_paged_stack_workspace(stack.cfg, kv, T, B)
+        workspace = alloc_paged_stack_workspace(stack.cfg, kv, T, B, loras)
     attn = _paged_attn(kv, stack.cfg.n_heads, max_new, max_len, window, sinks, scale)
-    _check(load_library().qtale_paged_stack_forward(
-        ctx._h, C.byref(stack.cfg), stack._w, stack.n, first_layer, x.data_ptr(), T, _ints(seq_offsets, kv, B + 1), B, _ints(positions, kv, T),
-        kv._ref, _ints(slots, kv, B), rope._ref, C.byref(attn), _ints(missing, kv, stack.n), _ptr(sel_idx), _ptr(sel_count), _ptr(scores),
-        *_scratch(workspace, kv), _stream_of(kv)), "qtale_paged_stack_forward")
+    lib = load_library()
+    before = (ctx._h, C.byref(stack.cfg), stack._w)
+    tokens = (stack.n, first_layer, x.data_ptr(), T, _ints(seq_offsets, kv, B + 1), B, _ints(positions, kv, T), kv._ref, _ints(slots, kv, B))
+    after = (rope._ref, C.byref(attn), _ints(missing, kv, stack.n), _ptr(sel_idx), _ptr(sel_count), _ptr(scores), *_scratch(workspace, kv), _stream_of(kv))
+    if loras is None:
+        _check(lib.qtale_paged_stack_forward(*before, *tokens, *after), "qtale_paged_stack_forward")
+    else:
+        _check(lib.qtale_paged_stack_lora_forward(*before, loras._c, *tokens, _ints(adapter, kv, B), *after), "qtale_paged_stack_lora_forward")
 
 
 def qtale_profile_enable(ctx, on):

@@ -23,7 +23,7 @@ struct LoraRows {
 constexpr int kLoraMost = 3;     // linears with the same input that one launch takes
 
 int lora_splits(int M);                          // parts that the sums over K may be cut into
-size_t lora_inner_bytes(int R, int M);           // of one linear's inner values: [parts][M][R] fp32
+size_t lora_inner_bytes(int R, int M);           // of one linear's inner values, [parts][rows][R] fp32, for up to M rows
 
 // inner = down_a A_i of every row, in parts over K, for `n` linears of one input [M][K]; what belongs to no adapter, or lies past a rank, is not written.
 // *parts (host out): of each linear

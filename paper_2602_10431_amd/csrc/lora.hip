@@ -269,7 +269,11 @@ lora_outer_kernel(LoraOuter p) {
 }
 
 int lora_splits(int M) { return M <= 256 ? 8 : M <= 2048 ? 4 : 2; }
-size_t lora_inner_bytes(int R, int M) { return (static_cast<size_t>(lora_splits(M)) * M * R * 4 + 255) / 256 * 256; }
+size_t lora_inner_bytes(int R, int M) {
+    // enough for any number of rows up to M
+    const size_t rows = M <= 256 ? static_cast<size_t>(8) * M : M <= 2048 ? std::max<size_t>(8 * 256, static_cast<size_t>(4) * M) : std::max<size_t>(4 * 2048, static_cast<size_t>(2) * M);
+    return (rows * R * 4 + 255) / 256 * 256;
+}
 
 template <int RT, bool ALONE>
 static void inner_form(const LoraInner& p, int R, dim3 grid, hipStream_t stream) {
@@ -280,6 +284,7 @@ static void inner_form(const LoraInner& p, int R, dim3 grid, hipStream_t stream)
 }
 
 hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, const void* A, float* const* inner, int* parts, hipStream_t stream) {
+    if (rows.M <= 0 || n <= 0) return hipSuccess;
     LoraInner p{};
     int R = 0;
     for (int i = 0; i < n; ++i) {
@@ -298,6 +303,7 @@ hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, cons
 
 template <int FORM>
 static hipError_t outer_form(const LoraOuter& p, int R, int N, hipStream_t stream) {
+    if (p.rows.M <= 0) return hipSuccess;
     const dim3 grid((p.rows.M + 15) / 16, (N + 64 * kOuterTiles - 1) / (64 * kOuterTiles));   // (neighbours share a part of up)
     if (R <= 32) hipLaunchKernelGGL((lora_outer_kernel<1, FORM>), grid, dim3(256), 0, stream, p);
     else if (R <= 64) hipLaunchKernelGGL((lora_outer_kernel<2, FORM>), grid, dim3(256), 0, stream, p);

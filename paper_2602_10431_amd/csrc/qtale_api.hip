@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/qtale.h"
+#include "lora_check.h"
 #include "paged_check.h"
 #include "qtale_kernels.h"
 
@@ -223,6 +224,39 @@ struct PagedCall {
     float* attn_ws;
 };
 
+// A layer call with adapters: those of its linears, the sequences' choice, and where their scratch lies.
+struct LoraCall {
+    const qtale_layer_lora* layer;
+    const int32_t* adapter;                     // [B]
+    float* inner[kLoraMost];
+    void* pair;                                 // [rows][2 inter] fp16: gate and up before their product
+};
+
+// Inner values of those of `n` linears of one input that have adapters (`at`: which of them).
+struct LoraInners {
+    LoraDev l[kLoraMost];
+    const float* inner[kLoraMost];
+    int parts[kLoraMost];
+};
+hipError_t lora_inners(const LoraCall& lc, const qtale_lora* const* which, int n, const LoraRows& rows, const void* A, LoraInners* out, hipStream_t stream) {
+    LoraDev l[kLoraMost];
+    float* inner[kLoraMost];
+    int parts[kLoraMost], at[kLoraMost], found = 0;
+    for (int i = 0; i < n; ++i) {
+        out->l[i] = lora_device(which[i]);
+        out->inner[i] = lc.inner[i];
+        out->parts[i] = 0;
+        if (out->l[i].n == 0) continue;
+        l[found] = out->l[i];
+        inner[found] = lc.inner[i];
+        at[found++] = i;
+    }
+    if (found == 0) return hipSuccess;
+    const hipError_t e = launch_lora_inner(l, found, rows, A, inner, parts, stream);
+    for (int i = 0; i < found; ++i) out->parts[at[i]] = parts[i];
+    return e;
+}
+
 // Room for the executed tokens, rotary embedding and append, attention: in place on the compact q|k|v rows.
 int paged_attention_block(qtale_ctx* ctx, const qtale_layer_cfg* c, const PagedCall& pc, const Workspace& ws, int M_max, int B,
                           const int32_t* positions, hipStream_t stream) {
@@ -254,7 +288,7 @@ int paged_attention_block(qtale_ctx* ctx, const qtale_layer_cfg* c, const PagedC
 int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_layer_weights* w, void* x, int T,
                        const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_kv* kv,
                        int32_t* sel_idx, int32_t* sel_count, float* scores, const Workspace& ws,
-                       hipStream_t stream, LayerLink* link = nullptr, const PagedCall* paged = nullptr) {
+                       hipStream_t stream, LayerLink* link = nullptr, const PagedCall* paged = nullptr, const LoraCall* lora = nullptr) {
     const int bf16 = c->act_dtype == QTALE_ACT_BF16;
     const int H = c->hidden, nh = c->n_heads, nkv = c->n_kv_heads, d = c->head_dim, I = c->inter;
     const int ratio_mode = ctx->mode == QTALE_MODE_RATIO;
@@ -302,7 +336,8 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
     qg.epilogue = EPI_STORE_F16; qg.out = ws.qkv; qg.ldo = qkv_w;
 
     const bool scored = link && link->scores_ready;
-    const bool few_fused = few_prologue_fits(T, M_max, H);
+    const bool few_fused = !lora && few_prologue_fits(T, M_max, H);   // (adapters need the linears' inputs in memory)
+    const LoraRows lora_rows{lora ? lora->adapter : nullptr, ws.row_seq, count, M_max, B};
     if (!scored && (!few_fused || w->router_hidden > 0)) {
         Prof pr(ctx, stream, 0);
         if (w->router_hidden > 0)
@@ -351,6 +386,14 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
     {
         Prof pr(ctx, stream, 3);
         HIP_TRY(launch_gemm_w4a16(qg, stream));
+        if (lora) {
+            const qtale_lora* which[3] = {&lora->layer->q, &lora->layer->k, &lora->layer->v};
+            const int columns[3] = {0, nh * d, (nh + nkv) * d};
+            LoraInners in;
+            HIP_TRY(lora_inners(*lora, which, 3, lora_rows, ws.nbuf, &in, stream));
+            for (int i = 0; i < 3; ++i)
+                if (in.l[i].n) HIP_TRY(launch_lora_add(in.l[i], lora_rows, in.inner[i], in.parts[i], reinterpret_cast<uint16_t*>(ws.qkv) + columns[i], qkv_w, 0, stream));
+        }
     }
     // Prefill attention: the work list comes from the launch before it, the partial sums of key ranges go to what lies free until
     // the o-proj: the buffers from h to the parts of the GEMMs, which adjoin (the ranges' counters first)
@@ -393,8 +436,15 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
         g.A = ws.attn; g.count = count; g.M_max = M_max; g.rows_exact = ratio_mode; g.streams = streams; g.K = nh * d; g.group = c->group; g.bits = lbits; g.n_w = 1;
         g.w[0] = {w->o.prepacked, w->o.N, w->o.K};
         g.epilogue = EPI_RESID_F32; g.out = ws.h; g.ldo = H; g.resid = x; g.idx = ws.idx; g.bf16 = bf16;
-        g.part = o_part; g.part_floats = o_floats; g.n_parts = &o_parts;
+        const bool adapted = lora && lora->layer->o.n_adapters > 0;   // (they add to the sum of all parts)
+        if (!adapted) { g.part = o_part; g.part_floats = o_floats; g.n_parts = &o_parts; }
         HIP_TRY(launch_gemm_w4a16(g, stream));
+        if (adapted) {
+            const qtale_lora* which[1] = {&lora->layer->o};
+            LoraInners in;
+            HIP_TRY(lora_inners(*lora, which, 1, lora_rows, ws.attn, &in, stream));
+            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.inner[0], in.parts[0], ws.h, H, 1, stream));
+        }
     }
     if (!few_fused) {
         Prof pr(ctx, stream, 7);
@@ -415,10 +465,24 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             pro.h = ws.h; pro.gain = w->norm2;
             g.pro = &pro;
         }
+        const bool adapted = lora && (lora->layer->gate.n_adapters > 0 || lora->layer->up.n_adapters > 0);
+        if (adapted) { g.epilogue = EPI_STORE_F16; g.out = lora->pair; g.ldo = 2 * I; }
         HIP_TRY(launch_gemm_w4a16(g, stream));
+        if (adapted) {
+            const qtale_lora* which[2] = {&lora->layer->gate, &lora->layer->up};
+            LoraInners in;
+            HIP_TRY(lora_inners(*lora, which, 2, lora_rows, ws.nbuf, &in, stream));
+            HIP_TRY(launch_lora_swiglu(in.l[0], in.l[1], lora_rows, in.inner[0], in.inner[1], in.parts[0], in.parts[1], lora->pair, ws.act, I, stream));
+        }
     }
     {
         Prof pr(ctx, stream, 9);
+        if (lora && lora->layer->down.n_adapters > 0) {          // into the residual that the product is added to
+            const qtale_lora* which[1] = {&lora->layer->down};
+            LoraInners in;
+            HIP_TRY(lora_inners(*lora, which, 1, lora_rows, ws.act, &in, stream));
+            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.inner[0], in.parts[0], ws.h, H, 1, stream));
+        }
         GemmArgs g{};
         g.A = ws.act; g.count = count; g.M_max = M_max; g.rows_exact = ratio_mode; g.streams = streams; g.K = I; g.group = c->group; g.bits = lbits; g.n_w = 1;
         g.w[0] = {w->down.prepacked, w->down.N, w->down.K};
@@ -697,10 +761,30 @@ size_t qtale_paged_stack_workspace_bytes(const qtale_layer_cfg* cfg, const qtale
            paged_attention_bytes(cfg->n_heads, cfg->n_kv_heads, cfg->head_dim, max_tokens, max_seqs);
 }
 
-int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, int n_layers, int first_layer,
-                              void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_paged_kv* kv,
-                              const int32_t* slots, const qtale_rope* rope, const qtale_paged_attn* attn, int32_t* missing,
-                              int32_t* sel_idx, int32_t* sel_count, float* scores, void* workspace, size_t workspace_bytes, void* stream) {
+namespace {
+
+size_t lora_stack_bytes(const qtale_layer_cfg* cfg, int max_rank, int max_tokens) {
+    return kLoraMost * lora_inner_bytes(max_rank, max_tokens) + align_up(static_cast<size_t>(max_tokens) * 2 * cfg->inter * 2, 256);
+}
+
+int check_layer_lora(const qtale_layer_cfg* c, const qtale_layer_lora* l, int* max_rank) {
+    const int H = c->hidden, qd = c->n_heads * c->head_dim, kd = c->n_kv_heads * c->head_dim;
+    const struct { const qtale_lora* l; int N, K; } all[] = {{&l->q, qd, H}, {&l->k, kd, H}, {&l->v, kd, H}, {&l->o, H, qd},
+                                                             {&l->gate, c->inter, H}, {&l->up, c->inter, H}, {&l->down, H, c->inter}};
+    for (const auto& x : all) {
+        if (x.l->n_adapters == 0) continue;
+        const int e = check_lora(x.l, x.N, x.K, true);
+        if (e) return e;
+        *max_rank = std::max(*max_rank, x.l->max_rank);
+    }
+    return QTALE_OK;
+}
+
+// loras and adapter: both or neither
+int paged_stack(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, const qtale_layer_lora* loras, int n_layers, int first_layer,
+                void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_paged_kv* kv, const int32_t* slots,
+                const int32_t* adapter, const qtale_rope* rope, const qtale_paged_attn* attn, int32_t* missing, int32_t* sel_idx, int32_t* sel_count,
+                float* scores, void* workspace, size_t workspace_bytes, void* stream) {
     int e = check_forward_args(ctx, cfg, x, T, seq_offsets, B, positions, workspace, workspace_bytes);
     if (e) return e;
     if ((e = check_paged(kv, true)) || (e = check_rope(rope, cfg->head_dim)) || (e = check_paged_attn(attn, kv))) return e;
@@ -712,8 +796,19 @@ int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const 
     if (!slots && B > kv->n_slots) return QTALE_ERR_SHAPE;
     for (int l = 0; l < n_layers; ++l)
         if ((e = check_weights(cfg, &layers[l]))) return e;
+    int max_rank = 0;
+    for (int l = 0; l < n_layers && loras; ++l)
+        if ((e = check_layer_lora(cfg, &loras[l], &max_rank))) return e;
     if (T == 0) return QTALE_OK;
-    if (workspace_bytes < qtale_paged_stack_workspace_bytes(cfg, kv, T, B)) return QTALE_ERR_WORKSPACE_TOO_SMALL;
+    const size_t stack_bytes = qtale_paged_stack_workspace_bytes(cfg, kv, T, B);
+    if (workspace_bytes < stack_bytes + (max_rank > 0 ? lora_stack_bytes(cfg, max_rank, T) : 0)) return QTALE_ERR_WORKSPACE_TOO_SMALL;
+    LoraCall lc{};
+    if (max_rank > 0) {
+        char* at = reinterpret_cast<char*>(workspace) + stack_bytes;
+        lc.adapter = adapter;
+        for (int i = 0; i < kLoraMost; ++i, at += lora_inner_bytes(max_rank, T)) lc.inner[i] = reinterpret_cast<float*>(at);
+        lc.pair = at;
+    }
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Workspace ws = carve(cfg, T, B, workspace);
     PagedCall pc{};
@@ -733,12 +828,39 @@ int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const 
         }
         pc.layer = first_layer + l;
         pc.missing = missing ? missing + l : nullptr;
+        if (max_rank > 0) lc.layer = &loras[l];
         e = layer_forward_impl(ctx, cfg, &layers[l], x, T, seq_offsets, B, positions, nullptr, sel_idx ? sel_idx + static_cast<size_t>(l) * T : nullptr,
-                               sel_count ? sel_count + l : nullptr, scores ? scores + static_cast<size_t>(l) * T : nullptr, ws, s, &link, &pc);
+                               sel_count ? sel_count + l : nullptr, scores ? scores + static_cast<size_t>(l) * T : nullptr, ws, s, &link, &pc, max_rank > 0 ? &lc : nullptr);
         if (e) return e;
         scores_ready = link.next_scored;
     }
     return QTALE_OK;
+}
+
+}  // namespace
+
+int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, int n_layers, int first_layer,
+                              void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_paged_kv* kv,
+                              const int32_t* slots, const qtale_rope* rope, const qtale_paged_attn* attn, int32_t* missing,
+                              int32_t* sel_idx, int32_t* sel_count, float* scores, void* workspace, size_t workspace_bytes, void* stream) {
+    return paged_stack(ctx, cfg, layers, nullptr, n_layers, first_layer, x, T, seq_offsets, B, positions, kv, slots, nullptr, rope, attn, missing, sel_idx,
+                       sel_count, scores, workspace, workspace_bytes, stream);
+}
+
+size_t qtale_paged_stack_lora_workspace_bytes(const qtale_layer_cfg* cfg, const qtale_paged_kv* kv, int max_rank, int max_tokens, int max_seqs) {
+    const size_t stack = qtale_paged_stack_workspace_bytes(cfg, kv, max_tokens, max_seqs);
+    if (stack == 0 || max_rank < 0 || max_rank > 128 || max_rank % 8 != 0) return 0;
+    return stack + (max_rank > 0 ? lora_stack_bytes(cfg, max_rank, max_tokens) : 0);
+}
+
+int qtale_paged_stack_lora_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, const qtale_layer_lora* loras,
+                                   int n_layers, int first_layer, void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions,
+                                   const qtale_paged_kv* kv, const int32_t* slots, const int32_t* adapter, const qtale_rope* rope,
+                                   const qtale_paged_attn* attn, int32_t* missing, int32_t* sel_idx, int32_t* sel_count, float* scores,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+    if ((n_layers > 0 && !loras) || (T > 0 && !adapter)) return QTALE_ERR_INVALID_ARG;
+    return paged_stack(ctx, cfg, layers, loras, n_layers, first_layer, x, T, seq_offsets, B, positions, kv, slots, adapter, rope, attn, missing, sel_idx,
+                       sel_count, scores, workspace, workspace_bytes, stream);
 }
 
 int qtale_router_select(qtale_ctx* ctx, int act_dtype, const void* x, int T, int hidden, const float* router_w,
