@@ -268,10 +268,12 @@ lora_outer_kernel(LoraOuter p) {
     }
 }
 
-int lora_splits(int M) { return M <= 256 ? 8 : M <= 2048 ? 4 : 2; }
+// Parts of K that fill the chip: tiles of 64 rows, three workgroups per CU.
+constexpr int kInnerFill = 768;
+int lora_splits(int M) { return std::min(std::max((kInnerFill * 64 + M - 1) / std::max(M, 1), 1), 8); }
 size_t lora_inner_bytes(int R, int M) {
-    // enough for any number of rows up to M
-    const size_t rows = M <= 256 ? static_cast<size_t>(8) * M : M <= 2048 ? std::max<size_t>(8 * 256, static_cast<size_t>(4) * M) : std::max<size_t>(4 * 2048, static_cast<size_t>(2) * M);
+    // enough for any number of rows up to M: parts * M <= 8 M, and <= 64 * kInnerFill + M
+    const size_t rows = std::min<size_t>(static_cast<size_t>(8) * M, static_cast<size_t>(kInnerFill) * 64 + M);
     return (rows * R * 4 + 255) / 256 * 256;
 }
 

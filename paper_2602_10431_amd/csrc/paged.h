@@ -108,7 +108,7 @@ constexpr int kWideCols = 256;                   // ... of its form with two hal
 constexpr int kChunkTileKeys = 64;
 constexpr int kSpanSeqs = 1024;                  // bound on the sequences of a call that is cut into spans
 constexpr int part_stride(int d) { return d + 4; }   // floats of a column's sums: numerators, reference point, denominator, (chunk) ranges, unused
-PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks);
+PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks);
 size_t paged_attention_bytes(int nh, int nkv, int d, int T, int B);   // of workspace, for any call of at most T tokens and B sequences
 // All launches of a call; a: everything but `take` and what follows it, which the plan says.
 hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int d, int T, float* workspace, hipStream_t stream);

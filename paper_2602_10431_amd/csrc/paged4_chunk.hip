@@ -2,11 +2,11 @@
 //
 // The waves of a workgroup unpack a tile together: codes less their zero point as fp16 multiples of 2^-24 (code bits 4 - 7: of 2^-20, with the 16 in the
 // queries' elements or taken from the result), exact, into LDS, K as [key][d], V transposed as [column][key] in the order of the second product's
-// operand, which the layout of a value page gives without permutations.  Tile t + 1 is unpacked and tile t + 2 requested while tile t is
-// computed; one barrier per tile.  Scales stay outside the products:
+// operand, which the layout of a value page gives without permutations.  Scales stay outside the products:
 //   score = s_j (q . (c_j - z_j)),   out = sum_j (p_j t_j) (c'_j - z'_j) / sum_j p_j.
-// Queries are fp16 relative to their row's power of two.  Probabilities are 2^(score - m_run), where m_run holds the reference point, the lift
-// (kChunkLift) and log2 of t_ref, a power of two above all t so far: so p t fits fp16 whatever the values' size, for one multiplication.
+// Queries are fp16; a row that is too large for it, or small, comes relative to its power of two.  Probabilities are 2^(score - m_run), where m_run holds the
+// reference point, the lift (kChunkLift) and log2 of t_ref, a power of two above all t so far: so p t fits fp16 whatever the values' size, for
+// one multiplication.
 #include <algorithm>
 
 #include "paged4.h"
@@ -24,61 +24,120 @@ __device__ __forceinline__ u32x4_t codes_less4(uint32_t w, uint32_t z) {
     const uint32_t y = w >> 8, z16 = z << 4;
     return u32x4_t{less(w & 0x000f000fu, z), less(w & 0x00f000f0u, z16), less(y & 0x000f000fu, z), less(y & 0x00f000f0u, z16)};
 }
+// Where 16-byte chunk c of a row lies: at chunk c ^ swizzle, such that what a read or a write touches at a time spreads over the banks.
 template <int D> __device__ __forceinline__ int k4_swizzle(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
 __device__ __forceinline__ int v4_swizzle(int col) { return ((col >> 1) ^ (col >> 4)) & 7; }
 
-// NW waves of 32 columns.  SPLIT: key ranges.
-template <int D, bool BF16, bool SPLIT, int NW>
-__global__ void __launch_bounds__(64 * NW, 2)
-paged4_chunk_kernel(PagedAttnDev p) {
-    using H = Act16<false>;
-    constexpr int KS = D / 16;                   // k-steps of the scores
-    constexpr int DF = D / 32;                   // output fragments
-    constexpr int S = D / 32;                    // words of codes per lane
-    constexpr int COLS = 32 * NW, TILE = kTileKeys * D;
+// A tile in LDS.
+template <int D>
+struct Tile4 {
+    uint16_t* K;                 // [64 keys][D]
+    uint16_t* V;                 // [D columns][64 keys]
+    float *ks, *ts, *tmax;       // scales of keys (with the softmax scale) and values, the largest of 16 values each
+};
+
+// One wave's part of unpacking tiles: 16 keys, or 16 values, or both.
+template <int D, bool BF16>
+struct Unpack4 {
+    static constexpr int S = D / 32;             // words of codes per lane
     typedef uint32_t Words __attribute__((ext_vector_type(S)));
-    __shared__ __attribute__((aligned(1024))) uint16_t Ks[2][TILE], Vs[2][TILE];
-    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys], tmax[2][4];   // scales of keys and values, largest of 16 values each
+    const PagedAttnDev& p;
+    int hk, part, hi;
+    uint32_t params_at, block;
+    float unit;
+    Words kw, vw;
+    uint32_t kp;
+    u32x4_t vp;
 
-    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lhi = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave & 3;   // part: which 16 keys of a tile this wave unpacks
-
-    int hk, item, z = 0, b, qt;
-    find_head(p, &hk, &item);
-    if (SPLIT) {
-        z = __builtin_amdgcn_readfirstlane(item / p.items);
-        item -= z * p.items;
+    __device__ __forceinline__ Unpack4(const PagedAttnDev& p, int hk, int part, int hi)
+        : p(p), hk(hk), part(part), hi(hi), params_at(static_cast<uint32_t>(D / 2) << p.shift), block(params_at + (4u << p.shift)), unit(p.scale_log2 * 0x1p24f) {}
+    static __device__ __forceinline__ Words load(__amdgpu_buffer_rsrc_t buf, uint32_t off, uint32_t base) {
+        if constexpr (S == 4) return __builtin_amdgcn_raw_buffer_load_b128(buf, off, base, 0);
+        else return __builtin_amdgcn_raw_buffer_load_b64(buf, off, base, 0);
     }
-    if (!find_columns<COLS>(p, item, &b, &qt)) return;
-    SeqView s(p, b);
-    s.uniform();
-    const int c_lo = qt * COLS, c_hi = min(c_lo + COLS, s.n * p.rep) - 1;   // this workgroup's columns
-    const KeySteps<kTileKeys> walk(s.first + __builtin_amdgcn_readfirstlane(c_lo / p.rep), s.first + __builtin_amdgcn_readfirstlane(c_hi / p.rep), s.len, p.window, p.sinks);
-    int t0 = 0, t1 = walk.steps, ranges = 1;
-    if (SPLIT) {
-        // ranges of about equal length over the whole call, as many as are to run at once; no item is cut into more than p.ranges
-        int work = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 64) work += b0 + lane < p.B ? chunk_work(p, b0 + lane) : 0;
+    // the head's block of a page; of one that is gone: an empty buffer, zeros
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint16_t* pool, int page) const {
+        return buffer_of(reinterpret_cast<const char*>(pool) + (static_cast<size_t>(max(page, 0)) * p.nkv + hk) * block, page < 0 ? 0 : static_cast<int>(block));
+    }
+    // key0: the tile's first
+    __device__ __forceinline__ void request_keys(int key0, int page) {
+        const int lane = threadIdx.x & 63;
+        const uint32_t t = (key0 + 16 * part) & ((1 << p.shift) - 1);
+        const auto buf = buffer(p.k, page);
+        kw = load(buf, (lane >> 2) * (D / 2) + (lane & 3) * (D / 8), t * (D / 2));
+        kp = __builtin_amdgcn_raw_buffer_load_b32(buf, 4 * (lane >> 2), params_at + 4 * t, 0);
+    }
+    __device__ __forceinline__ void request_values(int key0, int page) {
+        const int lane = threadIdx.x & 63;
+        const uint32_t t = (key0 + 16 * part) & ((1 << p.shift) - 1);
+        const auto buf = buffer(p.v, page);
+        vw = load(buf, (lane >> 4) * (2 * D) + (lane & 15) * (D / 8), t * (D / 2));
+        vp = __builtin_amdgcn_raw_buffer_load_b128(buf, 16 * (lane >> 4), params_at + 4 * t, 0);
+    }
+    // Places from `hi` on get scales of zero (what lies in unused places may be anything, zero points too).
+    __device__ __forceinline__ void put_keys(int key0, const Tile4<D>& to) const {
+        const int lane = threadIdx.x & 63, key = 16 * part + (lane >> 2);
+        const uint32_t zz = __builtin_amdgcn_perm(kp, kp, 0x07060706u) & 0x000f000fu;
 #pragma unroll
-        for (int x = 32; x > 0; x >>= 1) work += __shfl_xor(work, x, 64);
-        const int wanted = max(p.target / p.nkv, 1);
-        const int per = __builtin_amdgcn_readfirstlane(max(max((work + wanted - 1) / wanted, (walk.steps + p.ranges - 1) / p.ranges), 4));
-        ranges = __builtin_amdgcn_readfirstlane(max((walk.steps + per - 1) / per, 1));
-        if (z >= ranges) return;
-        t0 = z * per;
-        t1 = min(t0 + per, walk.steps);
+        for (int w = 0; w < S; ++w)
+            *reinterpret_cast<u32x4_t*>(&to.K[key * D + (((S * (lane & 3) + w) ^ k4_swizzle<D>(key)) * 8)]) = codes_less4(kw[w], zz);
+        if ((lane & 3) == 0) to.ks[key] = key0 + key < hi ? act_to_float<BF16>(static_cast<uint16_t>(kp & 0xffffu)) * unit : 0.0f;
     }
-    // this lane's column (clamped to a live one): query, head, its place, keys after `reach` are in its window
-    const int col = min(c_lo + 32 * wave + l32, c_hi), qi = col / p.rep, head = hk * p.rep + col - qi * p.rep;
-    const int place = s.first + qi, reach = p.window > 0 ? place - p.window : INT32_MIN;
-    const bool mine = c_lo + 32 * wave + l32 <= c_hi;
-    const int w_first = s.first + __builtin_amdgcn_readfirstlane(min(c_lo + 32 * wave, c_hi) / p.rep);   // places of the wave's queries
-    const int w_last = s.first + __builtin_amdgcn_readfirstlane(min(c_lo + 32 * wave + 31, c_hi) / p.rep);
+    __device__ __forceinline__ void put_values(int key0, const Tile4<D>& to) const {
+        const int lane = threadIdx.x & 63, four = lane >> 4, c = lane & 15;
+        float4_t t4;
+        float big = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            t4[r] = key0 + 16 * part + 4 * four + r < hi ? act_to_float<BF16>(static_cast<uint16_t>(vp[r] & 0xffffu)) : 0.0f;
+            big = fmaxf(big, t4[r]);
+        }
+        if (c == 0) *reinterpret_cast<float4_t*>(&to.ts[16 * part + 4 * four]) = t4;
+        big = fmaxf(big, __shfl_xor(big, 16, 64));
+        big = fmaxf(big, __shfl_xor(big, 32, 64));
+        if (lane == 0) to.tmax[part] = big;
+        const uint32_t z01 = __builtin_amdgcn_perm(vp[1], vp[0], 0x07060302u) & 0x000f000fu, z23 = __builtin_amdgcn_perm(vp[3], vp[2], 0x07060302u) & 0x000f000fu;
+        // tokens 4 four .. + 3 of 16: chunk 2 part + (four & 1) of a column's row, its half four >> 1
+#pragma unroll
+        for (int h = 0; h < S / 2; ++h) {
+            const u32x4_t a = codes_less4(vw[2 * h], z01), b = codes_less4(vw[2 * h + 1], z23);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int column = (D / 16) * c + 4 * h + i;
+                *reinterpret_cast<u32x2_t*>(&to.V[column * kTileKeys + (((2 * part + (four & 1)) ^ v4_swizzle(column)) * 8) + 4 * (four >> 1)]) = u32x2_t{a[i], b[i]};
+            }
+        }
+    }
+};
 
-    // queries as fp16, the row's largest at 2^13; up: the power of two that a score's unit stands for
-    u32x4_t qf[KS];
-    float up;
-    {
+// One wave's 32 columns: their queries, scores of a tile, probabilities and sums.
+template <int D, bool BF16>
+struct Columns4 {
+    using H = Act16<false>;
+    static constexpr int KS = D / 16;            // k-steps of the scores
+    static constexpr int DF = D / 32;            // output fragments
+    static constexpr int PV = 4 * DF, ALL = PV + 2 * KS;
+    int qi, head, place, reach;                  // this lane's column (clamped to a live one): query, head, its place, keys after `reach` are in its window
+    bool mine, plain;                            // the lane's column exists; all columns of the wave have up == 1
+    int w_first, w_last;                         // places of the wave's queries
+    u32x4_t qf[KS], pf[4];
+    float up;                                    // the power of two that a score's unit stands for
+    int k_at[KS], v_at[4];                       // LDS elements that this lane reads
+    float16_t st[2], o[DF];
+    float m_run, l_run;
+    int t_exp;                                   // log2 of t_ref
+
+    // columns .. c_hi; c0: the wave's first
+    __device__ __forceinline__ Columns4(const PagedAttnDev& p, const SeqView& s, int hk, int c0, int c_hi) {
+        const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
+        const int col = min(c0 + l32, c_hi);
+        qi = col / p.rep;
+        head = hk * p.rep + col - qi * p.rep;
+        place = s.first + qi;
+        reach = p.window > 0 ? place - p.window : INT32_MIN;
+        mine = c0 + l32 <= c_hi;
+        w_first = s.first + __builtin_amdgcn_readfirstlane(min(c0, c_hi) / p.rep);   // (divisions run on the vector ALUs)
+        w_last = s.first + __builtin_amdgcn_readfirstlane(min(c0 + 31, c_hi) / p.rep);
         const uint16_t* qrow = p.q + (s.row0 + qi) * p.q_stride + head * D + 8 * lhi;
         float big = 0.0f;
 #pragma unroll
@@ -88,242 +147,397 @@ paged4_chunk_kernel(PagedAttnDev p) {
             for (int w = 0; w < 4; ++w) big = fmaxf(big, fmaxf(fabsf(Act16<BF16>::low(qf[k][w])), fabsf(Act16<BF16>::high(qf[k][w]))));
         }
         big = fmaxf(big, __shfl_xor(big, 32, 64));
-        const int e = min(max(static_cast<int>(__float_as_uint(big) >> 23) - 127, -100), 127);
-        const float f = ldexpf(1.0f, 13 - e), f16 = f * 0.0625f;
+        // (elements of a row between 2^-4 and 2^15 at its largest: a sixteenth of one that is 2^-6 of the largest still has all its bits)
+        const int e = static_cast<int>(__float_as_uint(big) >> 23) - 127, move = e >= 15 || e < -4 ? 13 - min(max(e, -100), 127) : 0;
+        const float f = ldexpf(1.0f, move), f16 = f * 0.0625f;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int w = 0; w < 4; ++w) qf[k][w] = H::pack(Act16<BF16>::low(qf[k][w]) * (w & 1 ? f16 : f), Act16<BF16>::high(qf[k][w]) * (w & 1 ? f16 : f));
-        up = ldexpf(1.0f, e - 13);
+        up = ldexpf(1.0f, -move);
+        plain = __all(move == 0);
+        // chunk 2 k + lhi of key l32; chunk 2 s2 + lhi of column 32 f + l32: v_at[(f ^ s2) & 3] + 32 f rows (the swizzle of that column is l32's with 2 f
+        // flipped in)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) k_at[k] = l32 * D + (((2 * k + lhi) ^ k4_swizzle<D>(l32)) * 8);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v_at[x] = l32 * kTileKeys + (((2 * x + lhi) ^ v4_swizzle(l32)) * 8);
+#pragma unroll
+        for (int f = 0; f < DF; ++f)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[f][r] = 0.0f;
+        m_run = kPagedNone;
+        l_run = 0.0f;
+        t_exp = -60;
     }
-    const float unit = p.scale_log2 * 0x1p24f;
 
-    // LDS elements that this lane reads: chunk 2 k + lhi of key l32; chunk 2 s2 + lhi of column l32 of a fragment
-    int k_at[KS];
+    __device__ __forceinline__ u32x4_t operand(const uint16_t* V, const uint16_t* K, int i) const {
+        if (i < PV) {
+            const int s2 = i / DF, f = i % DF;
+            return *reinterpret_cast<const u32x4_t*>(&V[32 * f * kTileKeys + v_at[(f ^ s2) & 3]]);
+        }
+        return *reinterpret_cast<const u32x4_t*>(&K[((i - PV) & 1) * 32 * D + k_at[(i - PV) >> 1]]);
+    }
+    // Products FROM .. ALL - 1 of O^T += V^T P^T of one tile, then S^T = K Q^T of the next; operands read AHEAD products before their use.
+    template <int FROM, int TO>
+    __device__ __forceinline__ void products(const uint16_t* V, const uint16_t* K) {
+        constexpr int AHEAD = 6;
+        u32x4_t x[AHEAD];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) k_at[k] = l32 * D + (((2 * k + lhi) ^ k4_swizzle<D>(l32)) * 8);
-    auto v_chunk = [&](int f, int s2) { return (32 * f + l32) * kTileKeys + (((2 * s2 + lhi) ^ v4_swizzle(32 * f + l32)) * 8); };
+        for (int i = 0; i < AHEAD; ++i) x[i] = operand(V, K, FROM + i);
+        if (TO > PV) {
+#pragma unroll
+            for (int kf = 0; kf < 2; ++kf)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[kf][r] = 0.0f;
+        }
+#pragma unroll
+        for (int i = FROM; i < TO; ++i) {
+            const u32x4_t now = x[(i - FROM) % AHEAD];
+            if (i < PV) o[i % DF] = H::mfma32(now, pf[i / DF], o[i % DF]);
+            else st[(i - PV) & 1] = H::mfma32(now, qf[(i - PV) >> 1], st[(i - PV) & 1]);
+            if (i + AHEAD < TO) x[(i - FROM) % AHEAD] = operand(V, K, i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
 
-    // what a wave requests of a tile: its 16 keys' codes and words s | z << 16 (NW 8: waves 0 - 3 keys, waves 4 - 7 values)
-    const bool keys = NW == 4 || wave < 4, values = NW == 4 || wave >= 4;
-    const PageRow pages(p, s.slot);
-    const uint32_t params_at = static_cast<uint32_t>(D / 2) << p.shift, block = params_at + (4u << p.shift);
-    const int my_key = lane >> 2, my_part = lane & 3, my_four = lane >> 4, my_c = lane & 15;
-    Words kw, vw;
-    uint32_t kp = 0;
-    u32x4_t vp;
-    auto load = [](__amdgpu_buffer_rsrc_t buf, uint32_t off, uint32_t base) __attribute__((always_inline)) {
-        if constexpr (S == 4) return __builtin_amdgcn_raw_buffer_load_b128(buf, off, base, 0);
-        else return __builtin_amdgcn_raw_buffer_load_b64(buf, off, base, 0);
-    };
-    auto request = [&](int tile, int page) __attribute__((always_inline)) {
-        const uint32_t t = (walk.key(tile) + 16 * part) & ((1 << p.shift) - 1);
-        const size_t at = (static_cast<size_t>(max(page, 0)) * p.nkv + hk) * block;
-        const int size = page < 0 || tile >= t1 ? 0 : static_cast<int>(block);   // (of a page that is gone: an empty buffer, zeros)
-        if (keys) {
-            const auto buf = buffer_of(reinterpret_cast<const char*>(p.k) + at, size);
-            kw = load(buf, my_key * (D / 2) + my_part * (D / 8), t * (D / 2));
-            kp = __builtin_amdgcn_raw_buffer_load_b32(buf, 4 * my_key, params_at + 4 * t, 0);
-        }
-        if (values) {
-            const auto buf = buffer_of(reinterpret_cast<const char*>(p.v) + at, size);
-            vw = load(buf, my_four * (2 * D) + my_c * (D / 8), t * (D / 2));
-            vp = __builtin_amdgcn_raw_buffer_load_b128(buf, 16 * my_four, params_at + 4 * t, 0);
-        }
-    };
-    // the requested tile -> LDS; places from `hi` on get scales of zero (what lies there may be anything)
-    auto unpack = [&](int tile, int buf) __attribute__((always_inline)) {
-        const int key0 = walk.key(tile) + 16 * part;
-        if (keys) {
-            const int key = 16 * part + my_key;
-            const uint32_t zz = __builtin_amdgcn_perm(kp, kp, 0x07060706u) & 0x000f000fu;   // (in unused places it may be anything)
-#pragma unroll
-            for (int w = 0; w < S; ++w)
-                *reinterpret_cast<u32x4_t*>(&Ks[buf][key * D + (((S * my_part + w) ^ k4_swizzle<D>(key)) * 8)]) = codes_less4(kw[w], zz);
-            if (my_part == 0) ks[buf][key] = key0 + my_key < walk.hi ? act_to_float<BF16>(static_cast<uint16_t>(kp & 0xffffu)) * unit : 0.0f;
-        }
-        if (values) {
-            float t4[4], big = 0.0f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                t4[r] = key0 + 4 * my_four + r < walk.hi ? act_to_float<BF16>(static_cast<uint16_t>(vp[r] & 0xffffu)) : 0.0f;
-                big = fmaxf(big, t4[r]);
-            }
-            if (my_c == 0) *reinterpret_cast<float4_t*>(&ts[buf][16 * part + 4 * my_four]) = float4_t{t4[0], t4[1], t4[2], t4[3]};
-            big = fmaxf(big, __shfl_xor(big, 16, 64));
-            big = fmaxf(big, __shfl_xor(big, 32, 64));
-            if (lane == 0) tmax[buf][part] = big;
-            const uint32_t z01 = __builtin_amdgcn_perm(vp[1], vp[0], 0x07060302u) & 0x000f000fu, z23 = __builtin_amdgcn_perm(vp[3], vp[2], 0x07060302u) & 0x000f000fu;
-            // tokens 4 my_four .. + 3 of 16: chunk 2 part + (my_four & 1) of a column's row, its half my_four >> 1
-#pragma unroll
-            for (int h = 0; h < S / 2; ++h) {
-                const u32x4_t a = codes_less4(vw[2 * h], z01), c = codes_less4(vw[2 * h + 1], z23);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int column = (D / 16) * my_c + 4 * h + i;
-                    *reinterpret_cast<u32x2_t*>(&Vs[buf][column * kTileKeys + (((2 * part + (my_four & 1)) ^ v4_swizzle(column)) * 8) + 4 * (my_four >> 1)]) = u32x2_t{a[i], c[i]};
-                }
-            }
-        }
-    };
-    auto ids_of = [&](int tile) __attribute__((always_inline)) { return tile_pages(pages, walk.key(min(tile, walk.steps - 1)), part); };
-
-    float16_t o[DF];
-#pragma unroll
-    for (int f = 0; f < DF; ++f)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[f][r] = 0.0f;
-    float m_run = kPagedNone, l_run = 0.0f;
-    int t_exp = -60;                             // log2 of t_ref
-    auto turn = [&](int t, int gone, int buf) __attribute__((always_inline)) {
-        const int key0 = walk.key(t);
-        float16_t st[2];
-#pragma unroll
-        for (int kf = 0; kf < 2; ++kf)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) st[kf][r] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) {
-            const int kf = i / KS, k = i % KS;
-            st[kf] = H::mfma32(*reinterpret_cast<const u32x4_t*>(&Ks[buf][kf * 32 * D + k_at[k]]), qf[k], st[kf]);
-        }
+    // Scores -> probabilities as operands, times their values' scales; the probabilities' sum.  FAST: scores are products (st) times their key's scale, one
+    // fused operation; else st holds scores, of `hidden` keys minus infinity.
+    template <bool FAST>
+    __device__ __forceinline__ float weigh(const Tile4<D>& tile, uint32_t hidden) {
+        const int lhi = (threadIdx.x & 63) >> 5;
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int kf = 0; kf < 2; ++kf)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
-                const float4_t x = *reinterpret_cast<const float4_t*>(&ks[buf][32 * kf + 8 * q4 + 4 * lhi]);
+                const int at = 32 * kf + 8 * q4 + 4 * lhi;
+                const float4_t t4 = *reinterpret_cast<const float4_t*>(&tile.ts[at]);
+                float4_t k4 = {0.f, 0.f, 0.f, 0.f};
+                if (FAST) k4 = *reinterpret_cast<const float4_t*>(&tile.ks[at]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) st[kf][4 * q4 + r] *= x[r];
+                for (int r = 0; r < 4; r += 2) {
+                    const int i = 4 * q4 + r;
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(st[kf][i], FAST ? k4[r] : up, -m_run));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(st[kf][i + 1], FAST ? k4[r + 1] : up, -m_run));
+                    sum[q4] += p0 + p1;
+                    float w0 = p0 * t4[r], w1 = p1 * t4[r + 1];
+                    if (!FAST) {                                 // (a scale that the column does not see may be NaN)
+                        w0 = hidden >> (16 * kf + i) & 1 ? 0.0f : w0;
+                        w1 = hidden >> (16 * kf + i + 1) & 1 ? 0.0f : w1;
+                    }
+                    uint32_t w = H::pack(w0, w1);
+                    asm("" : "+v"(w));                           // (packed here: carried past the caller's branch, 32 values would take 16 registers more)
+                    pf[kf * 2 + (q4 >> 1)][2 * (q4 & 1) + (r >> 1)] = w;
+                }
             }
-        // a tile that every query of the wave sees whole needs no mask
+        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+    // st: products -> scores (in units of `up`)
+    __device__ __forceinline__ void scale_scores(const Tile4<D>& tile) {
+        const int lhi = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int kf = 0; kf < 2; ++kf)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const float4_t k4 = *reinterpret_cast<const float4_t*>(&tile.ks[32 * kf + 8 * q4 + 4 * lhi]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) st[kf][4 * q4 + r] *= k4[r];
+            }
+    }
+    // Probabilities of keys key0 .. key0 + 63; gone: bit per 16 keys without a page.
+    __device__ __forceinline__ void softmax(const PagedAttnDev& p, const Tile4<D>& tile, int key0, int gone, int hi) {
+        const int lhi = (threadIdx.x & 63) >> 5;
+        // values' scales above the reference so far: the next power of two but one
+        const float4_t tm = *reinterpret_cast<const float4_t*>(tile.tmax);
+        const float tx = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3])))));
+        if (tx > ldexpf(1.0f, t_exp)) {
+            const int e = min(static_cast<int>(__float_as_uint(tx) >> 23) - 127 + 2, 126);
+            const float beta = ldexpf(1.0f, t_exp - e);
+            m_run = m_run > kPagedNone ? m_run + static_cast<float>(e - t_exp) : m_run;
+            rescale(beta);
+            t_exp = e;
+        }
+        // The reference point stays as long as the probabilities' sum over the lane's keys does not pass fp16's largest number, so each fits; it is seen
+        // from the sum that is needed anyway.
+        const float most = ldexpf(65504.0f, -t_exp);
+        // A tile that every query of the wave sees whole needs no mask.  One fused operation is exact enough while a score's last bit, which the reference
+        // point has been rounded to, is small.
+        const bool all = gone == 0 && key0 + kTileKeys <= min(w_first + 1, hi) && (p.window == 0 || key0 > w_last - p.window || key0 + kTileKeys <= p.sinks);
+        float sum = 0.0f;
+        if (all && plain) {
+            sum = weigh<true>(tile, 0u);
+            if (!__any(!(sum <= most) | (fabsf(m_run) > 0x1p20f))) {
+                l_run += sum;
+                return;
+            }
+        }
+        scale_scores(tile);
         uint32_t hidden = 0;
-        const bool all = gone == 0 && key0 + kTileKeys <= min(w_first + 1, walk.hi) && (p.window == 0 || key0 > w_last - p.window || key0 + kTileKeys <= p.sinks);
         if (!all) {
 #pragma unroll
             for (int kf = 0; kf < 2; ++kf)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int key = key0 + kf * 32 + 8 * (r >> 2) + 4 * lhi + (r & 3);
-                    const bool seen = (key <= place) & (key < walk.hi) & ((gone >> (kf * 2 + (r >> 3)) & 1) == 0) & ((key > reach) | (key < p.sinks));
+                    const bool seen = (key <= place) & (key < hi) & ((gone >> (kf * 2 + (r >> 3)) & 1) == 0) & ((key > reach) | (key < p.sinks));
                     st[kf][r] = seen ? st[kf][r] : -INFINITY;
                     hidden |= seen ? 0u : 1u << (16 * kf + r);
                 }
         }
-        // values' scales above the reference so far: the next power of two but one
-        const float4_t tm = *reinterpret_cast<const float4_t*>(tmax[buf]);
-        const float tx = fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3]));
-        if (tx > ldexpf(1.0f, t_exp)) {
-            const int e = min(static_cast<int>(__float_as_uint(tx) >> 23) - 127 + 2, 126);
-            const float beta = ldexpf(1.0f, t_exp - e);
-            m_run = m_run > kPagedNone ? m_run + static_cast<float>(e - t_exp) : m_run;
-            l_run *= beta;
+        float mx = -INFINITY;
 #pragma unroll
-            for (int f = 0; f < DF; ++f)
+        for (int kf = 0; kf < 2; ++kf)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[f][r] *= beta;
-            t_exp = e;
-        }
-        // Probabilities; the reference point stays as long as their sum over the lane's keys does not pass fp16's largest number, so each fits.
-        u32x4_t pf[4];
-        auto weigh = [&](float16_t* st) __attribute__((always_inline)) {
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int kf = 0; kf < 2; ++kf)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    const float4_t t4 = *reinterpret_cast<const float4_t*>(&ts[buf][32 * kf + 8 * q4 + 4 * lhi]);
-#pragma unroll
-                    for (int r = 0; r < 4; r += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(fmaf(st[kf][4 * q4 + r], up, -m_run)), p1 = __builtin_amdgcn_exp2f(fmaf(st[kf][4 * q4 + r + 1], up, -m_run));
-                        sum[q4] += p0 + p1;
-                        float w0 = p0 * t4[r], w1 = p1 * t4[r + 1];
-                        if (!all) {                              // (a scale that the column does not see may be NaN)
-                            w0 = hidden >> (16 * kf + 4 * q4 + r) & 1 ? 0.0f : w0;
-                            w1 = hidden >> (16 * kf + 4 * q4 + r + 1) & 1 ? 0.0f : w1;
-                        }
-                        uint32_t w = H::pack(w0, w1);
-                        asm("" : "+v"(w));
-                        pf[kf * 2 + (q4 >> 1)][2 * (q4 & 1) + (r >> 1)] = w;
-                    }
-                }
-            return (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        };
-        float sum = weigh(st);
-        if (__any(!(sum <= ldexpf(65504.0f, -t_exp)))) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int kf = 0; kf < 2; ++kf)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kf][r]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * up;
-            const float m_new = fmaxf(m_run, mx - (kChunkLift4 - static_cast<float>(t_exp))), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-            l_run *= alpha;
-#pragma unroll
-            for (int f = 0; f < DF; ++f)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[f][r] *= alpha;
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kf][r]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * up;
+        const float m_new = fmaxf(m_run, mx - (kChunkLift4 - static_cast<float>(t_exp)));
+        if (__any(m_new != m_run)) {
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
             m_run = m_new;
-            sum = weigh(st);
+            rescale(alpha);
         }
-        l_run += sum;
+        l_run += weigh<false>(tile, hidden);
+    }
+    __device__ __forceinline__ void rescale(float by) {
+        l_run *= by;
 #pragma unroll
-        for (int s2 = 0; s2 < 4; ++s2)
+        for (int f = 0; f < DF; ++f)
 #pragma unroll
-            for (int f = 0; f < DF; ++f) o[f] = H::mfma32(*reinterpret_cast<const u32x4_t*>(&Vs[buf][v_chunk(f, s2)]), pf[s2], o[f]);
+            for (int r = 0; r < 16; ++r) o[f][r] *= by;
+    }
+
+    // Results: to the output, or (SPLIT, several ranges) among the sums of range z.  (Odd columns' codes were times 16.)
+    template <bool SPLIT>
+    __device__ __forceinline__ void put(const PagedAttnDev& p, const SeqView& s, int z, int ranges) {
+        const int lhi = (threadIdx.x & 63) >> 5;
+        const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+        if (!mine) return;
+        if (SPLIT) {
+            float* dst = p.part + ((static_cast<size_t>(s.row0 + qi) * p.nh + head) * p.ranges + z) * part_stride(D);
+            if (lhi == 0) dst[D + 2] = static_cast<float>(ranges);
+            if (ranges > 1) {
+#pragma unroll
+                for (int f = 0; f < DF; ++f)
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4)
+                        *reinterpret_cast<float4_t*>(dst + f * 32 + 8 * q4 + 4 * lhi) =
+                            float4_t{o[f][4 * q4] * 0x1p24f, o[f][4 * q4 + 1] * 0x1p20f, o[f][4 * q4 + 2] * 0x1p24f, o[f][4 * q4 + 3] * 0x1p20f};
+                if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{m_run, l_tot};
+                return;
+            }
+        }
+        const float inv = l_tot != 0.0f ? 0x1p20f / l_tot : 0.0f;   // a row that sees no key is zero
+        uint16_t* orow = p.out + (s.row0 + qi) * p.out_stride + head * D;
+#pragma unroll
+        for (int f = 0; f < DF; ++f)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                u32x2_t w;
+                w[0] = Act16<BF16>::pack(o[f][4 * q4] * 16.0f * inv, o[f][4 * q4 + 1] * inv);
+                w[1] = Act16<BF16>::pack(o[f][4 * q4 + 2] * 16.0f * inv, o[f][4 * q4 + 3] * inv);
+                *reinterpret_cast<u32x2_t*>(orow + f * 32 + 8 * q4 + 4 * lhi) = w;
+            }
+    }
+};
+
+// The tiles of an item that this workgroup walks, and how many ranges the item has.
+struct Range4 { int t0, t1, ranges; };
+template <int PER>
+__device__ __forceinline__ Range4 range_of(const PagedAttnDev& p, int steps, int z) {
+    // ranges of about equal length over the whole call, as many as are to run at once; no item is cut into more than p.ranges
+    const int lane = threadIdx.x & 63;
+    int work = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) work += b0 + lane < p.B ? chunk_work<PER>(p, b0 + lane) : 0;
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) work += __shfl_xor(work, x, 64);
+    const int wanted = max(p.target / p.nkv, 1);
+    const int per = __builtin_amdgcn_readfirstlane(max(max((work + wanted - 1) / wanted, (steps + p.ranges - 1) / p.ranges), 4));
+    const int ranges = __builtin_amdgcn_readfirstlane(max((steps + per - 1) / per, 1));
+    return Range4{z * per, min(z * per + per, steps), ranges};
+}
+
+// Four waves, 128 columns.  Tile t + 1 is unpacked and tile t + 2 requested while tile t is computed; one barrier per tile, two workgroups per CU.
+template <int D, bool BF16, bool SPLIT>
+__global__ void __launch_bounds__(256, 2)
+paged4_chunk_kernel(PagedAttnDev p) {
+    using Cols = Columns4<D, BF16>;
+    constexpr int TILE = kTileKeys * D;
+    __shared__ __attribute__((aligned(1024))) uint16_t Ks[2][TILE], Vs[2][TILE];
+    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys], tmax[2][4];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    int hk, item, z = 0, b, qt;
+    find_head(p, &hk, &item);
+    if (SPLIT) {
+        z = __builtin_amdgcn_readfirstlane(item / p.items);
+        item -= z * p.items;
+    }
+    if (!find_columns<kChunkCols>(p, item, &b, &qt)) return;
+    SeqView s(p, b);
+    s.uniform();
+    const int c_lo = qt * kChunkCols, c_hi = min(c_lo + kChunkCols, s.n * p.rep) - 1;   // this workgroup's columns
+    const KeySteps<kTileKeys> walk(s.first + __builtin_amdgcn_readfirstlane(c_lo / p.rep), s.first + __builtin_amdgcn_readfirstlane(c_hi / p.rep), s.len, p.window, p.sinks);
+    Range4 range{0, walk.steps, 1};
+    if (SPLIT) range = range_of<kChunkCols>(p, walk.steps, z);
+    if (SPLIT && z >= range.ranges) return;
+    Cols cw(p, s, hk, c_lo + 32 * wave, c_hi);
+    const PageRow pages(p, s.slot);
+    Unpack4<D, BF16> un(p, hk, wave, walk.hi);
+    const int t0 = range.t0, t1 = range.t1;
+    auto tile = [&](int t) __attribute__((always_inline)) {
+        const int i = (t - t0) & 1;
+        return Tile4<D>{Ks[i], Vs[i], ks[i], ts[i], tmax[i]};
+    };
+    auto ids_of = [&](int t) __attribute__((always_inline)) { return tile_pages(pages, walk.key(min(t, walk.steps - 1)), wave); };
+    auto request = [&](int t, int page) __attribute__((always_inline)) {
+        if (t >= t1) page = -1;
+        un.request_keys(walk.key(t), page);
+        un.request_values(walk.key(t), page);
+    };
+    auto unpack = [&](int t) __attribute__((always_inline)) {
+        un.put_keys(walk.key(t), tile(t));
+        un.put_values(walk.key(t), tile(t));
     };
     if (t0 < t1) {
         // page ids are read a tile before the request that uses them
         TilePages i0 = ids_of(t0), i1 = ids_of(t0 + 1), i2 = ids_of(t0 + 2);
         request(t0, i0.page);
-        unpack(t0, 0);
+        unpack(t0);
         request(t0 + 1, i1.page);
         for (int t = t0; t < t1; ++t) {
-            const int buf = (t - t0) & 1;
             __syncthreads();                                     // tile t is in LDS, and the other buffers have been read
-            if (t + 1 < t1) unpack(t + 1, buf ^ 1);
+            if (t + 1 < t1) unpack(t + 1);
             request(t + 2, i2.page);
-            turn(t, i0.gone, buf);
+            const Tile4<D> now = tile(t);
+            cw.template products<Cols::PV, Cols::ALL>(now.V, now.K);
+            cw.softmax(p, now, walk.key(t), i0.gone, walk.hi);
+            cw.template products<0, Cols::PV>(now.V, now.K);
             i0 = i1;
             i1 = i2;
             i2 = ids_of(t + 3);
         }
     }
+    cw.template put<SPLIT>(p, s, z, range.ranges);
+}
 
-    const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-    if (!mine) return;
-    // (odd columns' codes were times 16)
+// Eight waves, 256 columns, one workgroup per CU, two waves per SIMD that take turns as in paged_wide_kernel: while the first half of the waves runs its
+// products (matrix cores, LDS), the second half runs its softmax and unpacks (vector ALUs), then they change places.
+//   phase      0         1             2             3             4
+//   half 0     S0, P0    O0, S1        P1, K2 in     O1, S2        P2, K3 in
+//   half 1     S0        P0, V1 in     O0, S1        P1, V2 in     O1, S2
+// "K2 in": keys of tile 2 go into LDS, in the place of tile 0's, which phase 0 was the last to read; V1 likewise.
+template <int D, bool BF16, bool SPLIT>
+__global__ void __launch_bounds__(512, 2)
+paged4_wide_kernel(PagedAttnDev p) {
+    using Cols = Columns4<D, BF16>;
+    constexpr int TILE = kTileKeys * D;
+    __shared__ __attribute__((aligned(1024))) uint16_t Ks[2][TILE], Vs[2][TILE];
+    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys], tmax[2][4];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    int hk, item, z = 0, b, qt;
+    find_head(p, &hk, &item);
     if (SPLIT) {
-        float* dst = p.part + ((static_cast<size_t>(s.row0 + qi) * p.nh + head) * p.ranges + z) * part_stride(D);
-        if (lhi == 0) dst[D + 2] = static_cast<float>(ranges);
-        if (ranges > 1) {
-#pragma unroll
-            for (int f = 0; f < DF; ++f)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4)
-                    *reinterpret_cast<float4_t*>(dst + f * 32 + 8 * q4 + 4 * lhi) = float4_t{o[f][4 * q4] * 0x1p24f, o[f][4 * q4 + 1] * 0x1p20f, o[f][4 * q4 + 2] * 0x1p24f, o[f][4 * q4 + 3] * 0x1p20f};
-            if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{m_run, l_tot};
-            return;
+        z = __builtin_amdgcn_readfirstlane(item / p.items);
+        item -= z * p.items;
+    }
+    if (!find_columns<kWideCols>(p, item, &b, &qt)) return;
+    SeqView s(p, b);
+    s.uniform();
+    const int c_lo = qt * kWideCols, c_hi = min(c_lo + kWideCols, s.n * p.rep) - 1;
+    const KeySteps<kTileKeys> walk(s.first + __builtin_amdgcn_readfirstlane(c_lo / p.rep), s.first + __builtin_amdgcn_readfirstlane(c_hi / p.rep), s.len, p.window, p.sinks);
+    Range4 range{0, walk.steps, 1};
+    if (SPLIT) range = range_of<kWideCols>(p, walk.steps, z);
+    if (SPLIT && z >= range.ranges) return;
+    Cols cw(p, s, hk, c_lo + 32 * wave, c_hi);
+    const PageRow pages(p, s.slot);
+    Unpack4<D, BF16> un(p, hk, wave & 3, walk.hi);
+    const int t0 = range.t0, n = range.t1 - range.t0;            // (tiles below are counted from t0)
+    auto tile = [&](int t) __attribute__((always_inline)) { return Tile4<D>{Ks[t & 1], Vs[t & 1], ks[t & 1], ts[t & 1], tmax[t & 1]}; };
+    auto key0 = [&](int t) __attribute__((always_inline)) { return walk.key(t0 + t); };
+    auto ids_of = [&](int t) __attribute__((always_inline)) { return tile_pages(pages, walk.key(min(t0 + t, walk.steps - 1)), wave & 3); };
+    // What a wave has written to LDS is there, and its reads have been consumed; requests of its own stay outstanding: a bare barrier that no access
+    // and no instruction is moved across.
+    auto phase_end = [&]() __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+    if (n > 0) {
+        TilePages i0 = ids_of(0), i1 = ids_of(1), i2 = ids_of(2);
+        if (wave < 4) {
+            un.request_keys(key0(0), i0.page);
+            un.put_keys(key0(0), tile(0));
+            un.request_keys(key0(1), 1 < n ? i1.page : -1);
+            un.put_keys(key0(1), tile(1));
+            un.request_keys(key0(2), 2 < n ? i2.page : -1);
+        } else {
+            un.request_values(key0(0), i0.page);
+            un.put_values(key0(0), tile(0));
+            un.request_values(key0(1), 1 < n ? i1.page : -1);
+        }
+        phase_end();
+        cw.template products<Cols::PV, Cols::ALL>(Vs[0], Ks[0]);
+        // (both halves walk the same barriers; past the last tile the scores are of whatever lies there, and not used)
+        auto turn = [&](int t) __attribute__((always_inline)) {
+            __builtin_amdgcn_s_setprio(1);
+            cw.template products<0, Cols::ALL>(Vs[t & 1], Ks[(t + 1) & 1]);
+            __builtin_amdgcn_s_setprio(0);
+            phase_end();
+        };
+        if (wave < 4) {
+            cw.softmax(p, tile(0), key0(0), i0.gone, walk.hi);
+            phase_end();
+            auto both = [&](int t) __attribute__((always_inline)) {
+                turn(t);
+                un.put_keys(key0(t + 2), tile(t));               // (of a tile past the last: zeros)
+                i0 = i1;
+                i1 = i2;
+                i2 = ids_of(t + 3);
+                un.request_keys(key0(t + 3), t + 3 < n ? i2.page : -1);
+                cw.softmax(p, tile(t + 1), key0(t + 1), t + 1 < n ? i0.gone : 15, walk.hi);
+                phase_end();
+            };
+            for (int t = 0; t < n; t += 2) {
+                both(t);
+                if (t + 1 < n) both(t + 1);
+            }
+        } else {
+            phase_end();
+            auto both = [&](int t) __attribute__((always_inline)) {
+                un.put_values(key0(t + 1), tile(t + 1));
+                un.request_values(key0(t + 2), t + 2 < n ? i2.page : -1);
+                cw.softmax(p, tile(t), key0(t), i0.gone, walk.hi);
+                i0 = i1;
+                i1 = i2;
+                i2 = ids_of(t + 3);
+                phase_end();
+                turn(t);
+            };
+            for (int t = 0; t < n; t += 2) {
+                both(t);
+                if (t + 1 < n) both(t + 1);
+            }
         }
     }
-    const float inv = l_tot != 0.0f ? 0x1p20f / l_tot : 0.0f;    // a row that sees no key is zero
-    uint16_t* orow = p.out + (s.row0 + qi) * p.out_stride + head * D;
-#pragma unroll
-    for (int f = 0; f < DF; ++f)
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-            u32x2_t w;
-            w[0] = Act16<BF16>::pack(o[f][4 * q4] * 16.0f * inv, o[f][4 * q4 + 1] * inv);
-            w[1] = Act16<BF16>::pack(o[f][4 * q4 + 2] * 16.0f * inv, o[f][4 * q4 + 3] * inv);
-            *reinterpret_cast<u32x2_t*>(orow + f * 32 + 8 * q4 + 4 * lhi) = w;
-        }
+    cw.template put<SPLIT>(p, s, z, range.ranges);
 }
 
 template <int D, bool BF16>
 static hipError_t chunk4_form(const PagedAttnDev& a, int groups, hipStream_t stream) {
     const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.items) * a.ranges * a.nkv));
-    if (groups == 0) hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, false, 8>), grid, dim3(512), 0, stream, a);
-    else if (a.ranges > 1) hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, true, 4>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, false, 4>), grid, dim3(256), 0, stream, a);
+    if (groups == 0) {
+        if (a.ranges > 1) hipLaunchKernelGGL((paged4_wide_kernel<D, BF16, true>), grid, dim3(512), 0, stream, a);
+        else hipLaunchKernelGGL((paged4_wide_kernel<D, BF16, false>), grid, dim3(512), 0, stream, a);
+    } else if (a.ranges > 1) {
+        hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, true>), grid, dim3(256), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, false>), grid, dim3(256), 0, stream, a);
+    }
     return hipGetLastError();
 }
 

@@ -196,7 +196,7 @@ int qtale_paged_attention(const qtale_paged_kv* kv, int layer, const qtale_paged
     const int64_t row = static_cast<int64_t>(attn->n_heads) * kv->head_dim;
     if ((e = check_rows(q, q_stride, row, 8)) || (e = check_rows(out, out_stride, row, 4))) return e;
     const PagedAttnBounds m = attn_bounds(attn, kv, T);
-    const PagedAttnPlan plan = plan_paged_attention(attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B, m.max_new, m.max_len, attn->window, attn->sinks);
+    const PagedAttnPlan plan = plan_paged_attention((kv->dtype & QTALE_KV_INT4) != 0, attn->n_heads, kv->n_kv_heads, kv->head_dim, T, B, m.max_new, m.max_len, attn->window, attn->sinks);
     if (plan.too_large) return QTALE_ERR_UNSUPPORTED;
     if ((e = check_workspace(workspace, workspace_bytes, plan.bytes))) return e;
     PagedAttnDev a = attn_device(kv, layer, attn, m, T);

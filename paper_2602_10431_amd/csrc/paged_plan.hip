@@ -24,7 +24,7 @@ static size_t decode_bytes(int nkv, int d, int B) {
     const size_t pieces = (static_cast<size_t>(std::min(B, kSpanSeqs)) * sizeof(int4) + 255) / 256 * 256;
     return pieces + static_cast<size_t>(decode_spans(nkv, d)) * nkv * 2 * kDecodeCols * part_stride(d) * 4;
 }
-PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks) {
+PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks) {
     PagedAttnPlan l{};
     const int rep = nh / nkv, cus = device_cus();
     const int64_t seen = window > 0 ? std::min<int64_t>(max_len, static_cast<int64_t>(window) + sinks + max_new) : max_len;   // keys of a sequence
@@ -54,7 +54,21 @@ PagedAttnPlan plan_paged_attention(int nh, int nkv, int d, int T, int B, int max
     if (l.decode && l.cols <= kDecodeCols && B <= kSpanSeqs && pairs < 2 * cus && scaled * (10 * filled - 9 * pairs) > 8000 * filled) l.spans = decode_spans(nkv, d);
     l.stream_keys = pairs >= 4 * cus;
     l.ranges = l.groups = 1;
-    if (l.chunk) {
+    if (l.chunk && q4) {
+        // (the wide form, one workgroup per CU)
+        const int64_t wide = (static_cast<int64_t>(T) * rep + static_cast<int64_t>(kWideCols - 1) * std::min(B, T)) / kWideCols, wide_wgs = std::max<int64_t>(wide * nkv, 1);
+        if (cols > kChunkCols) {
+            l.groups = 0;
+            items = wide;
+            if (tiles * (cus - wide_wgs) > 12 * cus) {
+                l.target = cus;
+                l.ranges = static_cast<int>(std::max<int64_t>(std::min<int64_t>({2 * ((cus + wide_wgs - 1) / wide_wgs), tiles / 8, 32}), 1));
+            }
+        } else if (cut) {
+            l.target = static_cast<int>(two);
+            l.ranges = static_cast<int>(std::max<int64_t>(std::min<int64_t>({2 * ((two + wgs - 1) / wgs), tiles / 8, 32}), 1));
+        }
+    } else if (l.chunk) {
         // Ranges for two workgroups per CU; else, where the tiles fill less than 7/8 of the CUs' places, two groups of waves per workgroup, which share a
         // tile's keys.  us, ranges / groups / neither: heads of 128, 4 per kv head, 500 rows on 24000 keys 218 / 393 / -, 2 x 300 on 2000
         // 59 / 61 / -, 1500 on 0 50 / 35 / 44, 1000 on 0 - / 23.6 / 27.3; heads of 64 2 x 700 on 1400 52 / 45 / 58, 1500 on 0 30 / 24 / 34; one

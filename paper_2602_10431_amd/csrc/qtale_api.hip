@@ -276,7 +276,7 @@ int paged_attention_block(qtale_ctx* ctx, const qtale_layer_cfg* c, const PagedC
     }
     Prof pr(ctx, stream, 5);
     const PagedAttnBounds m = attn_bounds(pc.attn, pc.kv, M_max);
-    const PagedAttnPlan plan = plan_paged_attention(nh, nkv, d, M_max, B, m.max_new, m.max_len, pc.attn->window, pc.attn->sinks);
+    const PagedAttnPlan plan = plan_paged_attention(pc.cache.q4, nh, nkv, d, M_max, B, m.max_new, m.max_len, pc.attn->window, pc.attn->sinks);
     if (plan.too_large) return QTALE_ERR_UNSUPPORTED;
     PagedAttnDev a = attn_device(pc.kv, pc.layer, pc.attn, m, M_max);
     a.q = qkv; a.q_stride = width; a.out = reinterpret_cast<uint16_t*>(ws.attn); a.out_stride = nh * d;
