@@ -22,16 +22,16 @@ struct LoraRows {
 };
 constexpr int kLoraMost = 3;     // linears with the same input that one launch takes
 
-int lora_splits(int M);                          // parts that the sums over K may be cut into
-size_t lora_inner_bytes(int R, int M);           // of one linear's inner values, [parts][rows][R] fp32, for up to M rows
+size_t lora_inner_bytes(int R, int M);           // of one linear's inner values, for up to M rows
 
-// inner = down_a A_i of every row, in parts over K, for `n` linears of one input [M][K]; what belongs to no adapter, or lies past a rank, is not written.
-// *parts (host out): of each linear
-hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, const void* A, float* const* inner, int* parts, hipStream_t stream);
+// inner = down_a A_i of every row, for `n` linears of one input [M][K]: in parts over K for the calls below, or, of many rows, their sums as the second
+// product's operands.  What belongs to no adapter, or lies past a rank, is not written.  *operands, *parts (host out): of each linear, for the calls below
+hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, const void* A, float* const* inner, const float** operands, int* parts,
+                             hipStream_t stream);
 // out (fp16, or fp32 if f32; ldo elements between rows) += scale up_a inner_i
-hipError_t launch_lora_add(const LoraDev& l, const LoraRows& rows, const float* inner, int parts, void* out, int ldo, int f32, hipStream_t stream);
+hipError_t launch_lora_add(const LoraDev& l, const LoraRows& rows, const float* operands, int parts, void* out, int ldo, int f32, hipStream_t stream);
 // out [M][N] = silu(gate + ...) * (up + ...); base [M][2 N] fp16: gate's columns, then up's
-hipError_t launch_lora_swiglu(const LoraDev& lg, const LoraDev& lu, const LoraRows& rows, const float* inner_g, const float* inner_u, int parts_g, int parts_u,
-                              const void* base, void* out, int N, hipStream_t stream);
+hipError_t launch_lora_swiglu(const LoraDev& lg, const LoraDev& lu, const LoraRows& rows, const float* operands_g, const float* operands_u, int parts_g,
+                              int parts_u, const void* base, void* out, int N, hipStream_t stream);
 
 }  // namespace qtale

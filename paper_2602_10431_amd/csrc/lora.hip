@@ -16,17 +16,18 @@ namespace qtale {
 
 __device__ __forceinline__ float4_t mfma(const half8_t& a, const half8_t& b, const float4_t& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// Adapter of row i (the lane's): -1 for none.
-__device__ __forceinline__ int adapter_of(const LoraDev& l, const LoraRows& rows, int i, int M) {
+// Number that row i (the lane's) chooses its adapters by: -1 for none.
+__device__ __forceinline__ int choice_of(const LoraRows& rows, int i, int M) {
     if (i >= M) return -1;
     int seq = i;
     if (rows.row_seq) {
         seq = rows.row_seq[i];
         if (static_cast<uint32_t>(seq) >= static_cast<uint32_t>(rows.n_seq)) return -1;
     }
-    const int a = rows.adapter[seq];
-    return static_cast<uint32_t>(a) < static_cast<uint32_t>(l.n) ? a : -1;
+    return max(rows.adapter[seq], -1);
 }
+// ... which a linear may have an adapter for or not
+__device__ __forceinline__ int adapter_of(const LoraDev& l, int choice) { return static_cast<uint32_t>(choice) < static_cast<uint32_t>(l.n) ? choice : -1; }
 __device__ __forceinline__ int rank_of(const LoraDev& l, int a) { return l.rank ? min(max(l.rank[a], 0), l.R) : l.R; }
 
 // As the shared product's results: saturating; a NaN stays one.
@@ -40,9 +41,10 @@ struct LoraInner {
     int parts;
 };
 
-// One workgroup per (16 RT rows, part of K[, adapter of the tile]); NR tiles of 16 inner values.  ALONE: each adapter of the tile has its own workgroup.
-template <int RT, int NR, bool ALONE>
-__global__ void __launch_bounds__(256)
+// One workgroup of NW waves per (16 RT rows, part of K[, adapter of the tile]); NR tiles of 16 inner values.  ALONE: each adapter of the tile has its own
+// workgroup.
+template <int RT, int NR, int NW, bool ALONE>
+__global__ void __launch_bounds__(64 * NW)
 lora_inner_kernel(LoraInner p) {
     const LoraDev& l = p.l[blockIdx.z];
     const int M = p.rows.count ? min(*p.rows.count, p.rows.M) : p.rows.M;
@@ -50,14 +52,14 @@ lora_inner_kernel(LoraInner p) {
     if (row0 >= M) return;
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    __shared__ float4_t sums[3][RT * NR][64];
-    const int mine = adapter_of(l, p.rows, row0 + lane, lane < 16 * RT ? M : 0);   // lane x: row x of the tile
+    __shared__ float4_t sums[NW - 1][RT * NR][64];
+    const int mine = adapter_of(l, choice_of(p.rows, row0 + lane, lane < 16 * RT ? M : 0));   // lane x: row x of the tile
     int own[RT];                                                 // this lane's columns: rows c, 16 + c, ...
 #pragma unroll
     for (int t = 0; t < RT; ++t) own[t] = __shfl(mine, 16 * t + c, 64);
     uint64_t left = __ballot(mine >= 0);
     int skip = ALONE ? blockIdx.y & 15 : 0;
-    const int units = (l.K + 127) / 128, step = 4 * p.parts;     // units of 128 columns of K: this wave's are part * 4 + wave, + step, ...
+    const int units = (l.K + 127) / 128, step = NW * p.parts;    // units of 128 columns of K: this wave's are part * NW + wave, + step, ...
     const size_t stride = static_cast<size_t>(p.rows.M) * l.R;
     const uint16_t* rows_at[RT];
 #pragma unroll
@@ -73,7 +75,7 @@ lora_inner_kernel(LoraInner p) {
         for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int r = 0; r < NR; ++r) acc[t][r] = float4_t{0.f, 0.f, 0.f, 0.f};
-        for (int u = part * 4 + wave; u < units; u += step) {
+        for (int u = part * NW + wave; u < units; u += step) {
             half8_t x[4][RT], w[4][NR];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -97,7 +99,7 @@ lora_inner_kernel(LoraInner p) {
 #pragma unroll
                     for (int r = 0; r < NR; ++r) acc[t][r] = mfma(w[j][r], x[j][t], acc[t][r]);
         }
-        // the four waves meet in LDS; the first writes
+        // the waves meet in LDS; the first writes
         if (wave > 0) {
 #pragma unroll
             for (int t = 0; t < RT; ++t)
@@ -110,7 +112,9 @@ lora_inner_kernel(LoraInner p) {
             for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int r = 0; r < NR; ++r) {
-                    const float4_t y = (acc[t][r] + sums[0][t * NR + r][lane]) + (sums[1][t * NR + r][lane] + sums[2][t * NR + r][lane]);
+                    float4_t y = acc[t][r];
+#pragma unroll
+                    for (int w = 0; w < NW - 1; ++w) y += sums[w][t * NR + r][lane];
                     // lane (c, g): row c, inner values 16 r + 4 g .. + 3 (R is a multiple of 8)
                     if (own[t] == a && 16 * r + 4 * g < rank)
                         *reinterpret_cast<float4_t*>(p.inner[blockIdx.z] + part * stride + static_cast<size_t>(row0 + 16 * t + c) * l.R + 16 * r + 4 * g) = y;
@@ -121,30 +125,41 @@ lora_inner_kernel(LoraInner p) {
     }
 }
 
-// Inner values of this lane's row as operands: k-step s has values 32 s + 8 g ..; *unit: what a unit of the products stands for.
+// Inner values of this lane's row (one that there is) as operands, zeros from `rank` on: k-step s has values 32 s + 8 g ..; returns the power of two that a
+// unit of the products stands for.  All loads go out together and without a branch: what is not wanted is loaded from a place that is there.
 template <int NS>
-__device__ __forceinline__ void inner_operand(const LoraDev& l, int a, const float* inner, int parts, size_t stride, int row, int g, half8_t* x, float* unit) {
+__device__ __forceinline__ float inner_operand(const LoraDev& l, int rank, const float* inner, int parts, size_t stride, int row, int g, half8_t* x) {
+    constexpr int AT_ONCE = NS == 1 ? 4 : 2;
     float v[NS][8], big = 0.0f;
-    const int rank = a >= 0 ? rank_of(l, a) : 0;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        const int r0 = 32 * s + 8 * g;
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[s][e] = 0.0f;
-        if (r0 < rank) {
-            const float* at = inner + static_cast<size_t>(row) * l.R + r0;
-            for (int z = 0; z < parts; ++z) {
-                const float4_t y0 = *reinterpret_cast<const float4_t*>(at + z * stride), y1 = *reinterpret_cast<const float4_t*>(at + z * stride + 4);
+    const float* at = inner + static_cast<size_t>(row) * l.R;
+    for (int z0 = 0; z0 < parts; z0 += AT_ONCE) {
+        float4_t y[AT_ONCE][NS][2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { v[s][e] += y0[e]; v[s][4 + e] += y1[e]; }
+        for (int z = 0; z < AT_ONCE; ++z)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const float* from = at + min(z0 + z, parts - 1) * stride + min(32 * s + 8 * g, l.R - 8);
+                y[z][s][0] = *reinterpret_cast<const float4_t*>(from);
+                y[z][s][1] = *reinterpret_cast<const float4_t*>(from + 4);
             }
-        }
+#pragma unroll
+        for (int z = 0; z < AT_ONCE; ++z)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[s][e] += z0 + z < parts ? y[z][s][e >> 2][e & 3] : 0.0f;
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[s][e] = r0 + e < rank ? v[s][e] : 0.0f;
+            v[s][e] = 32 * s + 8 * g + e < rank ? v[s][e] : 0.0f;
             big = fmaxf(big, fabsf(v[s][e]));
         }
-    }
     big = fmaxf(big, __shfl_xor(big, 16, 64));
     big = fmaxf(big, __shfl_xor(big, 32, 64));
     const int e = min(max(static_cast<int>(__float_as_uint(big) >> 23) - 127, -100), 127);
@@ -153,43 +168,57 @@ __device__ __forceinline__ void inner_operand(const LoraDev& l, int a, const flo
     for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[s][i] = static_cast<half_t>(v[s][i] * f);
-    *unit = a >= 0 ? ldexpf(l.scale ? l.scale[a] : 1.0f, e - 12) : 0.0f;
+    return ldexpf(1.0f, e - 12);
 }
+__device__ __forceinline__ float scale_of(const LoraDev& l, int a) { return l.scale ? l.scale[a] : 1.0f; }
 
-// y[j] = up_a inner of columns n0 + 16 j + 4 g .. + 3 and the lane's row, for the rows' own adapters (0 for those without); left: rows that have one.
-template <int NS, int NT>
-__device__ __forceinline__ void outer_product(const LoraDev& l, uint64_t left, int mine, int own, const half8_t* x, int n0, float4_t* y) {
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+// Many rows: the parts' sums as operands, once: [M][32 NS] fp16 relative to the row's power of two, zeros from its adapter's rank on, then [M] of what a
+// unit of the products stands for (0 for a row without an adapter).
+struct LoraPack {
+    LoraDev l[kLoraMost];
+    float* inner[kLoraMost];
+    uint16_t* out[kLoraMost];
+    LoraRows rows;
+    int parts;
+};
+__host__ __device__ inline int operand_width(int R) { return R <= 32 ? 32 : R <= 64 ? 64 : 128; }
+__device__ __forceinline__ const float* operand_units(const uint16_t* operands, int R, int M) { return reinterpret_cast<const float*>(operands + static_cast<size_t>(M) * operand_width(R)); }
+
+__global__ void __launch_bounds__(256)
+lora_pack_kernel(LoraPack p) {
+    const LoraDev& l = p.l[blockIdx.y];
+    const int M = p.rows.count ? min(*p.rows.count, p.rows.M) : p.rows.M;
+    const int row = blockIdx.x * 16 + (threadIdx.x >> 4), r0 = 8 * (threadIdx.x & 15), at_row = min(row, M - 1);
+    const size_t stride = static_cast<size_t>(p.rows.M) * l.R;
+    const float* from = p.inner[blockIdx.y] + static_cast<size_t>(at_row) * l.R + min(r0, l.R - 8);
+    float4_t y[8][2];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) y[j] = float4_t{0.f, 0.f, 0.f, 0.f};
-    while (left != 0) {
-        const int a = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(left)) - 1));
-        left &= ~__ballot(mine == a);
-        const int rank = rank_of(l, a);
-        half8_t w[NT][NS];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const uint16_t* at = l.up + (static_cast<size_t>(a) * l.N + min(n0 + 16 * j + c, l.N - 1)) * l.R;
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const int r0 = 32 * s + 8 * g;
-                w[j][s] = half8_t{};
-                if (r0 < rank) w[j][s] = *reinterpret_cast<const half8_t*>(at + r0);
-                if (r0 + 8 > rank && r0 < rank) {                // what lies past the rank may be anything
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[j][s][e] = r0 + e < rank ? w[j][s][e] : static_cast<half_t>(0.0f);
-                }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            float4_t d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < NS; ++s) d = mfma(w[j][s], x[s], d);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[j][r] = own == a ? d[r] : y[j][r];
-        }
+    for (int z = 0; z < 8; ++z) {
+        y[z][0] = *reinterpret_cast<const float4_t*>(from + min(z, p.parts - 1) * stride);
+        y[z][1] = *reinterpret_cast<const float4_t*>(from + min(z, p.parts - 1) * stride + 4);
     }
+    const int a = adapter_of(l, choice_of(p.rows, at_row, M));
+    const int rank = a >= 0 ? rank_of(l, a) : 0;
+    float v[8], big = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] = 0.0f;
+#pragma unroll
+        for (int z = 0; z < 8; ++z) v[e] += z < p.parts ? y[z][e >> 2][e & 3] : 0.0f;
+        v[e] = r0 + e < rank ? v[e] : 0.0f;
+        big = fmaxf(big, fabsf(v[e]));
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
+    if (row >= M) return;
+    const int e = min(max(static_cast<int>(__float_as_uint(big) >> 23) - 127, -100), 127), width = operand_width(l.R);
+    const float f = ldexpf(1.0f, 12 - e);
+    half8_t x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = static_cast<half_t>(v[i] * f);
+    uint16_t* out = p.out[blockIdx.y];
+    if (r0 < width) *reinterpret_cast<half8_t*>(out + static_cast<size_t>(row) * width + r0) = x;
+    if (r0 == 0) const_cast<float*>(operand_units(out, l.R, p.rows.M))[row] = a >= 0 ? ldexpf(scale_of(l, a), e - 12) : 0.0f;
 }
 
 struct LoraOuter {
@@ -202,91 +231,245 @@ struct LoraOuter {
     int ldo;
 };
 enum { LORA_ADD_F16, LORA_ADD_F32, LORA_SWIGLU };
-constexpr int kOuterTiles = 4;   // of 16 columns per wave
 
-// One wave per 16 rows x 64 columns.
-template <int NS, int FORM>
+// up_a of columns n .. n + 15 (lane c: column n + c), k-step s: inner values 32 s + 8 g ..
+template <int NS>
+__device__ __forceinline__ void up_operand(const LoraDev& l, int a, int n, u32x4_t* w) {
+    const int c = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    const uint16_t* at = l.up + (static_cast<size_t>(a) * l.N + min(n + c, l.N - 1)) * l.R;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) w[s] = *reinterpret_cast<const u32x4_t*>(at + min(32 * s + 8 * g, l.R - 8));
+}
+// What lies past the rank may be anything: bits of this lane's operands that stay.
+template <int NS>
+__device__ __forceinline__ void rank_mask(int rank, u32x4_t* mask) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mask[s][e] = (32 * s + 8 * g + 2 * e < rank ? 0xffffu : 0u) | (32 * s + 8 * g + 2 * e + 1 < rank ? 0xffff0000u : 0u);
+}
+template <int NS>
+__device__ __forceinline__ float4_t outer_product(const u32x4_t* w, const u32x4_t* mask, const half8_t* x) {
+    float4_t y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < NS; ++s) y = mfma(__builtin_bit_cast(half8_t, w[s] & mask[s]), x[s], y);
+    return y;
+}
+
+// Four values of a row: what is there and what is added.
+template <int FORM> struct OuterRow;
+template <> struct OuterRow<LORA_ADD_F32> {
+    float4_t old;
+    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) { old = *reinterpret_cast<const float4_t*>(static_cast<const float*>(p.out) + row * p.ldo + n); }
+    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t& y, const float4_t&) const { *reinterpret_cast<float4_t*>(static_cast<float*>(p.out) + row * p.ldo + n) = old + y; }
+};
+__device__ __forceinline__ float half_of(const U2& w, int r) { return half_bits_to_float(static_cast<uint16_t>((r < 2 ? w.x : w.y) >> (16 * (r & 1)) & 0xffffu)); }
+__device__ __forceinline__ U2 halves(const float4_t& y) {
+    return U2{to_half(y[0]) | static_cast<uint32_t>(to_half(y[1])) << 16, to_half(y[2]) | static_cast<uint32_t>(to_half(y[3])) << 16};
+}
+template <> struct OuterRow<LORA_ADD_F16> {
+    U2 old;
+    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) { old = *reinterpret_cast<const U2*>(static_cast<const uint16_t*>(p.out) + row * p.ldo + n); }
+    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t& y, const float4_t&) const {
+        float4_t sum;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] = half_of(old, r) + y[r];
+        *reinterpret_cast<U2*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(sum);
+    }
+};
+template <> struct OuterRow<LORA_SWIGLU> {
+    U2 gate, up;
+    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int N) {
+        const uint16_t* from = p.base + row * 2 * N + n;
+        gate = *reinterpret_cast<const U2*>(from);
+        up = *reinterpret_cast<const U2*>(from + N);
+    }
+    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t& yg, const float4_t& yu) const {
+        float4_t out;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float x = half_of(gate, r) + yg[r];
+            out[r] = x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)) * (half_of(up, r) + yu[r]);   // (off by 2^-22 or so)
+        }
+        *reinterpret_cast<U2*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(out);
+    }
+};
+
+// Few rows, which mostly choose differently: a workgroup per (16 rows, 256 NT columns, number that some of the rows choose by), which writes those rows.
+// The rows' operands are made once, by a wave per linear, in LDS; a wave's first columns are on their way meanwhile.
+template <int NS, int FORM, int NT>
 __global__ void __launch_bounds__(256)
-lora_outer_kernel(LoraOuter p) {
-    constexpr int NT = kOuterTiles, NL = FORM == LORA_SWIGLU ? 2 : 1;
+lora_few_kernel(LoraOuter p, int steps) {
+    constexpr int NL = FORM == LORA_SWIGLU ? 2 : 1;
     const int M = p.rows.count ? min(*p.rows.count, p.rows.M) : p.rows.M;
     const int row0 = blockIdx.x * 16, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int N = FORM == LORA_SWIGLU ? p.ldo : p.l[0].N, n0 = (blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * (16 * NT);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int N = FORM == LORA_SWIGLU ? p.ldo : p.l[0].N;
+    if (row0 >= M) return;
+    __shared__ half8_t operands[NL][NS][64];
+    __shared__ float units[NL][16];
+    const int mine = choice_of(p.rows, row0 + lane, lane < 16 ? M : 0);   // lane x: row x of the tile
+    // rows that there are (and have something to add, where nothing else is done), then those of the blockIdx.z-th choice
+    uint64_t rows = __ballot(lane < 16 && row0 + lane < M && (FORM == LORA_SWIGLU || adapter_of(p.l[0], mine) >= 0));
+    int choice = -1;
+    for (int skip = blockIdx.z; rows != 0; --skip) {
+        choice = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(rows)) - 1));
+        const uint64_t same = __ballot(mine == choice) & rows;
+        if (skip == 0) { rows = same; break; }
+        rows &= ~same;
+    }
+    if (rows == 0) return;                                       // (the same in all waves)
+    const bool own = (rows >> c & 1) != 0;
+    const size_t row = row0 + c;
+    int a[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) a[i] = adapter_of(p.l[i], choice);
+    u32x4_t w[NL][NT][NS];
+    OuterRow<FORM> there[NT];
+    auto fetch = [&](int n0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            if (a[i] < 0) continue;                              // (the same in all lanes)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) up_operand<NS>(p.l[i], a[i], n0 + 16 * j, w[i][j]);
+        }
+        if (own) {                                               // (N is a multiple of 8)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) there[j].read(p, row, min(n0 + 16 * j + 4 * g, N - 4), N);
+        }
+    };
+    int n0 = (blockIdx.y * steps * 4 + wave) * (16 * NT);
+    fetch(n0);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        if (wave != i || a[i] < 0) continue;
+        half8_t x[NS];
+        const float unit = inner_operand<NS>(p.l[i], rank_of(p.l[i], a[i]), p.inner[i], p.parts[i], static_cast<size_t>(p.rows.M) * p.l[i].R, min(row0 + c, M - 1), g, x);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) operands[i][s][lane] = x[s];
+        if (g == 0) units[i][c] = unit * scale_of(p.l[i], a[i]);
+    }
+    u32x4_t mask[NL][NS];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) rank_mask<NS>(a[i] >= 0 ? rank_of(p.l[i], a[i]) : 0, mask[i]);
+    __syncthreads();
+    half8_t x[NL][NS];
+    float unit[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) x[i][s] = operands[i][s][lane];
+        unit[i] = units[i][c];
+    }
+#pragma unroll 1
+    for (int step = 0; step < steps && n0 < N; ++step, n0 += 64 * NT) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float4_t y[NL];
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                y[i] = float4_t{0.f, 0.f, 0.f, 0.f};
+                if (a[i] >= 0) y[i] = outer_product<NS>(w[i][j], mask[i], x[i]) * unit[i];
+            }
+            if (own && n0 + 16 * j + 4 * g < N) there[j].write(p, row, n0 + 16 * j + 4 * g, y[0], y[NL - 1]);
+        }
+        if (step + 1 < steps) fetch(n0 + 64 * NT);
+    }
+}
+
+// Many rows, operands made (lora_pack_kernel): a wave per 16 rows and 64 columns, which walks the adapters that the rows have, mostly one; the first one's
+// are on their way with everything else that the wave reads.
+template <int NS, int FORM>
+__global__ void __launch_bounds__(256)
+lora_many_kernel(LoraOuter p) {
+    constexpr int NT = NS == 4 ? 2 : 4, NL = FORM == LORA_SWIGLU ? 2 : 1;
+    const int M = p.rows.count ? min(*p.rows.count, p.rows.M) : p.rows.M;
+    // Workgroups go round-robin to the 8 XCDs: each has its own blocks of columns, whose part of up its L2 holds for all tiles of rows.
+    const int tiles = (p.rows.M + 15) / 16, local = blockIdx.x >> 3, block = local / tiles * 8 + (blockIdx.x & 7);
+    const int row0 = (local % tiles) * 16, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int N = FORM == LORA_SWIGLU ? p.ldo : p.l[0].N, n0 = (block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * (16 * NT);
     if (row0 >= M || n0 >= N) return;
-    const int row = row0 + c;
+    const size_t row = min(row0 + c, M - 1);
+    const int mine = choice_of(p.rows, row0 + lane, lane < 16 ? M : 0);   // lane x: row x of the tile
+    half8_t x[NL][NS];
+    float unit[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        if (p.l[i].n == 0) continue;
+        const uint16_t* operands = reinterpret_cast<const uint16_t*>(p.inner[i]);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) x[i][s] = *reinterpret_cast<const half8_t*>(operands + row * operand_width(p.l[i].R) + min(32 * s + 8 * g, operand_width(p.l[i].R) - 8));
+        unit[i] = operand_units(operands, p.l[i].R, p.rows.M)[row];
+    }
+    OuterRow<FORM> there[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) there[j].read(p, row, min(n0 + 16 * j + 4 * g, N - 4), N);   // (N is a multiple of 8)
+    const int choice = __shfl(mine, c, 64);                      // of this lane's row
+    const uint64_t rows = __ballot(lane < 16 && row0 + lane < M && (FORM == LORA_SWIGLU || adapter_of(p.l[0], mine) >= 0));
     float4_t y[NL][NT];
-    bool has = FORM == LORA_SWIGLU;                              // whether the lane's row is written
+    u32x4_t w[NL][NT][NS];
+    uint64_t left[NL];
+    int a[NL];
+    auto next = [&](int i) __attribute__((always_inline)) {      // the next adapter that a row has, its part of up
+        a[i] = -1;
+        if (left[i] == 0) return;
+        a[i] = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(left[i])) - 1));
+        left[i] &= ~__ballot(mine == a[i]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) up_operand<NS>(p.l[i], a[i], n0 + 16 * j, w[i][j]);
+    };
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        left[i] = rows & __ballot(adapter_of(p.l[i], mine) >= 0);
+        next(i);
+    }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) y[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
-        const LoraDev& l = p.l[i];
-        if (l.n == 0) continue;
-        const int mine = adapter_of(l, p.rows, row0 + lane, lane < 16 ? M : 0), own = __shfl(mine, c, 64);
-        const uint64_t left = __ballot(mine >= 0);
-        if (left == 0) continue;
-        has |= own >= 0;
-        half8_t x[NS];
-        float unit;
-        inner_operand<NS>(l, own, p.inner[i], p.parts[i], static_cast<size_t>(p.rows.M) * l.R, row, g, x, &unit);
-        outer_product<NS, NT>(l, left, mine, own, x, n0, y[i]);
+        while (a[i] >= 0) {
+            u32x4_t mask[NS];
+            rank_mask<NS>(rank_of(p.l[i], a[i]), mask);
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+            for (int j = 0; j < NT; ++j) {
+                const float4_t d = outer_product<NS>(w[i][j], mask, x[i]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[i][j][r] = own >= 0 ? y[i][j][r] * unit : 0.0f;
-    }
-    if (row >= M || !has) return;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int n = n0 + 16 * j + 4 * g;
-        if (n >= N) continue;                                    // (N is a multiple of 8)
-        const size_t at = static_cast<size_t>(row) * p.ldo + n;
-        if (FORM == LORA_ADD_F32) {
-            float4_t* to = reinterpret_cast<float4_t*>(static_cast<float*>(p.out) + at);
-            *to = *to + y[0][j];
-        } else if (FORM == LORA_ADD_F16) {
-            U2* to = reinterpret_cast<U2*>(static_cast<uint16_t*>(p.out) + at);
-            const U2 b = *to;
-            const uint32_t w[2] = {b.x, b.y};
-            uint16_t h[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) h[r] = to_half(half_bits_to_float(static_cast<uint16_t>(w[r >> 1] >> (16 * (r & 1)) & 0xffffu)) + y[0][j][r]);
-            *to = U2{h[0] | static_cast<uint32_t>(h[1]) << 16, h[2] | static_cast<uint32_t>(h[3]) << 16};
-        } else {
-            const uint16_t* from = p.base + static_cast<size_t>(row) * 2 * N + n;
-            const U2 bg = *reinterpret_cast<const U2*>(from), bu = *reinterpret_cast<const U2*>(from + N);
-            const uint32_t wg[2] = {bg.x, bg.y}, wu[2] = {bu.x, bu.y};
-            uint16_t h[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float gate = half_bits_to_float(static_cast<uint16_t>(wg[r >> 1] >> (16 * (r & 1)) & 0xffffu)) + y[0][j][r];
-                const float up = half_bits_to_float(static_cast<uint16_t>(wu[r >> 1] >> (16 * (r & 1)) & 0xffffu)) + y[NL - 1][j][r];
-                h[r] = to_half(gate / (1.0f + __expf(-gate)) * up);
+                for (int r = 0; r < 4; ++r) y[i][j][r] = choice == a[i] ? d[r] * unit[i] : y[i][j][r];
             }
-            *reinterpret_cast<U2*>(static_cast<uint16_t*>(p.out) + at) = U2{h[0] | static_cast<uint32_t>(h[1]) << 16, h[2] | static_cast<uint32_t>(h[3]) << 16};
+            next(i);
         }
     }
+    if ((rows >> c & 1) == 0) return;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+        if (n0 + 16 * j + 4 * g < N) there[j].write(p, row, n0 + 16 * j + 4 * g, y[0][j], y[NL - 1][j]);
 }
 
-// Parts of K that fill the chip: tiles of 64 rows, three workgroups per CU.
-constexpr int kInnerFill = 768;
-int lora_splits(int M) { return std::min(std::max((kInnerFill * 64 + M - 1) / std::max(M, 1), 1), 8); }
+constexpr int kLoraAlone = 256;  // rows up to which they are taken to choose differently
+
+// Parts of K: workgroups that fill the chip, each wave with a unit of 128 columns at least.
+constexpr int kManyFill = 512;
+static int inner_tile(int M) { return M <= 2048 ? 16 : 64; }
+static int inner_parts(int M, int K, int n) {
+    const int units = (K + 127) / 128;
+    if (M <= kLoraAlone) return std::min(std::max(units / 8, 1), 4);
+    const int wgs = (M + inner_tile(M) - 1) / inner_tile(M) * n;
+    return std::min(std::min((kManyFill + wgs - 1) / wgs, 8), std::max(units / 4, 1));
+}
 size_t lora_inner_bytes(int R, int M) {
-    // enough for any number of rows up to M: parts * M <= 8 M, and <= 64 * kInnerFill + M
-    const size_t rows = std::min<size_t>(static_cast<size_t>(8) * M, static_cast<size_t>(kInnerFill) * 64 + M);
-    return (rows * R * 4 + 255) / 256 * 256;
+    // enough for any number of rows up to M: parts * M <= 8 M, and <= 64 kManyFill + M
+    const size_t rows = std::min<size_t>(static_cast<size_t>(8) * M, static_cast<size_t>(kManyFill) * 64 + M);
+    return (rows * R * 4 + 255) / 256 * 256 + (static_cast<size_t>(M) * (2 * operand_width(R) + 4) + 255) / 256 * 256;
 }
 
-template <int RT, bool ALONE>
-static void inner_form(const LoraInner& p, int R, dim3 grid, hipStream_t stream) {
-    if (R <= 16) hipLaunchKernelGGL((lora_inner_kernel<RT, 1, ALONE>), grid, dim3(256), 0, stream, p);
-    else if (R <= 32) hipLaunchKernelGGL((lora_inner_kernel<RT, 2, ALONE>), grid, dim3(256), 0, stream, p);
-    else if (R <= 64) hipLaunchKernelGGL((lora_inner_kernel<RT, 4, ALONE>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((lora_inner_kernel<RT, 8, ALONE>), grid, dim3(256), 0, stream, p);
+template <int RT, int NR, int NW, bool ALONE>
+static void inner_launch(const LoraInner& p, int tiles, int n, hipStream_t stream) {
+    hipLaunchKernelGGL((lora_inner_kernel<RT, NR, NW, ALONE>), dim3(tiles, (ALONE ? 16 : 1) * p.parts, n), dim3(64 * NW), 0, stream, p);
 }
 
-hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, const void* A, float* const* inner, int* parts, hipStream_t stream) {
-    if (rows.M <= 0 || n <= 0) return hipSuccess;
+hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, const void* A, float* const* inner, const float** operands, int* parts,
+                             hipStream_t stream) {
     LoraInner p{};
     int R = 0;
     for (int i = 0; i < n; ++i) {
@@ -295,21 +478,61 @@ hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, cons
         R = std::max(R, l[i].R);
     }
     p.rows = rows; p.A = static_cast<const uint16_t*>(A);
-    p.parts = std::max(1, std::min(lora_splits(rows.M), (l[0].K + 511) / 512));
+    p.parts = inner_parts(rows.M, l[0].K, n);
     for (int i = 0; i < n; ++i) parts[i] = p.parts;
-    // Few rows, whose adapters mostly differ: a workgroup per adapter of the tile.  Many: a tile's adapters one after the other, mostly one.
-    if (rows.M <= 256) inner_form<1, true>(p, R, dim3((rows.M + 15) / 16, 16 * p.parts, n), stream);
-    else inner_form<4, false>(p, R, dim3((rows.M + 63) / 64, p.parts, n), stream);
+    // Few rows, whose adapters mostly differ: a workgroup per adapter of the tile.  Many: a tile's adapters one after the
+    // other, mostly one.
+    const int tile = inner_tile(rows.M), tiles = (rows.M + tile - 1) / tile;
+    if (rows.M <= kLoraAlone) {
+        if (R <= 16) inner_launch<1, 1, 8, true>(p, tiles, n, stream);
+        else if (R <= 32) inner_launch<1, 2, 8, true>(p, tiles, n, stream);
+        else if (R <= 64) inner_launch<1, 4, 8, true>(p, tiles, n, stream);
+        else inner_launch<1, 8, 8, true>(p, tiles, n, stream);
+    } else if (tile == 16) {
+        if (R <= 16) inner_launch<1, 1, 4, false>(p, tiles, n, stream);
+        else if (R <= 32) inner_launch<1, 2, 4, false>(p, tiles, n, stream);
+        else if (R <= 64) inner_launch<1, 4, 4, false>(p, tiles, n, stream);
+        else inner_launch<1, 8, 4, false>(p, tiles, n, stream);
+    } else {
+        if (R <= 16) inner_launch<4, 1, 4, false>(p, tiles, n, stream);
+        else if (R <= 32) inner_launch<4, 2, 4, false>(p, tiles, n, stream);
+        else if (R <= 64) inner_launch<4, 4, 4, false>(p, tiles, n, stream);
+        else inner_launch<4, 8, 4, false>(p, tiles, n, stream);
+    }
+    if (rows.M > kLoraAlone) {                                   // the sums become operands, behind the parts
+        LoraPack k{};
+        for (int i = 0; i < n; ++i) {
+            k.l[i] = l[i];
+            k.inner[i] = inner[i];
+            k.out[i] = reinterpret_cast<uint16_t*>(inner[i] + (static_cast<size_t>(p.parts) * rows.M * l[i].R + 63) / 64 * 64);
+        }
+        k.rows = rows; k.parts = p.parts;
+        hipLaunchKernelGGL(lora_pack_kernel, dim3((rows.M + 15) / 16, n), dim3(256), 0, stream, k);
+        for (int i = 0; i < n; ++i) operands[i] = reinterpret_cast<const float*>(k.out[i]);
+    } else {
+        for (int i = 0; i < n; ++i) operands[i] = inner[i];
+    }
     return hipGetLastError();
 }
 
+template <int NS, int FORM>
+static void outer_rank(const LoraOuter& p, int N, hipStream_t stream) {
+    constexpr int NT = 2, WIDE = NS == 4 ? 128 : 256;
+    // Few rows: about four workgroups per CU if they all choose differently.  (64 rows of 40 adapters, gate/up of 11008, us: one step of 256 columns 29.5, of
+    // 512 23, of 1024 18; four steps of 128 15.5.)
+    const int blocks = (N + 64 * NT - 1) / (64 * NT), steps = std::min(std::max(static_cast<int>(static_cast<int64_t>(p.rows.M) * blocks / 1024), 1), 8);
+    // (neighbours share a part of up)
+    if (p.rows.M <= kLoraAlone)
+        hipLaunchKernelGGL((lora_few_kernel<NS, FORM, NT>), dim3((p.rows.M + 15) / 16, (blocks + steps - 1) / steps, 16), dim3(256), 0, stream, p, steps);
+    else
+        hipLaunchKernelGGL((lora_many_kernel<NS, FORM>), dim3((p.rows.M + 15) / 16 * (((N + WIDE - 1) / WIDE + 7) / 8 * 8)), dim3(256), 0, stream, p);
+}
 template <int FORM>
 static hipError_t outer_form(const LoraOuter& p, int R, int N, hipStream_t stream) {
     if (p.rows.M <= 0) return hipSuccess;
-    const dim3 grid((p.rows.M + 15) / 16, (N + 64 * kOuterTiles - 1) / (64 * kOuterTiles));   // (neighbours share a part of up)
-    if (R <= 32) hipLaunchKernelGGL((lora_outer_kernel<1, FORM>), grid, dim3(256), 0, stream, p);
-    else if (R <= 64) hipLaunchKernelGGL((lora_outer_kernel<2, FORM>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((lora_outer_kernel<4, FORM>), grid, dim3(256), 0, stream, p);
+    if (R <= 32) outer_rank<1, FORM>(p, N, stream);
+    else if (R <= 64) outer_rank<2, FORM>(p, N, stream);
+    else outer_rank<4, FORM>(p, N, stream);
     return hipGetLastError();
 }
 

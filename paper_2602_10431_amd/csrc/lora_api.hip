@@ -61,10 +61,11 @@ int qtale_linear_lora_w4a16(const qtale_qlinear* w, int bits, int group, const q
     const LoraDev l = lora_device(lora);
     const LoraRows rows{adapter, nullptr, nullptr, M, 0};
     float* inner = static_cast<float*>(workspace);
+    const float* operands = nullptr;
     int parts = 0;
-    HIP_TRY(launch_lora_inner(&l, 1, rows, A, &inner, &parts, s));
+    HIP_TRY(launch_lora_inner(&l, 1, rows, A, &inner, &operands, &parts, s));
     HIP_TRY(base_linear(w, nullptr, bits, group, A, M, out, s));
-    HIP_TRY(launch_lora_add(l, rows, inner, parts, out, w->N, 0, s));
+    HIP_TRY(launch_lora_add(l, rows, operands, parts, out, w->N, 0, s));
     return QTALE_OK;
 }
 
@@ -92,12 +93,13 @@ int qtale_swiglu_lora_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, 
     void* base = at += inner_bytes(lora_up, M);
     LoraDev l[2];
     float* inner[2];
+    const float* operands[2] = {nullptr, nullptr};
     int parts[2] = {0, 0}, n = 0;
     if (lg.n) { l[n] = lg; inner[n++] = inner_g; }
     if (lu.n) { l[n] = lu; inner[n++] = inner_u; }
-    HIP_TRY(launch_lora_inner(l, n, rows, A, inner, parts, s));
+    HIP_TRY(launch_lora_inner(l, n, rows, A, inner, operands, parts, s));
     HIP_TRY(base_linear(gate, up, bits, group, A, M, base, s));
-    HIP_TRY(launch_lora_swiglu(lg, lu, rows, inner_g, inner_u, parts[0], parts[n - 1], base, out, gate->N, s));
+    HIP_TRY(launch_lora_swiglu(lg, lu, rows, operands[0], operands[n - 1], parts[0], parts[n - 1], base, out, gate->N, s));
     return QTALE_OK;
 }
 

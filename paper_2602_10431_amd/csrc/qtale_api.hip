@@ -235,25 +235,29 @@ struct LoraCall {
 // Inner values of those of `n` linears of one input that have adapters (`at`: which of them).
 struct LoraInners {
     LoraDev l[kLoraMost];
-    const float* inner[kLoraMost];
+    const float* operands[kLoraMost];
     int parts[kLoraMost];
 };
 hipError_t lora_inners(const LoraCall& lc, const qtale_lora* const* which, int n, const LoraRows& rows, const void* A, LoraInners* out, hipStream_t stream) {
     LoraDev l[kLoraMost];
     float* inner[kLoraMost];
+    const float* operands[kLoraMost];
     int parts[kLoraMost], at[kLoraMost], found = 0;
     for (int i = 0; i < n; ++i) {
         out->l[i] = lora_device(which[i]);
-        out->inner[i] = lc.inner[i];
+        out->operands[i] = nullptr;
         out->parts[i] = 0;
         if (out->l[i].n == 0) continue;
         l[found] = out->l[i];
         inner[found] = lc.inner[i];
         at[found++] = i;
     }
-    if (found == 0) return hipSuccess;
-    const hipError_t e = launch_lora_inner(l, found, rows, A, inner, parts, stream);
-    for (int i = 0; i < found; ++i) out->parts[at[i]] = parts[i];
+    if (found == 0 || rows.M <= 0) return hipSuccess;
+    const hipError_t e = launch_lora_inner(l, found, rows, A, inner, operands, parts, stream);
+    for (int i = 0; i < found; ++i) {
+        out->parts[at[i]] = parts[i];
+        out->operands[at[i]] = operands[i];
+    }
     return e;
 }
 
@@ -392,7 +396,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 3, lora_rows, ws.nbuf, &in, stream));
             for (int i = 0; i < 3; ++i)
-                if (in.l[i].n) HIP_TRY(launch_lora_add(in.l[i], lora_rows, in.inner[i], in.parts[i], reinterpret_cast<uint16_t*>(ws.qkv) + columns[i], qkv_w, 0, stream));
+                if (in.l[i].n) HIP_TRY(launch_lora_add(in.l[i], lora_rows, in.operands[i], in.parts[i], reinterpret_cast<uint16_t*>(ws.qkv) + columns[i], qkv_w, 0, stream));
         }
     }
     // Prefill attention: the work list comes from the launch before it, the partial sums of key ranges go to what lies free until
@@ -443,7 +447,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             const qtale_lora* which[1] = {&lora->layer->o};
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 1, lora_rows, ws.attn, &in, stream));
-            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.inner[0], in.parts[0], ws.h, H, 1, stream));
+            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.operands[0], in.parts[0], ws.h, H, 1, stream));
         }
     }
     if (!few_fused) {
@@ -472,7 +476,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             const qtale_lora* which[2] = {&lora->layer->gate, &lora->layer->up};
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 2, lora_rows, ws.nbuf, &in, stream));
-            HIP_TRY(launch_lora_swiglu(in.l[0], in.l[1], lora_rows, in.inner[0], in.inner[1], in.parts[0], in.parts[1], lora->pair, ws.act, I, stream));
+            HIP_TRY(launch_lora_swiglu(in.l[0], in.l[1], lora_rows, in.operands[0], in.operands[1], in.parts[0], in.parts[1], lora->pair, ws.act, I, stream));
         }
     }
     {
@@ -481,7 +485,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             const qtale_lora* which[1] = {&lora->layer->down};
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 1, lora_rows, ws.act, &in, stream));
-            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.inner[0], in.parts[0], ws.h, H, 1, stream));
+            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.operands[0], in.parts[0], ws.h, H, 1, stream));
         }
         GemmArgs g{};
         g.A = ws.act; g.count = count; g.M_max = M_max; g.rows_exact = ratio_mode; g.streams = streams; g.K = I; g.group = c->group; g.bits = lbits; g.n_w = 1;
