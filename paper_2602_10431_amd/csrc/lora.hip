@@ -232,11 +232,13 @@ struct LoraOuter {
 };
 enum { LORA_ADD_F16, LORA_ADD_F32, LORA_SWIGLU };
 
-// up_a of columns n .. n + 15 (lane c: column n + c), k-step s: inner values 32 s + 8 g ..
-template <int NS>
-__device__ __forceinline__ void up_operand(const LoraDev& l, int a, int n, u32x4_t* w) {
+// A wave's products of 16 NT columns from n0 on: product j has columns n0 + 4 NT (i / 4) + 4 j + i % 4, i < 16, so that lane (c, g), which gets i = 4 g .. 4 g + 3
+// of each, has 4 NT columns in a row of the matrix that it reads and writes.
+// up_a of product j's columns (lane c: i = c), k-step s: inner values 32 s + 8 g ..
+template <int NS, int NT>
+__device__ __forceinline__ void up_operand(const LoraDev& l, int a, int n0, int j, u32x4_t* w) {
     const int c = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
-    const uint16_t* at = l.up + (static_cast<size_t>(a) * l.N + min(n + c, l.N - 1)) * l.R;
+    const uint16_t* at = l.up + (static_cast<size_t>(a) * l.N + min(n0 + 4 * NT * (c >> 2) + 4 * j + (c & 3), l.N - 1)) * l.R;
 #pragma unroll
     for (int s = 0; s < NS; ++s) w[s] = *reinterpret_cast<const u32x4_t*>(at + min(32 * s + 8 * g, l.R - 8));
 }
@@ -257,42 +259,53 @@ __device__ __forceinline__ float4_t outer_product(const u32x4_t* w, const u32x4_
     return y;
 }
 
-// Four values of a row: what is there and what is added.
+// Eight values of a row: what is there and what is added (two products' four).
 template <int FORM> struct OuterRow;
 template <> struct OuterRow<LORA_ADD_F32> {
-    float4_t old;
-    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) { old = *reinterpret_cast<const float4_t*>(static_cast<const float*>(p.out) + row * p.ldo + n); }
-    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t& y, const float4_t&) const { *reinterpret_cast<float4_t*>(static_cast<float*>(p.out) + row * p.ldo + n) = old + y; }
+    float4_t old[2];
+    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) {
+        const float4_t* from = reinterpret_cast<const float4_t*>(static_cast<const float*>(p.out) + row * p.ldo + n);
+        old[0] = from[0];
+        old[1] = from[1];
+    }
+    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t* y, const float4_t*) const {
+        float4_t* to = reinterpret_cast<float4_t*>(static_cast<float*>(p.out) + row * p.ldo + n);
+        to[0] = old[0] + y[0];
+        to[1] = old[1] + y[1];
+    }
 };
-__device__ __forceinline__ float half_of(const U2& w, int r) { return half_bits_to_float(static_cast<uint16_t>((r < 2 ? w.x : w.y) >> (16 * (r & 1)) & 0xffffu)); }
-__device__ __forceinline__ U2 halves(const float4_t& y) {
-    return U2{to_half(y[0]) | static_cast<uint32_t>(to_half(y[1])) << 16, to_half(y[2]) | static_cast<uint32_t>(to_half(y[3])) << 16};
+__device__ __forceinline__ float half_of(const u32x4_t& w, int e) { return half_bits_to_float(static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)) & 0xffffu)); }
+__device__ __forceinline__ u32x4_t halves(const float* y) {
+    u32x4_t w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = to_half(y[2 * e]) | static_cast<uint32_t>(to_half(y[2 * e + 1])) << 16;
+    return w;
 }
 template <> struct OuterRow<LORA_ADD_F16> {
-    U2 old;
-    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) { old = *reinterpret_cast<const U2*>(static_cast<const uint16_t*>(p.out) + row * p.ldo + n); }
-    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t& y, const float4_t&) const {
-        float4_t sum;
+    u32x4_t old;
+    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) { old = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p.out) + row * p.ldo + n); }
+    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t* y, const float4_t*) const {
+        float sum[8];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum[r] = half_of(old, r) + y[r];
-        *reinterpret_cast<U2*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(sum);
+        for (int e = 0; e < 8; ++e) sum[e] = half_of(old, e) + y[e >> 2][e & 3];
+        *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(sum);
     }
 };
 template <> struct OuterRow<LORA_SWIGLU> {
-    U2 gate, up;
+    u32x4_t gate, up;
     __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int N) {
         const uint16_t* from = p.base + row * 2 * N + n;
-        gate = *reinterpret_cast<const U2*>(from);
-        up = *reinterpret_cast<const U2*>(from + N);
+        gate = *reinterpret_cast<const u32x4_t*>(from);
+        up = *reinterpret_cast<const u32x4_t*>(from + N);
     }
-    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t& yg, const float4_t& yu) const {
-        float4_t out;
+    __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t* yg, const float4_t* yu) const {
+        float out[8];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float x = half_of(gate, r) + yg[r];
-            out[r] = x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)) * (half_of(up, r) + yu[r]);   // (off by 2^-22 or so)
+        for (int e = 0; e < 8; ++e) {
+            const float x = half_of(gate, e) + yg[e >> 2][e & 3];
+            out[e] = x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)) * (half_of(up, e) + yu[e >> 2][e & 3]);   // (off by 2^-22 or so)
         }
-        *reinterpret_cast<U2*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(out);
+        *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(out);
     }
 };
 
@@ -326,17 +339,17 @@ lora_few_kernel(LoraOuter p, int steps) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) a[i] = adapter_of(p.l[i], choice);
     u32x4_t w[NL][NT][NS];
-    OuterRow<FORM> there[NT];
+    OuterRow<FORM> there[NT / 2];
     auto fetch = [&](int n0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             if (a[i] < 0) continue;                              // (the same in all lanes)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) up_operand<NS>(p.l[i], a[i], n0 + 16 * j, w[i][j]);
+            for (int j = 0; j < NT; ++j) up_operand<NS, NT>(p.l[i], a[i], n0, j, w[i][j]);
         }
         if (own) {                                               // (N is a multiple of 8)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) there[j].read(p, row, min(n0 + 16 * j + 4 * g, N - 4), N);
+            for (int h = 0; h < NT / 2; ++h) there[h].read(p, row, min(n0 + 4 * NT * g + 8 * h, N - 8), N);
         }
     };
     int n0 = (blockIdx.y * steps * 4 + wave) * (16 * NT);
@@ -364,86 +377,97 @@ lora_few_kernel(LoraOuter p, int steps) {
     }
 #pragma unroll 1
     for (int step = 0; step < steps && n0 < N; ++step, n0 += 64 * NT) {
+        float4_t y[NL][NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            float4_t y[NL];
+        for (int i = 0; i < NL; ++i)
 #pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                y[i] = float4_t{0.f, 0.f, 0.f, 0.f};
-                if (a[i] >= 0) y[i] = outer_product<NS>(w[i][j], mask[i], x[i]) * unit[i];
+            for (int j = 0; j < NT; ++j) {
+                y[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+                if (a[i] >= 0) y[i][j] = outer_product<NS>(w[i][j], mask[i], x[i]) * unit[i];
             }
-            if (own && n0 + 16 * j + 4 * g < N) there[j].write(p, row, n0 + 16 * j + 4 * g, y[0], y[NL - 1]);
-        }
+#pragma unroll
+        for (int h = 0; h < NT / 2; ++h)
+            if (own && n0 + 4 * NT * g + 8 * h < N) there[h].write(p, row, n0 + 4 * NT * g + 8 * h, &y[0][2 * h], &y[NL - 1][2 * h]);
         if (step + 1 < steps) fetch(n0 + 64 * NT);
     }
 }
 
-// Many rows, operands made (lora_pack_kernel): a wave per 16 rows and 64 columns, which walks the adapters that the rows have, mostly one; the first one's
-// are on their way with everything else that the wave reads.
+constexpr int many_tiles(int ns, int form) { return ns * (form == LORA_SWIGLU ? 2 : 1) >= 4 ? 2 : 4; }   // (registers)
+
+// Many rows, operands made (lora_pack_kernel): a wave per 64 rows and 16 NT columns, 16 rows at a time, the next ones on their way.  It walks the adapters
+// that the rows have, mostly one, and keeps its part of up until another comes.
 template <int NS, int FORM>
 __global__ void __launch_bounds__(256)
 lora_many_kernel(LoraOuter p) {
-    constexpr int NT = NS == 4 ? 2 : 4, NL = FORM == LORA_SWIGLU ? 2 : 1;
+    constexpr int NT = many_tiles(NS, FORM), NL = FORM == LORA_SWIGLU ? 2 : 1;
     const int M = p.rows.count ? min(*p.rows.count, p.rows.M) : p.rows.M;
-    // Workgroups go round-robin to the 8 XCDs: each has its own blocks of columns, whose part of up its L2 holds for all tiles of rows.
-    const int tiles = (p.rows.M + 15) / 16, local = blockIdx.x >> 3, block = local / tiles * 8 + (blockIdx.x & 7);
-    const int row0 = (local % tiles) * 16, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    // Workgroups go round-robin to the 8 XCDs: each has its own blocks of columns, whose part of up its L2 holds for all rows.
+    const int chunks = (p.rows.M + 63) / 64, local = blockIdx.x >> 3, block = local / chunks * 8 + (blockIdx.x & 7);
+    const int row0 = (local % chunks) * 64, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int N = FORM == LORA_SWIGLU ? p.ldo : p.l[0].N, n0 = (block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * (16 * NT);
     if (row0 >= M || n0 >= N) return;
-    const size_t row = min(row0 + c, M - 1);
-    const int mine = choice_of(p.rows, row0 + lane, lane < 16 ? M : 0);   // lane x: row x of the tile
-    half8_t x[NL][NS];
-    float unit[NL];
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        if (p.l[i].n == 0) continue;
-        const uint16_t* operands = reinterpret_cast<const uint16_t*>(p.inner[i]);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) x[i][s] = *reinterpret_cast<const half8_t*>(operands + row * operand_width(p.l[i].R) + min(32 * s + 8 * g, operand_width(p.l[i].R) - 8));
-        unit[i] = operand_units(operands, p.l[i].R, p.rows.M)[row];
-    }
-    OuterRow<FORM> there[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) there[j].read(p, row, min(n0 + 16 * j + 4 * g, N - 4), N);   // (N is a multiple of 8)
-    const int choice = __shfl(mine, c, 64);                      // of this lane's row
-    const uint64_t rows = __ballot(lane < 16 && row0 + lane < M && (FORM == LORA_SWIGLU || adapter_of(p.l[0], mine) >= 0));
-    float4_t y[NL][NT];
-    u32x4_t w[NL][NT][NS];
-    uint64_t left[NL];
-    int a[NL];
-    auto next = [&](int i) __attribute__((always_inline)) {      // the next adapter that a row has, its part of up
-        a[i] = -1;
-        if (left[i] == 0) return;
-        a[i] = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(left[i])) - 1));
-        left[i] &= ~__ballot(mine == a[i]);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) up_operand<NS>(p.l[i], a[i], n0 + 16 * j, w[i][j]);
+    struct Rows {                                                // what the wave reads of 16 rows
+        half8_t x[NL][NS];
+        float unit[NL];
+        OuterRow<FORM> there[NT / 2];
     };
+    auto read = [&](int t, Rows& to) __attribute__((always_inline)) {
+        const size_t row = min(row0 + 16 * t + c, M - 1);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        left[i] = rows & __ballot(adapter_of(p.l[i], mine) >= 0);
-        next(i);
-    }
+        for (int i = 0; i < NL; ++i) {
+            if (p.l[i].n == 0) continue;
+            const uint16_t* operands = reinterpret_cast<const uint16_t*>(p.inner[i]);
+            const int width = operand_width(p.l[i].R);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j) y[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
-        while (a[i] >= 0) {
-            u32x4_t mask[NS];
-            rank_mask<NS>(rank_of(p.l[i], a[i]), mask);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const float4_t d = outer_product<NS>(w[i][j], mask, x[i]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) y[i][j][r] = choice == a[i] ? d[r] * unit[i] : y[i][j][r];
-            }
-            next(i);
+            for (int s = 0; s < NS; ++s) to.x[i][s] = *reinterpret_cast<const half8_t*>(operands + row * width + min(32 * s + 8 * g, width - 8));
+            to.unit[i] = operand_units(operands, p.l[i].R, p.rows.M)[row];
         }
-    }
-    if ((rows >> c & 1) == 0) return;
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-        if (n0 + 16 * j + 4 * g < N) there[j].write(p, row, n0 + 16 * j + 4 * g, y[0][j], y[NL - 1][j]);
+        for (int h = 0; h < NT / 2; ++h) to.there[h].read(p, row, min(n0 + 4 * NT * g + 8 * h, N - 8), N);   // (N is a multiple of 8)
+    };
+    Rows now, next;
+    read(0, now);
+    const int mine = choice_of(p.rows, row0 + lane, M);          // lane x: row x of the 64
+    const uint64_t rows = __ballot(row0 + lane < M && (FORM == LORA_SWIGLU || adapter_of(p.l[0], mine) >= 0));
+    u32x4_t w[NL][NT][NS], mask[NL][NS];
+    int held[NL];                                                // the adapter whose part of up is there
+#pragma unroll
+    for (int i = 0; i < NL; ++i) held[i] = -1;
+#pragma unroll 1
+    for (int t = 0; t < 4 && row0 + 16 * t < M; ++t) {
+        if (t < 3) read(t + 1, next);
+        const uint32_t own = static_cast<uint32_t>(rows >> (16 * t)) & 0xffffu;
+        const int choice = __shfl(mine, 16 * t + c, 64);         // of this lane's row
+        float4_t y[NL][NT];
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) y[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+            uint32_t left = own & static_cast<uint32_t>(__ballot(adapter_of(p.l[i], mine) >= 0) >> (16 * t));
+            while (left != 0) {
+                const int a = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane(16 * t + __ffs(static_cast<int>(left)) - 1));
+                left &= ~static_cast<uint32_t>(__ballot(mine == a) >> (16 * t));
+                if (a != held[i]) {
+                    held[i] = a;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) up_operand<NS, NT>(p.l[i], a, n0, j, w[i][j]);
+                    rank_mask<NS>(rank_of(p.l[i], a), mask[i]);
+                }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const float4_t d = outer_product<NS>(w[i][j], mask[i], now.x[i]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[i][j][r] = choice == a ? d[r] * now.unit[i] : y[i][j][r];
+                }
+            }
+        }
+        if ((own >> c & 1) != 0) {
+#pragma unroll
+            for (int h = 0; h < NT / 2; ++h)
+                if (n0 + 4 * NT * g + 8 * h < N) now.there[h].write(p, row0 + 16 * t + c, n0 + 4 * NT * g + 8 * h, &y[0][2 * h], &y[NL - 1][2 * h]);
+        }
+        now = next;
+    }
 }
 
 constexpr int kLoraAlone = 256;  // rows up to which they are taken to choose differently
@@ -517,7 +541,7 @@ hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, cons
 
 template <int NS, int FORM>
 static void outer_rank(const LoraOuter& p, int N, hipStream_t stream) {
-    constexpr int NT = 2, WIDE = NS == 4 ? 128 : 256;
+    constexpr int NT = 2, WIDE = 64 * many_tiles(NS, FORM);
     // Few rows: about four workgroups per CU if they all choose differently.  (64 rows of 40 adapters, gate/up of 11008, us: one step of 256 columns 29.5, of
     // 512 23, of 1024 18; four steps of 128 15.5.)
     const int blocks = (N + 64 * NT - 1) / (64 * NT), steps = std::min(std::max(static_cast<int>(static_cast<int64_t>(p.rows.M) * blocks / 1024), 1), 8);
@@ -525,7 +549,7 @@ static void outer_rank(const LoraOuter& p, int N, hipStream_t stream) {
     if (p.rows.M <= kLoraAlone)
         hipLaunchKernelGGL((lora_few_kernel<NS, FORM, NT>), dim3((p.rows.M + 15) / 16, (blocks + steps - 1) / steps, 16), dim3(256), 0, stream, p, steps);
     else
-        hipLaunchKernelGGL((lora_many_kernel<NS, FORM>), dim3((p.rows.M + 15) / 16 * (((N + WIDE - 1) / WIDE + 7) / 8 * 8)), dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((lora_many_kernel<NS, FORM>), dim3((p.rows.M + 63) / 64 * (((N + WIDE - 1) / WIDE + 7) / 8 * 8)), dim3(256), 0, stream, p);
 }
 template <int FORM>
 static hipError_t outer_form(const LoraOuter& p, int R, int N, hipStream_t stream) {
