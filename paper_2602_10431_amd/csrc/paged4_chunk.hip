@@ -24,6 +24,11 @@ __device__ __forceinline__ u32x4_t codes_less4(uint32_t w, uint32_t z) {
     const uint32_t y = w >> 8, z16 = z << 4;
     return u32x4_t{less(w & 0x000f000fu, z), less(w & 0x00f000f0u, z16), less(y & 0x000f000fu, z), less(y & 0x00f000f0u, z16)};
 }
+// A value that is to be made where it is used: what is derived from it is not kept in registers across the loop.
+__device__ __forceinline__ int here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 // Where 16-byte chunk c of a row lies: at chunk c ^ swizzle, such that what a read or a write touches at a time spreads over the banks.
 template <int D> __device__ __forceinline__ int k4_swizzle(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
 __device__ __forceinline__ int v4_swizzle(int col) { return ((col >> 1) ^ (col >> 4)) & 7; }
@@ -33,7 +38,32 @@ template <int D>
 struct Tile4 {
     uint16_t* K;                 // [64 keys][D]
     uint16_t* V;                 // [D columns][64 keys]
-    float *ks, *ts, *tmax;       // scales of keys (with the softmax scale) and values, the largest of 16 values each
+    float *ks, *ts;              // scales of keys (with the softmax scale) and values
+    uint32_t* tmax;              // the largest of 16 values each, as bits; their sign: some are no numbers
+};
+
+// Pages of tiles one after the other: a lane per 16 keys holds the page of sixteen tiles, the next sixteen's are on their way.
+template <class Walk>
+struct TileWalk {
+    const PageRow& row;
+    const Walk& walk;
+    int t0, part, ids, later;
+    uint64_t bad;
+    __device__ __forceinline__ TileWalk(const PageRow& row, const Walk& walk, int t0, int part) : row(row), walk(walk), t0(t0), part(part), ids(0), later(read(0)), bad(0) {}
+    __device__ __forceinline__ int read(int t) const {
+        const int lane = threadIdx.x & 63;
+        return row.row[min((walk.key(min(t0 + t + (lane >> 2), walk.steps - 1)) + 16 * (lane & 3)) >> row.shift, row.last)];
+    }
+    // the tile after the last call's
+    __device__ __forceinline__ TilePages next(int t) {
+        if ((t & 15) == 0) {
+            ids = later;
+            bad = __ballot(static_cast<uint32_t>(ids) >= static_cast<uint32_t>(row.n_pages));
+            later = read(t + 16);
+        }
+        const int at = 4 * (t & 15), gone = __builtin_amdgcn_readfirstlane(static_cast<int>(bad >> at) & 15), page = __builtin_amdgcn_readlane(ids, at + part);
+        return TilePages{gone >> part & 1 ? -1 : page, gone};
+    }
 };
 
 // One wave's part of unpacking tiles: 16 keys, or 16 values, or both.
@@ -57,6 +87,7 @@ struct Unpack4 {
     }
     // the head's block of a page; of one that is gone: an empty buffer, zeros
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint16_t* pool, int page) const {
+        page = __builtin_amdgcn_readfirstlane(page);
         return buffer_of(reinterpret_cast<const char*>(pool) + (static_cast<size_t>(max(page, 0)) * p.nkv + hk) * block, page < 0 ? 0 : static_cast<int>(block));
     }
     // key0: the tile's first
@@ -78,34 +109,48 @@ struct Unpack4 {
     __device__ __forceinline__ void put_keys(int key0, const Tile4<D>& to) const {
         const int lane = threadIdx.x & 63, key = 16 * part + (lane >> 2);
         const uint32_t zz = __builtin_amdgcn_perm(kp, kp, 0x07060706u) & 0x000f000fu;
+        const int at = here(key * D + ((S * (lane & 3)) ^ k4_swizzle<D>(key)) * 8);   // of the lane's first chunk; chunk w: w flipped in
 #pragma unroll
-        for (int w = 0; w < S; ++w)
-            *reinterpret_cast<u32x4_t*>(&to.K[key * D + (((S * (lane & 3) + w) ^ k4_swizzle<D>(key)) * 8)]) = codes_less4(kw[w], zz);
+        for (int w = 0; w < S; ++w) *reinterpret_cast<u32x4_t*>(&to.K[at ^ (8 * w)]) = codes_less4(kw[w], zz);
         if ((lane & 3) == 0) to.ks[key] = key0 + key < hi ? act_to_float<BF16>(static_cast<uint16_t>(kp & 0xffffu)) * unit : 0.0f;
     }
     __device__ __forceinline__ void put_values(int key0, const Tile4<D>& to) const {
         const int lane = threadIdx.x & 63, four = lane >> 4, c = lane & 15;
         float4_t t4;
-        float big = 0.0f;
+        uint32_t big = 0;                                        // (numbers without their sign compare as their bits do)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             t4[r] = key0 + 16 * part + 4 * four + r < hi ? act_to_float<BF16>(static_cast<uint16_t>(vp[r] & 0xffffu)) : 0.0f;
-            big = fmaxf(big, t4[r]);
+            const uint32_t u = __float_as_uint(t4[r]) & 0x7fffffffu;
+            big = max(big, u);
         }
         if (c == 0) *reinterpret_cast<float4_t*>(&to.ts[16 * part + 4 * four]) = t4;
-        big = fmaxf(big, __shfl_xor(big, 16, 64));
-        big = fmaxf(big, __shfl_xor(big, 32, 64));
-        if (lane == 0) to.tmax[part] = big;
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = max(most, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(big), 16 * i)));
+        if (most >= 0x7f800000u) {                               // some are no numbers: the largest of the others, and a mark
+            big = 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t u = __float_as_uint(t4[r]) & 0x7fffffffu;
+                big = max(big, u < 0x7f800000u ? u : 0u);
+            }
+            most = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = max(most, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(big), 16 * i)));
+            most |= 0x80000000u;
+        }
+        if (lane == 0) to.tmax[part] = most;
         const uint32_t z01 = __builtin_amdgcn_perm(vp[1], vp[0], 0x07060302u) & 0x000f000fu, z23 = __builtin_amdgcn_perm(vp[3], vp[2], 0x07060302u) & 0x000f000fu;
-        // tokens 4 four .. + 3 of 16: chunk 2 part + (four & 1) of a column's row, its half four >> 1
+        // tokens 4 four .. + 3 of 16: chunk 2 part + (four & 1) of a column's row, its half four >> 1 (of the lane's columns, D / 16 from a multiple of that on,
+        // the swizzle is the first one's with half of what is added flipped in)
+        const int first = (D / 16) * c;
+        const int at = here(first * kTileKeys + (((2 * part + (four & 1)) ^ v4_swizzle(first)) * 8) + 4 * (four >> 1));
 #pragma unroll
         for (int h = 0; h < S / 2; ++h) {
             const u32x4_t a = codes_less4(vw[2 * h], z01), b = codes_less4(vw[2 * h + 1], z23);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int column = (D / 16) * c + 4 * h + i;
-                *reinterpret_cast<u32x2_t*>(&to.V[column * kTileKeys + (((2 * part + (four & 1)) ^ v4_swizzle(column)) * 8) + 4 * (four >> 1)]) = u32x2_t{a[i], b[i]};
-            }
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x2_t*>(&to.V[(at ^ (8 * (2 * h + (i >> 1)))) + (4 * h + i) * kTileKeys]) = u32x2_t{a[i], b[i]};
         }
     }
 };
@@ -201,88 +246,56 @@ struct Columns4 {
         }
     }
 
-    // Scores -> probabilities as operands, times their values' scales; the probabilities' sum.  FAST: scores are products (st) times their key's scale, one
-    // fused operation; else st holds scores, of `hidden` keys minus infinity.
-    template <bool FAST>
-    __device__ __forceinline__ float weigh(const Tile4<D>& tile, uint32_t hidden) {
-        const int lhi = (threadIdx.x & 63) >> 5;
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    // Keys' scales of the first half of a tile and the largest of the values': asked for before the wave unpacks, since beside the other half's operands a
+    // read takes long.
+    struct Scales { float4_t k[4]; u32x4_t most; };
+    __device__ __forceinline__ Scales scales(const Tile4<D>& tile) const {
+        const int quad = here(4 * ((threadIdx.x & 63) >> 5));
+        Scales x;
+        x.most = *reinterpret_cast<const u32x4_t*>(tile.tmax);
 #pragma unroll
-        for (int kf = 0; kf < 2; ++kf)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                const int at = 32 * kf + 8 * q4 + 4 * lhi;
-                const float4_t t4 = *reinterpret_cast<const float4_t*>(&tile.ts[at]);
-                float4_t k4 = {0.f, 0.f, 0.f, 0.f};
-                if (FAST) k4 = *reinterpret_cast<const float4_t*>(&tile.ks[at]);
-#pragma unroll
-                for (int r = 0; r < 4; r += 2) {
-                    const int i = 4 * q4 + r;
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(st[kf][i], FAST ? k4[r] : up, -m_run));
-                    const float p1 = __builtin_amdgcn_exp2f(fmaf(st[kf][i + 1], FAST ? k4[r + 1] : up, -m_run));
-                    sum[q4] += p0 + p1;
-                    float w0 = p0 * t4[r], w1 = p1 * t4[r + 1];
-                    if (!FAST) {                                 // (a scale that the column does not see may be NaN)
-                        w0 = hidden >> (16 * kf + i) & 1 ? 0.0f : w0;
-                        w1 = hidden >> (16 * kf + i + 1) & 1 ? 0.0f : w1;
-                    }
-                    uint32_t w = H::pack(w0, w1);
-                    asm("" : "+v"(w));                           // (packed here: carried past the caller's branch, 32 values would take 16 registers more)
-                    pf[kf * 2 + (q4 >> 1)][2 * (q4 & 1) + (r >> 1)] = w;
-                }
-            }
-        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        for (int i = 0; i < 4; ++i) x.k[i] = *reinterpret_cast<const float4_t*>(&tile.ks[quad + 8 * i]);
+        __builtin_amdgcn_sched_barrier(0);
+        return x;
     }
-    // st: products -> scores (in units of `up`)
-    __device__ __forceinline__ void scale_scores(const Tile4<D>& tile) {
-        const int lhi = (threadIdx.x & 63) >> 5;
+    // Probabilities of keys key0 .. key0 + 63, times their values' scales, as operands; gone: bit per 16 keys without a page.
+    __device__ __forceinline__ void softmax(const PagedAttnDev& p, const Tile4<D>& tile, Scales& x, int key0, int gone, int hi) {
+        key0 = __builtin_amdgcn_readfirstlane(key0);
+        gone = __builtin_amdgcn_readfirstlane(gone);
+        const int quad = here(4 * ((threadIdx.x & 63) >> 5));
+        const float* ks = tile.ks + quad;
+        const float* ts = tile.ts + quad;
+        uint32_t most = 0, odds = 0;                             // the largest scale of a value; the sign's bit: some are no numbers
 #pragma unroll
-        for (int kf = 0; kf < 2; ++kf)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                const float4_t k4 = *reinterpret_cast<const float4_t*>(&tile.ks[32 * kf + 8 * q4 + 4 * lhi]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) st[kf][4 * q4 + r] *= k4[r];
-            }
-    }
-    // Probabilities of keys key0 .. key0 + 63; gone: bit per 16 keys without a page.
-    __device__ __forceinline__ void softmax(const PagedAttnDev& p, const Tile4<D>& tile, int key0, int gone, int hi) {
-        const int lhi = (threadIdx.x & 63) >> 5;
-        // values' scales above the reference so far: the next power of two but one
-        const float4_t tm = *reinterpret_cast<const float4_t*>(tile.tmax);
-        const float tx = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3])))));
-        if (tx > ldexpf(1.0f, t_exp)) {
-            const int e = min(static_cast<int>(__float_as_uint(tx) >> 23) - 127 + 2, 126);
-            const float beta = ldexpf(1.0f, t_exp - e);
-            m_run = m_run > kPagedNone ? m_run + static_cast<float>(e - t_exp) : m_run;
-            rescale(beta);
-            t_exp = e;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = __builtin_amdgcn_readfirstlane(x.most[i]);
+            most = max(most, u & 0x7fffffffu);
+            odds |= u;
         }
-        // The reference point stays as long as the probabilities' sum over the lane's keys does not pass fp16's largest number, so each fits; it is seen
-        // from the sum that is needed anyway.
-        const float most = ldexpf(65504.0f, -t_exp);
-        // A tile that every query of the wave sees whole needs no mask.  One fused operation is exact enough while a score's last bit, which the reference
-        // point has been rounded to, is small.
+        const bool odd = (odds >> 31) != 0;
+        const float tx = __uint_as_float(most);
+        // products -> scores (in units of `up`)
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            const float4_t k4 = x.k[g & 3];
+            x.k[g & 3] = *reinterpret_cast<const float4_t*>(g < 4 ? ks + 8 * (g + 4) : ts + 8 * (g - 4));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st[g >> 2][4 * (g & 3) + r] *= k4[r];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // A tile that every query of the wave sees whole needs no mask.
         const bool all = gone == 0 && key0 + kTileKeys <= min(w_first + 1, hi) && (p.window == 0 || key0 > w_last - p.window || key0 + kTileKeys <= p.sinks);
-        float sum = 0.0f;
-        if (all && plain) {
-            sum = weigh<true>(tile, 0u);
-            if (!__any(!(sum <= most) | (fabsf(m_run) > 0x1p20f))) {
-                l_run += sum;
-                return;
-            }
-        }
-        scale_scores(tile);
-        uint32_t hidden = 0;
         if (!all) {
+            // of the lane's keys, key0 + quad + a constant each: constants up to `last` that are after `before`, or below `stay`
+            const int last = min(place, hi - 1) - key0 - quad, before = max(reach, -1) - key0 - quad, stay = p.sinks - key0 - quad;
 #pragma unroll
             for (int kf = 0; kf < 2; ++kf)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int key = key0 + kf * 32 + 8 * (r >> 2) + 4 * lhi + (r & 3);
-                    const bool seen = (key <= place) & (key < hi) & ((gone >> (kf * 2 + (r >> 3)) & 1) == 0) & ((key > reach) | (key < p.sinks));
+                    const int at = kf * 32 + 8 * (r >> 2) + (r & 3);
+                    const bool seen = (at <= last) & ((gone >> (kf * 2 + (r >> 3)) & 1) == 0) & ((at > before) | (at < stay));
                     st[kf][r] = seen ? st[kf][r] : -INFINITY;
-                    hidden |= seen ? 0u : 1u << (16 * kf + r);
+                    if (r & 1) __builtin_amdgcn_sched_barrier(0);   // (few masks at a time)
                 }
         }
         float mx = -INFINITY;
@@ -291,13 +304,44 @@ struct Columns4 {
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kf][r]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * up;
-        const float m_new = fmaxf(m_run, mx - (kChunkLift4 - static_cast<float>(t_exp)));
-        if (__any(m_new != m_run)) {
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        // The reference point stays as long as no probability passes 2^15 and no value's scale t_ref.  It moves so that the largest probability is 2^kChunkLift4,
+        // and t_ref to the next power of two but one.
+        const bool larger = tx > ldexpf(1.0f, t_exp);
+        const float above = mx + static_cast<float>(t_exp) - m_run;
+        if (larger || __any(above > 15.0f)) {
+            const int e = larger ? min(static_cast<int>(__float_as_uint(tx) >> 23) - 127 + 2, 126) : t_exp;
+            const float m_same = m_run > kPagedNone ? m_run + static_cast<float>(e - t_exp) : m_run, m_new = fmaxf(m_same, mx - (kChunkLift4 - static_cast<float>(e)));
+            rescale(__builtin_amdgcn_exp2f(m_run - m_new));
+            t_exp = e;
             m_run = m_new;
-            rescale(alpha);
         }
-        l_run += weigh<false>(tile, hidden);
+        if (odd) weigh<true>(x, ts);
+        else weigh<false>(x, ts);
+    }
+    // Scores -> probabilities, times their values' scales, as operands; the probabilities' sum.  ODD: a scale may be no number, and a probability of zero then
+    // takes no part; one of a key that is seen is never zero.
+    template <bool ODD>
+    __device__ __forceinline__ void weigh(Scales& x, const float* ts) {
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            const float4_t t4 = x.k[g & 3];
+            if (g < 4) x.k[g] = *reinterpret_cast<const float4_t*>(ts + 8 * (g + 4));
+            const int kf = g >> 2, q4 = g & 3;
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                float w[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float at = fmaf(st[kf][4 * q4 + r + i], up, -m_run), e = __builtin_amdgcn_exp2f(ODD ? (at < -100.0f && at > -INFINITY ? -100.0f : at) : at);
+                    sum[q4] += e;
+                    w[i] = ODD && e == 0.0f ? 0.0f : e * t4[r + i];
+                }
+                pf[kf * 2 + (q4 >> 1)][2 * (q4 & 1) + (r >> 1)] = H::pack(w[0], w[1]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
     __device__ __forceinline__ void rescale(float by) {
         l_run *= by;
@@ -364,7 +408,8 @@ paged4_chunk_kernel(PagedAttnDev p) {
     using Cols = Columns4<D, BF16>;
     constexpr int TILE = kTileKeys * D;
     __shared__ __attribute__((aligned(1024))) uint16_t Ks[2][TILE], Vs[2][TILE];
-    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys], tmax[2][4];
+    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys];
+    __shared__ __attribute__((aligned(16))) uint32_t tmax[2][4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     int hk, item, z = 0, b, qt;
@@ -389,7 +434,6 @@ paged4_chunk_kernel(PagedAttnDev p) {
         const int i = (t - t0) & 1;
         return Tile4<D>{Ks[i], Vs[i], ks[i], ts[i], tmax[i]};
     };
-    auto ids_of = [&](int t) __attribute__((always_inline)) { return tile_pages(pages, walk.key(min(t, walk.steps - 1)), wave); };
     auto request = [&](int t, int page) __attribute__((always_inline)) {
         if (t >= t1) page = -1;
         un.request_keys(walk.key(t), page);
@@ -400,8 +444,8 @@ paged4_chunk_kernel(PagedAttnDev p) {
         un.put_values(walk.key(t), tile(t));
     };
     if (t0 < t1) {
-        // page ids are read a tile before the request that uses them
-        TilePages i0 = ids_of(t0), i1 = ids_of(t0 + 1), i2 = ids_of(t0 + 2);
+        TileWalk ids(pages, walk, t0, wave);
+        TilePages i0 = ids.next(0), i1 = ids.next(1), i2 = ids.next(2);
         request(t0, i0.page);
         unpack(t0);
         request(t0 + 1, i1.page);
@@ -411,11 +455,12 @@ paged4_chunk_kernel(PagedAttnDev p) {
             request(t + 2, i2.page);
             const Tile4<D> now = tile(t);
             cw.template products<Cols::PV, Cols::ALL>(now.V, now.K);
-            cw.softmax(p, now, walk.key(t), i0.gone, walk.hi);
+            typename Cols::Scales sc = cw.scales(now);
+            cw.softmax(p, now, sc, walk.key(t), i0.gone, walk.hi);
             cw.template products<0, Cols::PV>(now.V, now.K);
             i0 = i1;
             i1 = i2;
-            i2 = ids_of(t + 3);
+            i2 = ids.next(t + 3 - t0);
         }
     }
     cw.template put<SPLIT>(p, s, z, range.ranges);
@@ -433,7 +478,8 @@ paged4_wide_kernel(PagedAttnDev p) {
     using Cols = Columns4<D, BF16>;
     constexpr int TILE = kTileKeys * D;
     __shared__ __attribute__((aligned(1024))) uint16_t Ks[2][TILE], Vs[2][TILE];
-    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys], tmax[2][4];
+    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys];
+    __shared__ __attribute__((aligned(16))) uint32_t tmax[2][4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     int hk, item, z = 0, b, qt;
@@ -456,7 +502,6 @@ paged4_wide_kernel(PagedAttnDev p) {
     const int t0 = range.t0, n = range.t1 - range.t0;            // (tiles below are counted from t0)
     auto tile = [&](int t) __attribute__((always_inline)) { return Tile4<D>{Ks[t & 1], Vs[t & 1], ks[t & 1], ts[t & 1], tmax[t & 1]}; };
     auto key0 = [&](int t) __attribute__((always_inline)) { return walk.key(t0 + t); };
-    auto ids_of = [&](int t) __attribute__((always_inline)) { return tile_pages(pages, walk.key(min(t0 + t, walk.steps - 1)), wave & 3); };
     // What a wave has written to LDS is there, and its reads have been consumed; requests of its own stay outstanding: a bare barrier that no access
     // and no instruction is moved across.
     auto phase_end = [&]() __attribute__((always_inline)) {
@@ -468,7 +513,8 @@ paged4_wide_kernel(PagedAttnDev p) {
         asm volatile("" ::: "memory");
     };
     if (n > 0) {
-        TilePages i0 = ids_of(0), i1 = ids_of(1), i2 = ids_of(2);
+        TileWalk ids(pages, walk, t0, wave & 3);
+        TilePages i0 = ids.next(0), i1 = ids.next(1), i2 = ids.next(2);
         if (wave < 4) {
             un.request_keys(key0(0), i0.page);
             un.put_keys(key0(0), tile(0));
@@ -490,37 +536,40 @@ paged4_wide_kernel(PagedAttnDev p) {
             phase_end();
         };
         if (wave < 4) {
-            cw.softmax(p, tile(0), key0(0), i0.gone, walk.hi);
+            typename Cols::Scales first = cw.scales(tile(0));
+            cw.softmax(p, tile(0), first, key0(0), i0.gone, walk.hi);
             phase_end();
             auto both = [&](int t) __attribute__((always_inline)) {
                 turn(t);
-                un.put_keys(key0(t + 2), tile(t));               // (of a tile past the last: zeros)
                 i0 = i1;
                 i1 = i2;
-                i2 = ids_of(t + 3);
+                i2 = ids.next(t + 3);
+                typename Cols::Scales sc = cw.scales(tile(t + 1));
+                un.put_keys(key0(t + 2), tile(t));               // (of a tile past the last: zeros)
                 un.request_keys(key0(t + 3), t + 3 < n ? i2.page : -1);
-                cw.softmax(p, tile(t + 1), key0(t + 1), t + 1 < n ? i0.gone : 15, walk.hi);
+                cw.softmax(p, tile(t + 1), sc, key0(t + 1), t + 1 < n ? i0.gone : 15, walk.hi);
                 phase_end();
             };
-            for (int t = 0; t < n; t += 2) {
+            for (int t = 0; t < n; ++t) {
                 both(t);
-                if (t + 1 < n) both(t + 1);
+
             }
         } else {
             phase_end();
             auto both = [&](int t) __attribute__((always_inline)) {
+                typename Cols::Scales sc = cw.scales(tile(t));
                 un.put_values(key0(t + 1), tile(t + 1));
                 un.request_values(key0(t + 2), t + 2 < n ? i2.page : -1);
-                cw.softmax(p, tile(t), key0(t), i0.gone, walk.hi);
+                cw.softmax(p, tile(t), sc, key0(t), i0.gone, walk.hi);
                 i0 = i1;
                 i1 = i2;
-                i2 = ids_of(t + 3);
+                i2 = ids.next(t + 3);
                 phase_end();
                 turn(t);
             };
-            for (int t = 0; t < n; t += 2) {
+            for (int t = 0; t < n; ++t) {
                 both(t);
-                if (t + 1 < n) both(t + 1);
+
             }
         }
     }
