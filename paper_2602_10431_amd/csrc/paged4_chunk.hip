@@ -516,15 +516,17 @@ paged4_wide_kernel(PagedAttnDev p) {
         TileWalk ids(pages, walk, t0, wave & 3);
         TilePages i0 = ids.next(0), i1 = ids.next(1), i2 = ids.next(2);
         if (wave < 4) {
-            un.request_keys(key0(0), i0.page);
-            un.put_keys(key0(0), tile(0));
+            Unpack4<D, BF16> first(p, hk, wave & 3, walk.hi);
+            first.request_keys(key0(0), i0.page);
             un.request_keys(key0(1), 1 < n ? i1.page : -1);
+            first.put_keys(key0(0), tile(0));
             un.put_keys(key0(1), tile(1));
             un.request_keys(key0(2), 2 < n ? i2.page : -1);
         } else {
-            un.request_values(key0(0), i0.page);
-            un.put_values(key0(0), tile(0));
+            Unpack4<D, BF16> first(p, hk, wave & 3, walk.hi);
+            first.request_values(key0(0), i0.page);
             un.request_values(key0(1), 1 < n ? i1.page : -1);
+            first.put_values(key0(0), tile(0));
         }
         phase_end();
         cw.template products<Cols::PV, Cols::ALL>(Vs[0], Ks[0]);

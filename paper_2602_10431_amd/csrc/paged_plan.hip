@@ -24,6 +24,30 @@ static size_t decode_bytes(int nkv, int d, int B) {
     const size_t pieces = (static_cast<size_t>(std::min(B, kSpanSeqs)) * sizeof(int4) + 255) / 256 * 256;
     return pieces + static_cast<size_t>(decode_spans(nkv, d)) * nkv * 2 * kDecodeCols * part_stride(d) * 4;
 }
+// Pages in 4 bits: whether sixteen columns at a time, which unpack in registers, take less time than tiles of 128 or 256 columns, which unpack once for all
+// of them but pass LDS and barriers.  Estimates in us, from runs of either alone.  A workgroup of the decode kernel walks a key in 6.2 ns (heads of 64: 5.6)
+// until a CU's others hold it up, 4.0 (3.1) ns for each of those.  A workgroup of the wide chunk kernel, one per CU, takes 15 us and 2.9 us per tile of 64
+// keys; the other's 8 and 2.4, two on a CU 3.1 per tile; ranges cost 14 us and 0.5 ns per row of sums.  us, decode / chunk kernel, heads of 128, 4 per kv
+// head (8): 1 x 32 tokens on 1500 keys 15 / 58, on 4000 29 / 33; 1 x 64 on 24000 138 / 65; 4 x 64 on 1500 23 / 50; 64 x 8 on 2000 42 / 100; 64 x 32 on 1000
+// 92 / 68; 1 x 500 on 700 27 / 51; 8 x 128 on 2000 78 / 111; 4 x 1000 on 0 110 / 90, 2 x 2000 159 / 129; one per kv head (32) 1 x 2000 on 0 87 / 105,
+// 4 x 1000 110 / 97; heads of 64 48 x 6 on 3000 37 / 104, 64 x 16 on 3000 83 / 112.
+static bool decode4_pays(int nh, int nkv, int d, int T, int B, int64_t max_new, int64_t seen, bool window) {
+    const int rep = nh / nkv, cus = device_cus();
+    const int64_t cols = max_new * rep, sixteens = (cols + kDecodeCols - 1) / kDecodeCols, live = std::min(B, T);
+    if (sixteens > 65535) return false;                          // (a grid's second extent)
+    auto workgroups = [&](int64_t per) {                         // per CU
+        return static_cast<double>(std::min((T * static_cast<int64_t>(rep) + (per - 1) * live) / per, live * ((cols + per - 1) / per)) * nkv) / cus;
+    };
+    const double longest = static_cast<double>(seen), mean = window ? longest : std::max(longest - 0.5 * static_cast<double>(max_new), 0.0);
+    const double by = workgroups(kDecodeCols), decode = 5.0 + 1.2 * by + 0.001 * mean * (d == 64 ? std::max(5.6, 3.1 * by) : std::max(6.2, 4.0 * by));
+    const bool wide = cols > kChunkCols;
+    const double r = std::max(workgroups(wide ? kWideCols : kChunkCols), 1e-3), begin = wide ? 15.0 : 8.0, tile = wide ? 2.9 : 2.4, shared = wide ? 2.9 : 1.55;
+    const double most = longest / kChunkTileKeys, some = mean / kChunkTileKeys;
+    const double whole = begin * std::max(r, 1.0) + std::max(tile * most, shared * r * some + (r > 1.0 ? tile * (most - some) : 0.0));
+    const double ranges = std::max(std::min({(wide ? 1.0 : 2.0) / r, most / 8, 32.0}), 1.0);
+    const double cut = begin + 14.0 + std::max(tile * most / ranges, shared * r * some) + 0.0005 * T * nh * ranges;
+    return decode < std::min(whole, cut);
+}
 PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks) {
     PagedAttnPlan l{};
     const int rep = nh / nkv, cus = device_cus();
@@ -42,7 +66,7 @@ PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B,
     // 14 / 21, 4 x 64 on 700 21 / 22; heads of 64 8 x 48 on 100 8 / 11.6.
     const int64_t by_sixteen = sixteens * B * nkv;
     const bool fits = by_sixteen <= cus ? !cut || 2 * wgs >= cus : by_sixteen <= 2 * cus ? scaled <= (sixteens == 2 ? 4000 : 900) : by_sixteen <= 3 * cus && scaled <= 160;
-    l.chunk = cols > kDecodeCols && !fits;
+    l.chunk = cols > kDecodeCols && !(q4 ? decode4_pays(nh, nkv, d, T, B, max_new, seen, window > 0) : fits);
     // Both run where the call seems to hold sequences of either kind: the mean is far below the longest.
     l.decode = !l.chunk || (4 * static_cast<int64_t>(T) < static_cast<int64_t>(B) * max_new && rep <= kDecodeCols);
     l.cols = static_cast<int>(l.chunk ? std::min<int64_t>(kDecodeCols, cols) : cols);
