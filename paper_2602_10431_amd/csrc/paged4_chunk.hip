@@ -93,14 +93,14 @@ struct Unpack4 {
     // key0: the tile's first
     __device__ __forceinline__ void request_keys(int key0, int page) {
         const int lane = threadIdx.x & 63;
-        const uint32_t t = (key0 + 16 * part) & ((1 << p.shift) - 1);
+        const uint32_t t = __builtin_amdgcn_readfirstlane((key0 + 16 * part) & ((1 << p.shift) - 1));
         const auto buf = buffer(p.k, page);
         kw = load(buf, (lane >> 2) * (D / 2) + (lane & 3) * (D / 8), t * (D / 2));
         kp = __builtin_amdgcn_raw_buffer_load_b32(buf, 4 * (lane >> 2), params_at + 4 * t, 0);
     }
     __device__ __forceinline__ void request_values(int key0, int page) {
         const int lane = threadIdx.x & 63;
-        const uint32_t t = (key0 + 16 * part) & ((1 << p.shift) - 1);
+        const uint32_t t = __builtin_amdgcn_readfirstlane((key0 + 16 * part) & ((1 << p.shift) - 1));
         const auto buf = buffer(p.v, page);
         vw = load(buf, (lane >> 4) * (2 * D) + (lane & 15) * (D / 8), t * (D / 2));
         vp = __builtin_amdgcn_raw_buffer_load_b128(buf, 16 * (lane >> 4), params_at + 4 * t, 0);
@@ -163,8 +163,8 @@ struct Columns4 {
     static constexpr int DF = D / 32;            // output fragments
     static constexpr int PV = 4 * DF, ALL = PV + 2 * KS;
     int qi, head, place, reach;                  // this lane's column (clamped to a live one): query, head, its place, keys after `reach` are in its window
-    bool mine, plain;                            // the lane's column exists; all columns of the wave have up == 1
-    int w_first, w_last;                         // places of the wave's queries
+    bool mine;                                   // the lane's column exists
+    int whole_from, whole_to, first_to;          // a tile that every query of the wave sees whole begins in whole_from .. whole_to, or not after first_to
     u32x4_t qf[KS], pf[4];
     float up;                                    // the power of two that a score's unit stands for
     int k_at[KS], v_at[4];                       // LDS elements that this lane reads
@@ -173,7 +173,7 @@ struct Columns4 {
     int t_exp;                                   // log2 of t_ref
 
     // columns .. c_hi; c0: the wave's first
-    __device__ __forceinline__ Columns4(const PagedAttnDev& p, const SeqView& s, int hk, int c0, int c_hi) {
+    __device__ __forceinline__ Columns4(const PagedAttnDev& p, const SeqView& s, int hk, int c0, int c_hi, int hi) {
         const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
         const int col = min(c0 + l32, c_hi);
         qi = col / p.rep;
@@ -181,8 +181,10 @@ struct Columns4 {
         place = s.first + qi;
         reach = p.window > 0 ? place - p.window : INT32_MIN;
         mine = c0 + l32 <= c_hi;
-        w_first = s.first + __builtin_amdgcn_readfirstlane(min(c0, c_hi) / p.rep);   // (divisions run on the vector ALUs)
-        w_last = s.first + __builtin_amdgcn_readfirstlane(min(c0 + 31, c_hi) / p.rep);
+        // (divisions run on the vector ALUs)
+        whole_to = min(s.first + __builtin_amdgcn_readfirstlane(min(c0, c_hi) / p.rep) + 1, hi) - kTileKeys;
+        whole_from = p.window > 0 ? s.first + __builtin_amdgcn_readfirstlane(min(c0 + 31, c_hi) / p.rep) - p.window + 1 : 0;
+        first_to = p.sinks - kTileKeys;
         const uint16_t* qrow = p.q + (s.row0 + qi) * p.q_stride + head * D + 8 * lhi;
         float big = 0.0f;
 #pragma unroll
@@ -200,7 +202,6 @@ struct Columns4 {
 #pragma unroll
             for (int w = 0; w < 4; ++w) qf[k][w] = H::pack(Act16<BF16>::low(qf[k][w]) * (w & 1 ? f16 : f), Act16<BF16>::high(qf[k][w]) * (w & 1 ? f16 : f));
         up = ldexpf(1.0f, -move);
-        plain = __all(move == 0);
         // chunk 2 k + lhi of key l32; chunk 2 s2 + lhi of column 32 f + l32: v_at[(f ^ s2) & 3] + 32 f rows (the swizzle of that column is l32's with 2 f
         // flipped in)
 #pragma unroll
@@ -284,7 +285,7 @@ struct Columns4 {
             __builtin_amdgcn_sched_barrier(0);
         }
         // A tile that every query of the wave sees whole needs no mask.
-        const bool all = gone == 0 && key0 + kTileKeys <= min(w_first + 1, hi) && (p.window == 0 || key0 > w_last - p.window || key0 + kTileKeys <= p.sinks);
+        const bool all = (gone == 0) & (key0 <= whole_to) & ((key0 >= whole_from) | (key0 <= first_to));
         if (!all) {
             // of the lane's keys, key0 + quad + a constant each: constants up to `last` that are after `before`, or below `stay`
             const int last = min(place, hi - 1) - key0 - quad, before = max(reach, -1) - key0 - quad, stay = p.sinks - key0 - quad;
@@ -426,7 +427,7 @@ paged4_chunk_kernel(PagedAttnDev p) {
     Range4 range{0, walk.steps, 1};
     if (SPLIT) range = range_of<kChunkCols>(p, walk.steps, z);
     if (SPLIT && z >= range.ranges) return;
-    Cols cw(p, s, hk, c_lo + 32 * wave, c_hi);
+    Cols cw(p, s, hk, c_lo + 32 * wave, c_hi, walk.hi);
     const PageRow pages(p, s.slot);
     Unpack4<D, BF16> un(p, hk, wave, walk.hi);
     const int t0 = range.t0, t1 = range.t1;
@@ -496,7 +497,7 @@ paged4_wide_kernel(PagedAttnDev p) {
     Range4 range{0, walk.steps, 1};
     if (SPLIT) range = range_of<kWideCols>(p, walk.steps, z);
     if (SPLIT && z >= range.ranges) return;
-    Cols cw(p, s, hk, c_lo + 32 * wave, c_hi);
+    Cols cw(p, s, hk, c_lo + 32 * wave, c_hi, walk.hi);
     const PageRow pages(p, s.slot);
     Unpack4<D, BF16> un(p, hk, wave & 3, walk.hi);
     const int t0 = range.t0, n = range.t1 - range.t0;            // (tiles below are counted from t0)
