@@ -24,6 +24,7 @@ struct GemmDev {
     int streams;                   // GemmArgs::streams (few-row kernel)
     int chunk_rows;                // wide kernel: rows per chunk
     int ksplit;                    // decode kernel: parts K is cut into across workgroups (1 = none)
+    int out32;                     // GemmArgs::out_f32
     int epi_rt;                    // decode kernel: epilogue chosen at run time (GemmEpilogue)
     int tail;                      // 0: all rows; 1: all but gemm_tail_rows(); 2: only those last rows (small-row kernels)
     int M_full;                    // tail == 2: host bound on the row count of the whole matrix (M_max bounds the tail)
@@ -350,7 +351,9 @@ __device__ __forceinline__ void store_tile(const GemmDev& p, const float16_t (&a
             for (int u = 0; u < 4; ++u) {
                 if (!ok[u]) continue;
                 const int row = row0 + (ps + u) * RPP;
-                if (EPI == EPI_STORE_F16 || EPI == EPI_SWIGLU_F16) {
+                if (EPI == EPI_STORE_F16 && p.out32) {
+                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + static_cast<size_t>(row) * p.ldo + col) = v[u];
+                } else if (EPI == EPI_STORE_F16 || EPI == EPI_SWIGLU_F16) {
                     uint2 o;
                     o.x = static_cast<uint32_t>(float_to_half_bits(v[u].x)) | (static_cast<uint32_t>(float_to_half_bits(v[u].y)) << 16);
                     o.y = static_cast<uint32_t>(float_to_half_bits(v[u].z)) | (static_cast<uint32_t>(float_to_half_bits(v[u].w)) << 16);

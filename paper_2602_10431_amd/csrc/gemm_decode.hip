@@ -224,7 +224,7 @@ gemm_decode_kernel(GemmDev p) {
                 }
             }
             const int row = row0 + lrow;
-            if (p.epi_rt == EPI_PARTIAL_F32) {
+            if (p.epi_rt == EPI_PARTIAL_F32 || p.out32) {         // (all of K: part 0)
                 float* dst = reinterpret_cast<float*>(p.out) + (static_cast<size_t>(ks) * p.M_max + row) * p.ldo + col;
                 *reinterpret_cast<float4*>(dst) = v;
             } else {

@@ -344,6 +344,7 @@ gemm_few_kernel(FewDev a) {
         }
         const size_t col = static_cast<size_t>((SWIGLU ? 0 : p.colbase[e_mat[i]]) + e_n[i]);
         if (SWIGLU) reinterpret_cast<uint16_t*>(p.out)[static_cast<size_t>(er) * p.ldo + col] = float_to_half_bits(silu_f(v[0]) * v[1]);
+        else if (epi == EPI_STORE_F16 && p.out32) reinterpret_cast<float*>(p.out)[static_cast<size_t>(er) * p.ldo + col] = v[0];
         else if (epi == EPI_STORE_F16) reinterpret_cast<uint16_t*>(p.out)[static_cast<size_t>(er) * p.ldo + col] = float_to_half_bits(v[0]);
         else if (epi == EPI_RESID_F32) reinterpret_cast<float*>(p.out)[static_cast<size_t>(er) * p.ldo + col] = resid[i] + v[0];
         else reinterpret_cast<uint16_t*>(p.out)[static_cast<size_t>(trow) * p.ldo + col] = float_to_act(resid[i] + v[0], p.bf16);

@@ -205,7 +205,9 @@ gemm_skinny_kernel(GemmDev p) {
         if (EPI == EPI_SWIGLU_F16) {
             v.x = silu_f(v.x) * u.x; v.y = silu_f(v.y) * u.y; v.z = silu_f(v.z) * u.z; v.w = silu_f(v.w) * u.w;
         }
-        if (EPI == EPI_STORE_F16 || EPI == EPI_SWIGLU_F16) {
+        if (EPI == EPI_STORE_F16 && p.out32) {
+            *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + static_cast<size_t>(row) * p.ldo + col) = v;
+        } else if (EPI == EPI_STORE_F16 || EPI == EPI_SWIGLU_F16) {
             uint2 o;
             o.x = static_cast<uint32_t>(float_to_half_bits(v.x)) | (static_cast<uint32_t>(float_to_half_bits(v.y)) << 16);
             o.y = static_cast<uint32_t>(float_to_half_bits(v.z)) | (static_cast<uint32_t>(float_to_half_bits(v.w)) << 16);

@@ -487,6 +487,7 @@ hipError_t launch_gemm_w4a16(const GemmArgs& a, hipStream_t stream) {
     d.resid = a.resid;
     d.idx = a.idx;
     d.bf16 = a.bf16;
+    d.out32 = a.epilogue == EPI_STORE_F16 && a.out_f32;
     d.bits = a.bits;
     d.streams = a.streams;
     // Few rows: the weight stream dominates and 128-row tiles cannot fill the chip.  Each range has a kernel of its own:

@@ -240,7 +240,7 @@ gemm_wide_kernel(GemmDev p) {
                 const float4 u = v[m][FN - 1][ps];
                 o.x = silu_f(o.x) * u.x; o.y = silu_f(o.y) * u.y; o.z = silu_f(o.z) * u.z; o.w = silu_f(o.w) * u.w;
             }
-            if (!SWIGLU && p.epi_rt == EPI_PARTIAL_F32) {
+            if (!SWIGLU && (p.epi_rt == EPI_PARTIAL_F32 || p.out32)) {   // (all of K: part 0)
                 *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + (static_cast<size_t>(ks) * p.M_max + row) * p.ldo + col) = o;
             } else {
                 uint2 h;

@@ -28,10 +28,13 @@ size_t lora_inner_bytes(int R, int M);           // of one linear's inner values
 // product's operands.  What belongs to no adapter, or lies past a rank, is not written.  *operands, *parts (host out): of each linear, for the calls below
 hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, const void* A, float* const* inner, const float** operands, int* parts,
                              hipStream_t stream);
-// out (fp16, or fp32 if f32; ldo elements between rows) += scale up_a inner_i
-hipError_t launch_lora_add(const LoraDev& l, const LoraRows& rows, const float* operands, int parts, void* out, int ldo, int f32, hipStream_t stream);
-// out [M][N] = silu(gate + ...) * (up + ...); base [M][2 N] fp16: gate's columns, then up's
+// out (ldo elements between rows) += scale up_a inner_i
+hipError_t launch_lora_add(const LoraDev& l, const LoraRows& rows, const float* operands, int parts, float* out, int ldo, hipStream_t stream);
+// out (fp16, ldo elements between rows) = base (ldb) + scale up_a inner_i, rounded once; rows without an adapter (of l without any: all) are base, rounded
+hipError_t launch_lora_round(const LoraDev& l, const LoraRows& rows, const float* operands, int parts, const float* base, int ldb, void* out, int ldo,
+                             hipStream_t stream);
+// out [M][N] = silu(gate + ...) * (up + ...); base [M][2 N]: gate's columns, then up's
 hipError_t launch_lora_swiglu(const LoraDev& lg, const LoraDev& lu, const LoraRows& rows, const float* operands_g, const float* operands_u, int parts_g,
-                              int parts_u, const void* base, void* out, int N, hipStream_t stream);
+                              int parts_u, const float* base, void* out, int N, hipStream_t stream);
 
 }  // namespace qtale

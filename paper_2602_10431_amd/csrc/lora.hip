@@ -226,11 +226,12 @@ struct LoraOuter {
     const float* inner[2];
     int parts[2];
     LoraRows rows;
-    const uint16_t* base;        // swiglu: [M][2 N]
+    const float* base;           // (what is added to, elsewhere) [M][ldb], ldb at least 2 N for swiglu
+    int ldb;
     void* out;
     int ldo;
 };
-enum { LORA_ADD_F16, LORA_ADD_F32, LORA_SWIGLU };
+enum { LORA_ROUND, LORA_ADD_F32, LORA_SWIGLU };
 
 // A wave's products of 16 NT columns from n0 on: product j has columns n0 + 4 NT (i / 4) + 4 j + i % 4, i < 16, so that lane (c, g), which gets i = 4 g .. 4 g + 3
 // of each, has 4 NT columns in a row of the matrix that it reads and writes.
@@ -274,36 +275,42 @@ template <> struct OuterRow<LORA_ADD_F32> {
         to[1] = old[1] + y[1];
     }
 };
-__device__ __forceinline__ float half_of(const u32x4_t& w, int e) { return half_bits_to_float(static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)) & 0xffffu)); }
 __device__ __forceinline__ u32x4_t halves(const float* y) {
     u32x4_t w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = to_half(y[2 * e]) | static_cast<uint32_t>(to_half(y[2 * e + 1])) << 16;
     return w;
 }
-template <> struct OuterRow<LORA_ADD_F16> {
-    u32x4_t old;
-    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) { old = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p.out) + row * p.ldo + n); }
+template <> struct OuterRow<LORA_ROUND> {
+    float4_t old[2];
+    __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int) {
+        const float4_t* from = reinterpret_cast<const float4_t*>(p.base + row * p.ldb + n);
+        old[0] = from[0];
+        old[1] = from[1];
+    }
     __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t* y, const float4_t*) const {
         float sum[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = half_of(old, e) + y[e >> 2][e & 3];
+        for (int e = 0; e < 8; ++e) sum[e] = old[e >> 2][e & 3] + y[e >> 2][e & 3];
         *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(sum);
     }
 };
 template <> struct OuterRow<LORA_SWIGLU> {
-    u32x4_t gate, up;
+    float4_t gate[2], up[2];
     __device__ __forceinline__ void read(const LoraOuter& p, size_t row, int n, int N) {
-        const uint16_t* from = p.base + row * 2 * N + n;
-        gate = *reinterpret_cast<const u32x4_t*>(from);
-        up = *reinterpret_cast<const u32x4_t*>(from + N);
+        const float* from = p.base + row * p.ldb + n;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            gate[h] = reinterpret_cast<const float4_t*>(from)[h];
+            up[h] = reinterpret_cast<const float4_t*>(from + N)[h];
+        }
     }
     __device__ __forceinline__ void write(const LoraOuter& p, size_t row, int n, const float4_t* yg, const float4_t* yu) const {
         float out[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float x = half_of(gate, e) + yg[e >> 2][e & 3];
-            out[e] = x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)) * (half_of(up, e) + yu[e >> 2][e & 3]);   // (off by 2^-22 or so)
+            const float x = gate[e >> 2][e & 3] + yg[e >> 2][e & 3];
+            out[e] = x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)) * (up[e >> 2][e & 3] + yu[e >> 2][e & 3]);   // (off by 2^-22 or so)
         }
         *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n) = halves(out);
     }
@@ -324,7 +331,7 @@ lora_few_kernel(LoraOuter p, int steps) {
     __shared__ float units[NL][16];
     const int mine = choice_of(p.rows, row0 + lane, lane < 16 ? M : 0);   // lane x: row x of the tile
     // rows that there are (and have something to add, where nothing else is done), then those of the blockIdx.z-th choice
-    uint64_t rows = __ballot(lane < 16 && row0 + lane < M && (FORM == LORA_SWIGLU || adapter_of(p.l[0], mine) >= 0));
+    uint64_t rows = __ballot(lane < 16 && row0 + lane < M && (FORM != LORA_ADD_F32 || adapter_of(p.l[0], mine) >= 0));
     int choice = -1;
     for (int skip = blockIdx.z; rows != 0; --skip) {
         choice = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(rows)) - 1));
@@ -428,7 +435,7 @@ lora_many_kernel(LoraOuter p) {
     Rows now, next;
     read(0, now);
     const int mine = choice_of(p.rows, row0 + lane, M);          // lane x: row x of the 64
-    const uint64_t rows = __ballot(row0 + lane < M && (FORM == LORA_SWIGLU || adapter_of(p.l[0], mine) >= 0));
+    const uint64_t rows = __ballot(row0 + lane < M && (FORM != LORA_ADD_F32 || adapter_of(p.l[0], mine) >= 0));
     u32x4_t w[NL][NT][NS], mask[NL][NS];
     int held[NL];                                                // the adapter whose part of up is there
 #pragma unroll
@@ -560,17 +567,23 @@ static hipError_t outer_form(const LoraOuter& p, int R, int N, hipStream_t strea
     return hipGetLastError();
 }
 
-hipError_t launch_lora_add(const LoraDev& l, const LoraRows& rows, const float* inner, int parts, void* out, int ldo, int f32, hipStream_t stream) {
+hipError_t launch_lora_add(const LoraDev& l, const LoraRows& rows, const float* inner, int parts, float* out, int ldo, hipStream_t stream) {
     LoraOuter p{};
     p.l[0] = l; p.inner[0] = inner; p.parts[0] = parts; p.rows = rows; p.out = out; p.ldo = ldo;
-    return f32 ? outer_form<LORA_ADD_F32>(p, l.R, l.N, stream) : outer_form<LORA_ADD_F16>(p, l.R, l.N, stream);
+    return outer_form<LORA_ADD_F32>(p, l.R, l.N, stream);
+}
+hipError_t launch_lora_round(const LoraDev& l, const LoraRows& rows, const float* inner, int parts, const float* base, int ldb, void* out, int ldo,
+                             hipStream_t stream) {
+    LoraOuter p{};
+    p.l[0] = l; p.inner[0] = inner; p.parts[0] = parts; p.rows = rows; p.base = base; p.ldb = ldb; p.out = out; p.ldo = ldo;
+    return outer_form<LORA_ROUND>(p, l.R, l.N, stream);
 }
 
 hipError_t launch_lora_swiglu(const LoraDev& lg, const LoraDev& lu, const LoraRows& rows, const float* inner_g, const float* inner_u, int parts_g, int parts_u,
-                              const void* base, void* out, int N, hipStream_t stream) {
+                              const float* base, void* out, int N, hipStream_t stream) {
     LoraOuter p{};
     p.l[0] = lg; p.l[1] = lu; p.inner[0] = inner_g; p.inner[1] = inner_u; p.parts[0] = parts_g; p.parts[1] = parts_u;
-    p.rows = rows; p.base = static_cast<const uint16_t*>(base); p.out = out; p.ldo = N;
+    p.rows = rows; p.base = base; p.ldb = 2 * N; p.out = out; p.ldo = N;
     return outer_form<LORA_SWIGLU>(p, std::max(lg.R, lu.R), N, stream);
 }
 

@@ -27,17 +27,17 @@ int check_lora_call(const int32_t* adapter, const void* A, const void* out, cons
     return have < need ? QTALE_ERR_WORKSPACE_TOO_SMALL : QTALE_OK;
 }
 
-// The shared product alone, of one linear or of two side by side ([M][2 N]).
-hipError_t base_linear(const qtale_qlinear* w, const qtale_qlinear* w2, int bits, int group, const void* A, int M, void* out, hipStream_t stream) {
+// The shared product alone in fp32 (it is rounded with what the adapters add), of one linear or of two side by side ([M][2 N]).
+hipError_t base_linear(const qtale_qlinear* w, const qtale_qlinear* w2, int bits, int group, const void* A, int M, float* out, hipStream_t stream) {
     GemmArgs g{};
     g.A = A; g.M_max = M; g.rows_exact = 1; g.K = w->K; g.group = group; g.bits = bits; g.n_w = w2 ? 2 : 1;
     g.w[0] = {w->prepacked, w->N, w->K};
     if (w2) g.w[1] = {w2->prepacked, w2->N, w2->K};
-    g.epilogue = EPI_STORE_F16; g.out = out; g.ldo = w->N * g.n_w;
+    g.epilogue = EPI_STORE_F16; g.out_f32 = 1; g.out = out; g.ldo = w->N * g.n_w;
     return launch_gemm_w4a16(g, stream);
 }
 
-size_t rows_bytes(int M, int N) { return (static_cast<size_t>(M) * N * 2 + 255) / 256 * 256; }
+size_t rows_bytes(int M, int N) { return (static_cast<size_t>(M) * N * 4 + 255) / 256 * 256; }
 size_t inner_bytes(const qtale_lora* l, int M) { return l ? lora_inner_bytes(l->max_rank, M) : 0; }
 
 }  // namespace
@@ -46,7 +46,7 @@ extern "C" {
 
 size_t qtale_lora_workspace_bytes(const qtale_lora* a, const qtale_lora* b, int M) {
     if (!a || check_lora(a, a->N, a->K, false) || (b && check_lora(b, a->N, a->K, false)) || M < 0 || a->N <= 0 || a->K <= 0) return 0;
-    return 256 + inner_bytes(a, M) + inner_bytes(b, M) + (b ? 2 * rows_bytes(M, a->N) : 0);
+    return 256 + inner_bytes(a, M) + inner_bytes(b, M) + (b ? 2 : 1) * rows_bytes(M, a->N);
 }
 
 int qtale_linear_lora_w4a16(const qtale_qlinear* w, int bits, int group, const qtale_lora* lora, const int32_t* adapter, const void* A, int M,
@@ -64,8 +64,9 @@ int qtale_linear_lora_w4a16(const qtale_qlinear* w, int bits, int group, const q
     const float* operands = nullptr;
     int parts = 0;
     HIP_TRY(launch_lora_inner(&l, 1, rows, A, &inner, &operands, &parts, s));
-    HIP_TRY(base_linear(w, nullptr, bits, group, A, M, out, s));
-    HIP_TRY(launch_lora_add(l, rows, operands, parts, out, w->N, 0, s));
+    float* base = reinterpret_cast<float*>(static_cast<char*>(workspace) + inner_bytes(lora, M));
+    HIP_TRY(base_linear(w, nullptr, bits, group, A, M, base, s));
+    HIP_TRY(launch_lora_round(l, rows, operands, parts, base, w->N, out, w->N, s));
     return QTALE_OK;
 }
 
@@ -90,7 +91,7 @@ int qtale_swiglu_lora_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, 
     char* at = static_cast<char*>(workspace);
     float* inner_g = reinterpret_cast<float*>(at);
     float* inner_u = reinterpret_cast<float*>(at += inner_bytes(lora_gate, M));
-    void* base = at += inner_bytes(lora_up, M);
+    float* base = reinterpret_cast<float*>(at += inner_bytes(lora_up, M));
     LoraDev l[2];
     float* inner[2];
     const float* operands[2] = {nullptr, nullptr};

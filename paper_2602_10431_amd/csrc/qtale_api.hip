@@ -229,7 +229,7 @@ struct LoraCall {
     const qtale_layer_lora* layer;
     const int32_t* adapter;                     // [B]
     float* inner[kLoraMost];
-    void* pair;                                 // [rows][2 inter] fp16: gate and up before their product
+    float* base;                                // [rows][q|k|v, or gate|up]: shared products that adapters' are added to before they are rounded
 };
 
 // Inner values of those of `n` linears of one input that have adapters (`at`: which of them).
@@ -389,14 +389,18 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
     int o_parts = 0;
     {
         Prof pr(ctx, stream, 3);
+        const bool adapted = lora && (lora->layer->q.n_adapters > 0 || lora->layer->k.n_adapters > 0 || lora->layer->v.n_adapters > 0);
+        if (adapted) { qg.out = lora->base; qg.out_f32 = 1; }
         HIP_TRY(launch_gemm_w4a16(qg, stream));
-        if (lora) {
+        if (adapted) {
             const qtale_lora* which[3] = {&lora->layer->q, &lora->layer->k, &lora->layer->v};
             const int columns[3] = {0, nh * d, (nh + nkv) * d};
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 3, lora_rows, ws.nbuf, &in, stream));
-            for (int i = 0; i < 3; ++i)
-                if (in.l[i].n) HIP_TRY(launch_lora_add(in.l[i], lora_rows, in.operands[i], in.parts[i], reinterpret_cast<uint16_t*>(ws.qkv) + columns[i], qkv_w, 0, stream));
+            for (int i = 0; i < 3; ++i) {
+                in.l[i].N = (i ? nkv : nh) * d;                  // (also of one without adapters)
+                HIP_TRY(launch_lora_round(in.l[i], lora_rows, in.operands[i], in.parts[i], lora->base + columns[i], qkv_w, reinterpret_cast<uint16_t*>(ws.qkv) + columns[i], qkv_w, stream));
+            }
         }
     }
     // Prefill attention: the work list comes from the launch before it, the partial sums of key ranges go to what lies free until
@@ -447,7 +451,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             const qtale_lora* which[1] = {&lora->layer->o};
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 1, lora_rows, ws.attn, &in, stream));
-            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.operands[0], in.parts[0], ws.h, H, 1, stream));
+            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.operands[0], in.parts[0], ws.h, H, stream));
         }
     }
     if (!few_fused) {
@@ -470,13 +474,13 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             g.pro = &pro;
         }
         const bool adapted = lora && (lora->layer->gate.n_adapters > 0 || lora->layer->up.n_adapters > 0);
-        if (adapted) { g.epilogue = EPI_STORE_F16; g.out = lora->pair; g.ldo = 2 * I; }
+        if (adapted) { g.epilogue = EPI_STORE_F16; g.out_f32 = 1; g.out = lora->base; g.ldo = 2 * I; }
         HIP_TRY(launch_gemm_w4a16(g, stream));
         if (adapted) {
             const qtale_lora* which[2] = {&lora->layer->gate, &lora->layer->up};
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 2, lora_rows, ws.nbuf, &in, stream));
-            HIP_TRY(launch_lora_swiglu(in.l[0], in.l[1], lora_rows, in.operands[0], in.operands[1], in.parts[0], in.parts[1], lora->pair, ws.act, I, stream));
+            HIP_TRY(launch_lora_swiglu(in.l[0], in.l[1], lora_rows, in.operands[0], in.operands[1], in.parts[0], in.parts[1], lora->base, ws.act, I, stream));
         }
     }
     {
@@ -485,7 +489,7 @@ int layer_forward_impl(qtale_ctx* ctx, const qtale_layer_cfg* c, const qtale_lay
             const qtale_lora* which[1] = {&lora->layer->down};
             LoraInners in;
             HIP_TRY(lora_inners(*lora, which, 1, lora_rows, ws.act, &in, stream));
-            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.operands[0], in.parts[0], ws.h, H, 1, stream));
+            HIP_TRY(launch_lora_add(in.l[0], lora_rows, in.operands[0], in.parts[0], ws.h, H, stream));
         }
         GemmArgs g{};
         g.A = ws.act; g.count = count; g.M_max = M_max; g.rows_exact = ratio_mode; g.streams = streams; g.K = I; g.group = c->group; g.bits = lbits; g.n_w = 1;
@@ -768,7 +772,7 @@ size_t qtale_paged_stack_workspace_bytes(const qtale_layer_cfg* cfg, const qtale
 namespace {
 
 size_t lora_stack_bytes(const qtale_layer_cfg* cfg, int max_rank, int max_tokens) {
-    return kLoraMost * lora_inner_bytes(max_rank, max_tokens) + align_up(static_cast<size_t>(max_tokens) * 2 * cfg->inter * 2, 256);
+    return kLoraMost * lora_inner_bytes(max_rank, max_tokens) + align_up(static_cast<size_t>(max_tokens) * std::max(2 * cfg->inter, (cfg->n_heads + 2 * cfg->n_kv_heads) * cfg->head_dim) * 4, 256);
 }
 
 int check_layer_lora(const qtale_layer_cfg* c, const qtale_layer_lora* l, int* max_rank) {
@@ -811,7 +815,7 @@ int paged_stack(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_we
         char* at = reinterpret_cast<char*>(workspace) + stack_bytes;
         lc.adapter = adapter;
         for (int i = 0; i < kLoraMost; ++i, at += lora_inner_bytes(max_rank, T)) lc.inner[i] = reinterpret_cast<float*>(at);
-        lc.pair = at;
+        lc.base = reinterpret_cast<float*>(at);
     }
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Workspace ws = carve(cfg, T, B, workspace);

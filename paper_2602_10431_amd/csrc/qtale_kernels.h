@@ -151,6 +151,7 @@ struct GemmArgs {
     int n_w;                   // number of weight matrices: 1, 2 (gate/up interleaved), 3 (q|k|v concatenated)
     GemmWeights w[3];
     int epilogue;
+    int out_f32;               // with EPI_STORE_F16: fp32 is stored
     void* out;                 // STORE/SWIGLU: fp16 [M][ldo]; RESID_F32: fp32 [M][ldo]; RESID_SCATTER: act dtype x [T][ldo]
     int ldo;
     const void* resid;         // RESID_F32: x (act dtype, rows via idx); RESID_SCATTER: h fp32 [M][ldo]

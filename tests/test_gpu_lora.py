@@ -35,17 +35,17 @@ def _adapters(qt, n, r, N, K, seed, ranks=None, scales=True, fill=None):
     return qt.Lora(down, up, rank, scale), down, up
 
 
-# Errors: the shared product in 32 bits and rounded to fp16, 2^-11 of it; the inner values in 32 bits (K products, their magnitudes' sum times 2^-24 (K
-# / 64 + 8), as 64 or more lanes add side by side) and as operands 2^-11 of each; the sum of up to 128 products 2^-24 * 130 of its magnitudes; the sum once
-# more to fp16, 2^-11 of it.  Weights of the shared product go into the matrix cores as fp16 (code - zero) * scale, 2^-11 each, its sums of K in 32 bits.
-def _expect(base, lora, down, up, x, ids):
+# Errors: the shared product in 32 bits; the inner values in 32 bits (K products, their magnitudes' sum times 2^-24 (K / 64 + 8), as 64 or more lanes add
+# side by side) and as operands 2^-11 of each; the sum of up to 128 products 2^-24 * 130 of its magnitudes; the sum of both, rounded once to fp16, 2^-11 of
+# it.  Weights of the shared product go into the matrix cores as fp16 (code - zero) * scale, 2^-11 each, its sums of K in 32 bits.
+def _expect(base, lora, down, up, x, ids, rounded=True):
     """(y, bound) in float64"""
     U = 2.0 ** -11
     xd, n = x.double(), down.shape[0]
     y = xd @ base.t()
     size = xd.abs() @ base.abs().t()
     K = x.shape[1]
-    bound = U * y.abs() + (U + 2.0 ** -24 * (K / 64 + 8)) * size
+    bound = (U + 2.0 ** -24 * (K / 64 + 8)) * size
     for a in range(n):
         rows = (ids == a).nonzero()[:, 0]
         if rows.numel() == 0:
@@ -58,7 +58,7 @@ def _expect(base, lora, down, up, x, ids):
         bound[rows] += s * ((U + 2.0 ** -24 * 132) * inner.abs() + 2.0 ** -24 * (K / 64 + 8) * big) @ u.abs().t()
         # (as fp16 of their row's power of two, inner values far below the row's largest keep 2^-25 of it)
         bound[rows] += s * 2.0 ** -24 * (inner.abs().amax(1, keepdim=True) if r else 0.0) * u.abs().sum(1)
-    return y, bound + U * y.abs() + 2.0 ** -24
+    return y, bound + (U * y.abs() + 2.0 ** -24 if rounded else 2.0 ** -24 * y.abs())
 
 
 def _ids(pattern, M, n, seed):
@@ -91,6 +91,28 @@ def test_linear(qt, N, K, group, M):
             assert torch.equal(got, qt.qtale_linear_w4a16(q, x))
 
 
+@pytest.mark.parametrize("M", [1, 20, 64, 200, 300, 700])
+def test_what_is_added_is_not_rounded_before(qt, M):
+    # Sums of a whole number and a fraction that fp16 cannot hold, from which the adapter takes the whole number again: the fraction is left, exactly.
+    K = N = 128
+    codes = torch.zeros(N, K, dtype=torch.int64)
+    n = torch.arange(N)
+    codes[n, n], codes[n, (n + 1) % K] = 1, 1
+    words = (codes.view(N, K // 8, 8) << (4 * torch.arange(8))).sum(2)
+    words = (words - ((words >> 31) << 32)).int().cuda()
+    q = qt.qtale_prepack(words, torch.ones(N, 1).half().cuda(), torch.zeros(N, 1).half().cuda(), N, K, 4, 128)
+    g = torch.Generator().manual_seed(M)
+    x = torch.empty(M, K)
+    x[:, 0::2] = torch.randint(1024, 2048, (M, K // 2), generator=g).float()
+    x[:, 1::2] = torch.randint(1, 1024, (M, K // 2), generator=g) / 1024
+    x = x.half().cuda()
+    up = torch.zeros(1, N, K)
+    up[0, n, (n + n % 2) % K] = -1.0
+    lora = qt.Lora(torch.eye(K).half().cuda()[None].contiguous(), up.half().cuda(), None, None)
+    out = qt.qtale_linear_lora_w4a16(q, lora, x, torch.zeros(M, dtype=torch.int32).cuda())
+    assert torch.equal(out, x[:, (n + 1 - n % 2).cuda()])
+
+
 @pytest.mark.parametrize("r", [1, 2, 7, 8, 15, 16, 17, 24, 32, 33, 61, 64, 100, 128])
 def test_ranks(qt, r):
     N, K = 328, 200
@@ -114,13 +136,13 @@ def test_gated(qt, bits, M):
     lu, du, uu = _adapters(qt, 9, 24, N, K, 4)                    # another pool, more adapters, another rank
     x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).half().cuda()
     ids = _ids("mixed", M, 9, M)
-    (g, bg), (u, bu) = _expect(pairs[0][1], lg, dg, ug, x, ids), _expect(pairs[1][1], lu, du, uu, x, ids)
+    (g, bg), (u, bu) = _expect(pairs[0][1], lg, dg, ug, x, ids, False), _expect(pairs[1][1], lu, du, uu, x, ids, False)
     only = torch.full_like(ids, -1)
     for a, b in ((lg, lu), (lg, None), (None, lu)):
         if a is None:
-            g, bg = _expect(pairs[0][1], lg, dg, ug, x, only)
+            g, bg = _expect(pairs[0][1], lg, dg, ug, x, only, False)
         if b is None:
-            (u1, bu1) = _expect(pairs[1][1], lu, du, uu, x, only)
+            (u1, bu1) = _expect(pairs[1][1], lu, du, uu, x, only, False)
         else:
             u1, bu1 = u, bu
         got = qt.qtale_swiglu_lora_w4a16(pairs[0][0], pairs[1][0], a, b, x, ids)
