@@ -1,12 +1,12 @@
 // Low-rank adapters of many requests beside a shared projection: y_i += scale[a] up_a (down_a A_i), a the adapter of row i.
 //
-// Both products run on the matrix cores in tiles of 16 rows that know nothing of the rows' order: a tile walks the adapters that occur in it, and a
+// Both products run on the matrix cores in tiles of 16 rows (or 64) that know nothing of the rows' order: a tile walks the adapters that occur in it, and a
 // row takes the result of its own and leaves the others'.  A decode step's tile of 16 requests reads each of its adapters once, which has to be; a
 // prompt's tile meets one.  Operands of rows that the result leaves out cannot reach it, whatever they hold (a select, not a product with zero).
-//   inner  D[r][row] = down_a A^T, K cut over the waves of a workgroup and over workgroups, so that a few requests fill the chip;
+//   inner  D[r][row] = down_a A^T, K cut over the waves of a workgroup and over workgroups (lora_splits), so that a few requests fill the chip;
 //          a part's sums are written, and added by the second kernel: no atomics, the same bits every time
-//   outer  D[n][row] = up_a inner^T: inner values go in as fp16 relative to their row's power of two, off by 2^-11 of each (or 2^-36 of the
-//          row's largest), as the rows that they come from are; the sum with the shared product, which stays in 32 bits until then, is rounded once
+//   outer  D[n][row] = up_a inner^T: inner values go in as fp16 relative to their row's power of two, off by 2^-12 of each (or 2^-36 of the
+//          row's largest): less than the rounding of the result they are added to
 #include <algorithm>
 
 #include "lora.h"
@@ -41,46 +41,53 @@ struct LoraInner {
     int parts;
 };
 
-// One workgroup of NW waves per (16 rows, part of K[, adapter of the tile]); NR tiles of 16 inner values.  ALONE: each adapter of the tile has its own
-// workgroup.  (Tiles of 64 rows read less of down where a request has many: 3800 rows in requests of 200, 14336 -> 4096, 465 us for the whole linear
-// instead of 470; but 3000 rows that all choose for themselves take 1385 instead of 1068.)
-template <int NR, int NW, bool ALONE>
+// One workgroup of NW waves per (16 RT rows, part of K[, adapter of the tile]); NR tiles of 16 inner values.  ALONE: each adapter of the tile has its own
+// workgroup.
+template <int RT, int NR, int NW, bool ALONE>
 __global__ void __launch_bounds__(64 * NW)
 lora_inner_kernel(LoraInner p) {
     const LoraDev& l = p.l[blockIdx.z];
     const int M = p.rows.count ? min(*p.rows.count, p.rows.M) : p.rows.M;
-    const int row0 = blockIdx.x * 16, part = ALONE ? blockIdx.y >> 4 : blockIdx.y;
+    const int row0 = blockIdx.x * (16 * RT), part = ALONE ? blockIdx.y >> 4 : blockIdx.y;
     if (row0 >= M) return;
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    __shared__ float4_t sums[NW - 1][NR][64];
-    const int mine = adapter_of(l, choice_of(p.rows, row0 + lane, lane < 16 ? M : 0));   // lane x: row x of the tile
-    const int own = __shfl(mine, c, 64);                         // of this lane's column, row c
+    __shared__ float4_t sums[NW - 1][RT * NR][64];
+    const int mine = adapter_of(l, choice_of(p.rows, row0 + lane, lane < 16 * RT ? M : 0));   // lane x: row x of the tile
+    int own[RT];                                                 // this lane's columns: rows c, 16 + c, ...
+#pragma unroll
+    for (int t = 0; t < RT; ++t) own[t] = __shfl(mine, 16 * t + c, 64);
     uint64_t left = __ballot(mine >= 0);
     int skip = ALONE ? blockIdx.y & 15 : 0;
     const int units = (l.K + 127) / 128, step = NW * p.parts;    // units of 128 columns of K: this wave's are part * NW + wave, + step, ...
     const size_t stride = static_cast<size_t>(p.rows.M) * l.R;
-    const uint16_t* row_at = p.A + static_cast<size_t>(min(row0 + c, M - 1)) * l.K;
+    const uint16_t* rows_at[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) rows_at[t] = p.A + static_cast<size_t>(min(row0 + 16 * t + c, M - 1)) * l.K;
     while (left != 0) {
         const int a = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(left)) - 1));
         left &= ~__ballot(mine == a);
         if (ALONE && skip-- > 0) continue;
         const int rank = rank_of(l, a);
         const uint16_t* down = l.down + static_cast<size_t>(a) * l.R * l.K;
-        float4_t acc[NR];
+        float4_t acc[RT][NR];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) acc[r] = float4_t{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) acc[t][r] = float4_t{0.f, 0.f, 0.f, 0.f};
         for (int u = part * NW + wave; u < units; u += step) {
-            half8_t x[4], w[4][NR];
+            half8_t x[4][RT], w[4][NR];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int k = u * 128 + 32 * j + 8 * g;
                 const bool in = k < l.K;                         // (K is a multiple of 8)
-                x[j] = *reinterpret_cast<const half8_t*>(row_at + (in ? k : 0));
+#pragma unroll
+                for (int t = 0; t < RT; ++t) x[j][t] = *reinterpret_cast<const half8_t*>(rows_at[t] + (in ? k : 0));
 #pragma unroll
                 for (int r = 0; r < NR; ++r) w[j][r] = *reinterpret_cast<const half8_t*>(down + static_cast<size_t>(min(16 * r + c, l.R - 1)) * l.K + (in ? k : 0));
                 if (!in) {
-                    x[j] = half8_t{};
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) x[j][t] = half8_t{};
 #pragma unroll
                     for (int r = 0; r < NR; ++r) w[j][r] = half8_t{};
                 }
@@ -88,24 +95,30 @@ lora_inner_kernel(LoraInner p) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int r = 0; r < NR; ++r) acc[r] = mfma(w[j][r], x[j], acc[r]);
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) acc[t][r] = mfma(w[j][r], x[j][t], acc[t][r]);
         }
         // the waves meet in LDS; the first writes
         if (wave > 0) {
 #pragma unroll
-            for (int r = 0; r < NR; ++r) sums[wave - 1][r][lane] = acc[r];
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) sums[wave - 1][t * NR + r][lane] = acc[t][r];
         }
         __syncthreads();
         if (wave == 0) {
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                float4_t y = acc[r];
+            for (int t = 0; t < RT; ++t)
 #pragma unroll
-                for (int w = 0; w < NW - 1; ++w) y += sums[w][r][lane];
-                // lane (c, g): row c, inner values 16 r + 4 g .. + 3 (R is a multiple of 8)
-                if (own == a && 16 * r + 4 * g < rank)
-                    *reinterpret_cast<float4_t*>(p.inner[blockIdx.z] + part * stride + static_cast<size_t>(row0 + c) * l.R + 16 * r + 4 * g) = y;
-            }
+                for (int r = 0; r < NR; ++r) {
+                    float4_t y = acc[t][r];
+#pragma unroll
+                    for (int w = 0; w < NW - 1; ++w) y += sums[w][t * NR + r][lane];
+                    // lane (c, g): row c, inner values 16 r + 4 g .. + 3 (R is a multiple of 8)
+                    if (own[t] == a && 16 * r + 4 * g < rank)
+                        *reinterpret_cast<float4_t*>(p.inner[blockIdx.z] + part * stride + static_cast<size_t>(row0 + 16 * t + c) * l.R + 16 * r + 4 * g) = y;
+                }
         }
         if (ALONE) return;
         __syncthreads();
@@ -464,28 +477,26 @@ lora_many_kernel(LoraOuter p) {
     }
 }
 
-// Rows up to which they are taken to choose differently: a workgroup per choice of a tile's rows, instead of one that walks them.  us, the whole linear, with /
-// without, 4096 -> 4096: 200 rows with 60 adapters 42.5 / 88, in requests of 40 rows 40 / 42; 500 rows with 60 adapters 68 / 94, in requests of 100
-// rows 45.7 / 43.5; 900 rows 99 / 116, in requests of 90 74 / 69.  (So many rows are mostly prompts.)
-constexpr int kLoraAlone = 256;
+constexpr int kLoraAlone = 256;  // rows up to which they are taken to choose differently
 
 // Parts of K: workgroups that fill the chip, each wave with a unit of 128 columns at least.
 constexpr int kManyFill = 512;
+static int inner_tile(int M) { return M <= 2048 ? 16 : 64; }
 static int inner_parts(int M, int K, int n) {
     const int units = (K + 127) / 128;
     if (M <= kLoraAlone) return std::min(std::max(units / 8, 1), 4);
-    const int wgs = (M + 15) / 16 * n;
+    const int wgs = (M + inner_tile(M) - 1) / inner_tile(M) * n;
     return std::min(std::min((kManyFill + wgs - 1) / wgs, 8), std::max(units / 4, 1));
 }
 size_t lora_inner_bytes(int R, int M) {
-    // enough for any number of rows up to M: parts * M <= 8 M, and <= 16 kManyFill + M
-    const size_t rows = std::min<size_t>(static_cast<size_t>(8) * M, static_cast<size_t>(kManyFill) * 16 + M);
+    // enough for any number of rows up to M: parts * M <= 8 M, and <= 64 kManyFill + M
+    const size_t rows = std::min<size_t>(static_cast<size_t>(8) * M, static_cast<size_t>(kManyFill) * 64 + M);
     return (rows * R * 4 + 255) / 256 * 256 + (static_cast<size_t>(M) * (2 * operand_width(R) + 4) + 255) / 256 * 256;
 }
 
-template <int NR, int NW, bool ALONE>
+template <int RT, int NR, int NW, bool ALONE>
 static void inner_launch(const LoraInner& p, int tiles, int n, hipStream_t stream) {
-    hipLaunchKernelGGL((lora_inner_kernel<NR, NW, ALONE>), dim3(tiles, (ALONE ? 16 : 1) * p.parts, n), dim3(64 * NW), 0, stream, p);
+    hipLaunchKernelGGL((lora_inner_kernel<RT, NR, NW, ALONE>), dim3(tiles, (ALONE ? 16 : 1) * p.parts, n), dim3(64 * NW), 0, stream, p);
 }
 
 hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, const void* A, float* const* inner, const float** operands, int* parts,
@@ -500,17 +511,24 @@ hipError_t launch_lora_inner(const LoraDev* l, int n, const LoraRows& rows, cons
     p.rows = rows; p.A = static_cast<const uint16_t*>(A);
     p.parts = inner_parts(rows.M, l[0].K, n);
     for (int i = 0; i < n; ++i) parts[i] = p.parts;
-    const int tiles = (rows.M + 15) / 16;
+    // Few rows, whose adapters mostly differ: a workgroup per adapter of the tile.  Many: a tile's adapters one after the
+    // other, mostly one.
+    const int tile = inner_tile(rows.M), tiles = (rows.M + tile - 1) / tile;
     if (rows.M <= kLoraAlone) {
-        if (R <= 16) inner_launch<1, 8, true>(p, tiles, n, stream);
-        else if (R <= 32) inner_launch<2, 8, true>(p, tiles, n, stream);
-        else if (R <= 64) inner_launch<4, 8, true>(p, tiles, n, stream);
-        else inner_launch<8, 8, true>(p, tiles, n, stream);
+        if (R <= 16) inner_launch<1, 1, 8, true>(p, tiles, n, stream);
+        else if (R <= 32) inner_launch<1, 2, 8, true>(p, tiles, n, stream);
+        else if (R <= 64) inner_launch<1, 4, 8, true>(p, tiles, n, stream);
+        else inner_launch<1, 8, 8, true>(p, tiles, n, stream);
+    } else if (tile == 16) {
+        if (R <= 16) inner_launch<1, 1, 4, false>(p, tiles, n, stream);
+        else if (R <= 32) inner_launch<1, 2, 4, false>(p, tiles, n, stream);
+        else if (R <= 64) inner_launch<1, 4, 4, false>(p, tiles, n, stream);
+        else inner_launch<1, 8, 4, false>(p, tiles, n, stream);
     } else {
-        if (R <= 16) inner_launch<1, 4, false>(p, tiles, n, stream);
-        else if (R <= 32) inner_launch<2, 4, false>(p, tiles, n, stream);
-        else if (R <= 64) inner_launch<4, 4, false>(p, tiles, n, stream);
-        else inner_launch<8, 4, false>(p, tiles, n, stream);
+        if (R <= 16) inner_launch<4, 1, 4, false>(p, tiles, n, stream);
+        else if (R <= 32) inner_launch<4, 2, 4, false>(p, tiles, n, stream);
+        else if (R <= 64) inner_launch<4, 4, 4, false>(p, tiles, n, stream);
+        else inner_launch<4, 8, 4, false>(p, tiles, n, stream);
     }
     if (rows.M > kLoraAlone) {                                   // the sums become operands, behind the parts
         LoraPack k{};
