@@ -3,10 +3,10 @@
 // Both products run on the matrix cores in tiles of 16 rows (or 64) that know nothing of the rows' order: a tile walks the adapters that occur in it, and a
 // row takes the result of its own and leaves the others'.  A decode step's tile of 16 requests reads each of its adapters once, which has to be; a
 // prompt's tile meets one.  Operands of rows that the result leaves out cannot reach it, whatever they hold (a select, not a product with zero).
-//   inner  D[r][row] = down_a A^T, K cut over the waves of a workgroup and over workgroups (lora_splits), so that a few requests fill the chip;
+//   inner  D[r][row] = down_a A^T, K cut over the waves of a workgroup and over workgroups, so that a few requests fill the chip;
 //          a part's sums are written, and added by the second kernel: no atomics, the same bits every time
-//   outer  D[n][row] = up_a inner^T: inner values go in as fp16 relative to their row's power of two, off by 2^-12 of each (or 2^-36 of the
-//          row's largest): less than the rounding of the result they are added to
+//   outer  D[n][row] = up_a inner^T: inner values go in as fp16 relative to their row's power of two, off by 2^-11 of each (or 2^-36 of the
+//          row's largest), as the rows that they come from are; the sum with the shared product, which stays in 32 bits until then, is rounded once
 #include <algorithm>
 
 #include "lora.h"
@@ -477,10 +477,15 @@ lora_many_kernel(LoraOuter p) {
     }
 }
 
-constexpr int kLoraAlone = 256;  // rows up to which they are taken to choose differently
+// Rows up to which they are taken to choose differently: a workgroup per choice of a tile's rows, instead of one that walks them.  us, the whole linear, with /
+// without, 4096 -> 4096: 200 rows with 60 adapters 42.5 / 88, in requests of 40 rows 40 / 42; 500 rows with 60 adapters 68 / 94, in requests of 100
+// rows 45.7 / 43.5; 900 rows 99 / 116, in requests of 90 74 / 69.  (So many rows are mostly prompts.)
+constexpr int kLoraAlone = 256;
 
 // Parts of K: workgroups that fill the chip, each wave with a unit of 128 columns at least.
 constexpr int kManyFill = 512;
+// Rows of a tile: more read less of down, if few adapters meet in one.  Tiles of 16 / 64, us: 3500 rows in requests of 500, 14336 -> 4096, 42 / 29; but 900
+// rows that all choose for themselves, 4096 -> 4096 as a whole, 116 / 205.
 static int inner_tile(int M) { return M <= 2048 ? 16 : 64; }
 static int inner_parts(int M, int K, int n) {
     const int units = (K + 127) / 128;

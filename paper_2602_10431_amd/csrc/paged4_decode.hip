@@ -7,8 +7,8 @@
 //   score = s_j (q . c_j - z_j sum(q)),   out = sum_j (p_j t_j) (c'_j - z'_j) / sum_j p_j,
 // the sum with z' as one more fragment of the second product whose operand rows are all z', so that both parts see the same rounded p t.
 // Queries are fp16 relative to their row's power of two (exact, but for elements 2^-34 of the largest), whatever the cache's type, and p t is fp16
-// relative to a running power of two of t, which it follows upwards: it is off by 2^-12 of itself or 2^-37 of the largest, less than the
-// output's own rounding.  All codes are finite, so that a row reaches a NaN (scale) only through a key that it sees.
+// relative to a running power of two of t, which it follows upwards: it is off by 2^-11 of itself or 2^-37 of the largest, as the
+// output's own rounding is.  All codes are finite, so that a row reaches a NaN (scale) only through a key that it sees.
 #include <algorithm>
 
 #include "paged4.h"
