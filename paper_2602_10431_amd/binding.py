@@ -756,6 +756,7 @@ def qtale_paged_read(kv, layer, seq_offsets, first=None, slots=None, k_out=None,
     """The values that entries first[b] .. of the slots stand for: (k_out, v_out), [T, n_kv_heads, head_dim] in kv.dtype (None: new tensors for T rows)."""
     B = seq_offsets.numel() - 1
     if k_out is None or v_out is None:
+        assert T is not None or k_out is not None or v_out is not None
         T = next(t.shape[0] for t in (k_out, v_out) if t is not None) if T is None else T
         k_out, v_out = (torch.empty((T, kv.n_kv_heads, kv.head_dim), dtype=kv.dtype, device=kv.device) if t is None else t for t in (k_out, v_out))
     T, nkv = k_out.shape[0], kv.n_kv_heads

@@ -67,6 +67,9 @@ __device__ __forceinline__ uint32_t key_order(uint32_t c) {
     return w;
 }
 
+// A workgroup per token (few tokens: per 256 units), so that cosines and sines, in 64 bits, are made once for all its heads.  Bound by HBM for many tokens, a
+// launch for few: 5100 tokens of 48 heads of 128 in bf16 30.5 us, 3.6 TB/s read and written (the rotation into 16-bit pages 28 us, 4.6 TB/s, twice the
+// writes for keys and values, and no exchanges); 64 tokens of 96 heads 5.4 us.
 // PAIRS: 0 half with r a multiple of 16 (a lane's partners are one chunk), 1 interleaved, 2 half with any r.  COPIES as in paged_rope_kernel.
 template <bool BF16, int PAIRS, bool COPIES>
 __global__ void __launch_bounds__(256)
@@ -174,7 +177,7 @@ hipError_t launch_paged4_rope(const PagedRopeArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// A workgroup per row: eight columns per thread.
+// A workgroup per row: eight columns per thread.  (5100 rows of 8 + 8 heads of 128: 11.2 us, 2.4 TB/s: a chain of table, word and code for so little.)
 __global__ void __launch_bounds__(256)
 paged_read_kernel(PagedReadArgs a) {
     const int i = blockIdx.x, d = a.kv.d, cpr = d >> 3;
