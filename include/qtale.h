@@ -250,7 +250,7 @@ typedef struct {
 } qtale_lora;
 
 /* Scratch of the two calls below with M rows: of a linear with `a` (b null), or of a gate/up pair with `a` and `b` (a pair with one of them alone
- * needs no more than with that one twice). */
+ * needs no more than with that one twice).  They do 8192 rows at a time: more need no more. */
 size_t qtale_lora_workspace_bytes(const qtale_lora* a, const qtale_lora* b, int M);
 
 /* qtale_linear_w4a16 with adapters. */

@@ -37,6 +37,8 @@ hipError_t base_linear(const qtale_qlinear* w, const qtale_qlinear* w2, int bits
     return launch_gemm_w4a16(g, stream);
 }
 
+// Rows that are done at a time, which bounds the scratch.  (Each product fills the chip many times over.)
+constexpr int kRowsAtOnce = 8192;
 size_t rows_bytes(int M, int N) { return (static_cast<size_t>(M) * N * 4 + 255) / 256 * 256; }
 size_t inner_bytes(const qtale_lora* l, int M) { return l ? lora_inner_bytes(l->max_rank, M) : 0; }
 
@@ -46,6 +48,7 @@ extern "C" {
 
 size_t qtale_lora_workspace_bytes(const qtale_lora* a, const qtale_lora* b, int M) {
     if (!a || check_lora(a, a->N, a->K, false) || (b && check_lora(b, a->N, a->K, false)) || M < 0 || a->N <= 0 || a->K <= 0) return 0;
+    M = std::min(M, kRowsAtOnce);
     return 256 + inner_bytes(a, M) + inner_bytes(b, M) + (b ? 2 : 1) * rows_bytes(M, a->N);
 }
 
@@ -59,14 +62,18 @@ int qtale_linear_lora_w4a16(const qtale_qlinear* w, int bits, int group, const q
     if ((e = check_lora_call(adapter, A, out, workspace, workspace_bytes, qtale_lora_workspace_bytes(lora, nullptr, M)))) return e;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const LoraDev l = lora_device(lora);
-    const LoraRows rows{adapter, nullptr, nullptr, M, 0};
     float* inner = static_cast<float*>(workspace);
-    const float* operands = nullptr;
-    int parts = 0;
-    HIP_TRY(launch_lora_inner(&l, 1, rows, A, &inner, &operands, &parts, s));
-    float* base = reinterpret_cast<float*>(static_cast<char*>(workspace) + inner_bytes(lora, M));
-    HIP_TRY(base_linear(w, nullptr, bits, group, A, M, base, s));
-    HIP_TRY(launch_lora_round(l, rows, operands, parts, base, w->N, out, w->N, s));
+    float* base = reinterpret_cast<float*>(static_cast<char*>(workspace) + inner_bytes(lora, std::min(M, kRowsAtOnce)));
+    for (int m = 0; m < M; m += kRowsAtOnce) {
+        const int n = std::min(M - m, kRowsAtOnce);
+        const LoraRows rows{adapter + m, nullptr, nullptr, n, 0};
+        const uint16_t* x = static_cast<const uint16_t*>(A) + static_cast<size_t>(m) * w->K;
+        const float* operands = nullptr;
+        int parts = 0;
+        HIP_TRY(launch_lora_inner(&l, 1, rows, x, &inner, &operands, &parts, s));
+        HIP_TRY(base_linear(w, nullptr, bits, group, x, n, base, s));
+        HIP_TRY(launch_lora_round(l, rows, operands, parts, base, w->N, static_cast<uint16_t*>(out) + static_cast<size_t>(m) * w->N, w->N, s));
+    }
     return QTALE_OK;
 }
 
@@ -83,24 +90,30 @@ int qtale_swiglu_lora_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, 
     if (M == 0) return QTALE_OK;
     if (!gate->prepacked || !up->prepacked) return QTALE_ERR_INVALID_ARG;
     // (a size for one of them counts the rows' buffers too: the pair's size with the larger rank twice is enough for either)
-    const size_t need = 256 + inner_bytes(lora_gate, M) + inner_bytes(lora_up, M) + 2 * rows_bytes(M, gate->N);
+    const int most = std::min(M, kRowsAtOnce);
+    const size_t need = 256 + inner_bytes(lora_gate, most) + inner_bytes(lora_up, most) + 2 * rows_bytes(most, gate->N);
     if ((e = check_lora_call(adapter, A, out, workspace, workspace_bytes, need))) return e;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const LoraDev lg = lora_device(lora_gate), lu = lora_device(lora_up);
-    const LoraRows rows{adapter, nullptr, nullptr, M, 0};
     char* at = static_cast<char*>(workspace);
     float* inner_g = reinterpret_cast<float*>(at);
-    float* inner_u = reinterpret_cast<float*>(at += inner_bytes(lora_gate, M));
-    float* base = reinterpret_cast<float*>(at += inner_bytes(lora_up, M));
-    LoraDev l[2];
-    float* inner[2];
-    const float* operands[2] = {nullptr, nullptr};
-    int parts[2] = {0, 0}, n = 0;
-    if (lg.n) { l[n] = lg; inner[n++] = inner_g; }
-    if (lu.n) { l[n] = lu; inner[n++] = inner_u; }
-    HIP_TRY(launch_lora_inner(l, n, rows, A, inner, operands, parts, s));
-    HIP_TRY(base_linear(gate, up, bits, group, A, M, base, s));
-    HIP_TRY(launch_lora_swiglu(lg, lu, rows, operands[0], operands[n - 1], parts[0], parts[n - 1], base, out, gate->N, s));
+    float* inner_u = reinterpret_cast<float*>(at += inner_bytes(lora_gate, most));
+    float* base = reinterpret_cast<float*>(at += inner_bytes(lora_up, most));
+    for (int m = 0; m < M; m += kRowsAtOnce) {
+        const int rows_here = std::min(M - m, kRowsAtOnce);
+        const LoraRows rows{adapter + m, nullptr, nullptr, rows_here, 0};
+        const uint16_t* x = static_cast<const uint16_t*>(A) + static_cast<size_t>(m) * gate->K;
+        LoraDev l[2];
+        float* inner[2];
+        const float* operands[2] = {nullptr, nullptr};
+        int parts[2] = {0, 0}, n = 0;
+        if (lg.n) { l[n] = lg; inner[n++] = inner_g; }
+        if (lu.n) { l[n] = lu; inner[n++] = inner_u; }
+        HIP_TRY(launch_lora_inner(l, n, rows, x, inner, operands, parts, s));
+        HIP_TRY(base_linear(gate, up, bits, group, x, rows_here, base, s));
+        HIP_TRY(launch_lora_swiglu(lg, lu, rows, operands[0], operands[n - 1], parts[0], parts[n - 1], base,
+                                   static_cast<uint16_t*>(out) + static_cast<size_t>(m) * gate->N, gate->N, s));
+    }
     return QTALE_OK;
 }
 

@@ -91,6 +91,24 @@ def test_linear(qt, N, K, group, M):
             assert torch.equal(got, qt.qtale_linear_w4a16(q, x))
 
 
+def test_more_rows_than_are_done_at_a_time(qt):
+    N, K, M = 72, 64, 8192 + 8192 + 5
+    pairs = [_base(qt, N, K, 4, 64, s) for s in (1, 2)]
+    lg, dg, ug = _adapters(qt, 3, 8, N, K, 3)
+    lu, du, uu = _adapters(qt, 3, 16, N, K, 4)
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).half().cuda()
+    ids = _ids("runs", M, 3, M)
+    ws = qt.alloc_lora_workspace([lg, lu], M)
+    assert ws.numel() == qt.alloc_lora_workspace([lg, lu], 8192).numel()
+    linear, gated = qt.qtale_linear_lora_w4a16(pairs[0][0], lg, x, ids), qt.qtale_swiglu_lora_w4a16(pairs[0][0], pairs[1][0], lg, lu, x, ids, workspace=ws)
+    for at in (0, 8192, 16384):                                   # the same rows, done apart
+        part = slice(at, min(at + 8192, M))
+        assert torch.equal(linear[part], qt.qtale_linear_lora_w4a16(pairs[0][0], lg, x[part], ids[part]))
+        assert torch.equal(gated[part], qt.qtale_swiglu_lora_w4a16(pairs[0][0], pairs[1][0], lg, lu, x[part], ids[part]))
+    y, bound = _expect(pairs[0][1], lg, dg, ug, x, ids)
+    assert bool(((linear.double() - y).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("M", [1, 20, 64, 200, 300, 700])
 def test_what_is_added_is_not_rounded_before(qt, M):
     # Sums of a whole number and a fraction that fp16 cannot hold, from which the adapter takes the whole number again: the fraction is left, exactly.
