@@ -115,7 +115,7 @@ hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int
 hipError_t launch_paged_decode(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);
 hipError_t launch_paged_pieces(const PagedAttnDev& a, int d, int bf16, hipStream_t stream);   // adds the spans' sums
 hipError_t launch_paged4_decode(const PagedAttnDev& a, int d, hipStream_t stream);
-hipError_t launch_paged4_chunk(const PagedAttnDev& a, int groups, int d, hipStream_t stream);
+hipError_t launch_paged4_chunk(const PagedAttnDev& a, int d, hipStream_t stream);
 hipError_t launch_paged_chunk(const PagedAttnDev& a, int groups, int d, int bf16, hipStream_t stream);
 hipError_t launch_chunk_combine(const PagedAttnDev& a, int d, int bf16, int T, hipStream_t stream);
 

@@ -8,10 +8,10 @@
 // reference point, the lift (kChunkLift) and log2 of t_ref, a power of two above all t so far: so p t fits fp16 whatever the values' size, for
 // one multiplication.
 //
-// What bounds it: a wave has 340 vector instructions and 110 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is a quarter
-// and the values' scales another: 4 x 4096 tokens, 32 heads on 8 of 128, 0.83 to 0.94 ms, card by card (580 to 665 TFLOP/s; 16-bit pages 0.59 ms); a wide
-// workgroup alone takes 2.9 us per tile.  Without the weighing of scores that call takes 0.56 ms, without the unpacking 0.79, matrix products and
-// barriers alone 0.50.  500 tokens on 24000 keys 325 us.
+// What bounds it: a wave has 350 vector instructions and 110 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is a quarter
+// and the values' scales another.  4 x 4096 tokens, 32 heads on 8 of 128, 0.78 ms, 710 TFLOP/s (16-bit pages 0.59 ms); 500 tokens on 24000 keys 295 us.
+// Eight waves on 256 columns whose halves take turns with the matrix cores and the vector ALUs, the best form for 16-bit pages, lose here, since the vector half
+// takes more than twice the other's time: 0.83 ms, 2 x 300 tokens on 6000 keys 139 us instead of 117, heads of 64 4 x 4096 700 instead of 548.
 #include <algorithm>
 
 #include "paged4.h"
@@ -393,12 +393,11 @@ struct Columns4 {
 
 // The tiles of an item that this workgroup walks, and how many ranges the item has.
 struct Range4 { int t0, t1, ranges; };
-template <int PER>
 __device__ __forceinline__ Range4 range_of(const PagedAttnDev& p, int steps, int z) {
     // ranges of about equal length over the whole call, as many as are to run at once; no item is cut into more than p.ranges
     const int lane = threadIdx.x & 63;
     int work = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) work += b0 + lane < p.B ? chunk_work<PER>(p, b0 + lane) : 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) work += b0 + lane < p.B ? chunk_work(p, b0 + lane) : 0;
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) work += __shfl_xor(work, x, 64);
     const int wanted = max(p.target / p.nkv, 1);
@@ -430,7 +429,7 @@ paged4_chunk_kernel(PagedAttnDev p) {
     const int c_lo = qt * kChunkCols, c_hi = min(c_lo + kChunkCols, s.n * p.rep) - 1;   // this workgroup's columns
     const KeySteps<kTileKeys> walk(s.first + __builtin_amdgcn_readfirstlane(c_lo / p.rep), s.first + __builtin_amdgcn_readfirstlane(c_hi / p.rep), s.len, p.window, p.sinks);
     Range4 range{0, walk.steps, 1};
-    if (SPLIT) range = range_of<kChunkCols>(p, walk.steps, z);
+    if (SPLIT) range = range_of(p, walk.steps, z);
     if (SPLIT && z >= range.ranges) return;
     Cols cw(p, s, hk, c_lo + 32 * wave, c_hi, walk.hi);
     const PageRow pages(p, s.slot);
@@ -457,10 +456,10 @@ paged4_chunk_kernel(PagedAttnDev p) {
         request(t0 + 1, i1.page);
         for (int t = t0; t < t1; ++t) {
             __syncthreads();                                     // tile t is in LDS, and the other buffers have been read
-            if (t + 1 < t1) unpack(t + 1);
-            request(t + 2, i2.page);
             const Tile4<D> now = tile(t);
             cw.template products<Cols::PV, Cols::ALL>(now.V, now.K);
+            if (t + 1 < t1) unpack(t + 1);
+            request(t + 2, i2.page);
             typename Cols::Scales sc = cw.scales(now);
             cw.softmax(p, now, sc, walk.key(t), i0.gone, walk.hi);
             cw.template products<0, Cols::PV>(now.V, now.K);
@@ -472,135 +471,17 @@ paged4_chunk_kernel(PagedAttnDev p) {
     cw.template put<SPLIT>(p, s, z, range.ranges);
 }
 
-// Eight waves, 256 columns, one workgroup per CU, two waves per SIMD that take turns as in paged_wide_kernel: while the first half of the waves runs its
-// products (matrix cores, LDS), the second half runs its softmax and unpacks (vector ALUs), then they change places.
-//   phase      0         1             2             3             4
-//   half 0     S0, P0    O0, S1        P1, K2 in     O1, S2        P2, K3 in
-//   half 1     S0        P0, V1 in     O0, S1        P1, V2 in     O1, S2
-// "K2 in": keys of tile 2 go into LDS, in the place of tile 0's, which phase 0 was the last to read; V1 likewise.
-template <int D, bool BF16, bool SPLIT>
-__global__ void __launch_bounds__(512, 2)
-paged4_wide_kernel(PagedAttnDev p) {
-    using Cols = Columns4<D, BF16>;
-    constexpr int TILE = kTileKeys * D;
-    __shared__ __attribute__((aligned(1024))) uint16_t Ks[2][TILE], Vs[2][TILE];
-    __shared__ __attribute__((aligned(16))) float ks[2][kTileKeys], ts[2][kTileKeys];
-    __shared__ __attribute__((aligned(16))) uint32_t tmax[2][4];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-    int hk, item, z = 0, b, qt;
-    find_head(p, &hk, &item);
-    if (SPLIT) {
-        z = __builtin_amdgcn_readfirstlane(item / p.items);
-        item -= z * p.items;
-    }
-    if (!find_columns<kWideCols>(p, item, &b, &qt)) return;
-    SeqView s(p, b);
-    s.uniform();
-    const int c_lo = qt * kWideCols, c_hi = min(c_lo + kWideCols, s.n * p.rep) - 1;
-    const KeySteps<kTileKeys> walk(s.first + __builtin_amdgcn_readfirstlane(c_lo / p.rep), s.first + __builtin_amdgcn_readfirstlane(c_hi / p.rep), s.len, p.window, p.sinks);
-    Range4 range{0, walk.steps, 1};
-    if (SPLIT) range = range_of<kWideCols>(p, walk.steps, z);
-    if (SPLIT && z >= range.ranges) return;
-    Cols cw(p, s, hk, c_lo + 32 * wave, c_hi, walk.hi);
-    const PageRow pages(p, s.slot);
-    Unpack4<D, BF16> un(p, hk, wave & 3, walk.hi);
-    const int t0 = range.t0, n = range.t1 - range.t0;            // (tiles below are counted from t0)
-    auto tile = [&](int t) __attribute__((always_inline)) { return Tile4<D>{Ks[t & 1], Vs[t & 1], ks[t & 1], ts[t & 1], tmax[t & 1]}; };
-    auto key0 = [&](int t) __attribute__((always_inline)) { return walk.key(t0 + t); };
-    // What a wave has written to LDS is there, and its reads have been consumed; requests of its own stay outstanding: a bare barrier that no access
-    // and no instruction is moved across.
-    auto phase_end = [&]() __attribute__((always_inline)) {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0)
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("" ::: "memory");
-    };
-    if (n > 0) {
-        TileWalk ids(pages, walk, t0, wave & 3);
-        TilePages i0 = ids.next(0), i1 = ids.next(1), i2 = ids.next(2);
-        if (wave < 4) {
-            Unpack4<D, BF16> first(p, hk, wave & 3, walk.hi);
-            first.request_keys(key0(0), i0.page);
-            un.request_keys(key0(1), 1 < n ? i1.page : -1);
-            first.put_keys(key0(0), tile(0));
-            un.put_keys(key0(1), tile(1));
-            un.request_keys(key0(2), 2 < n ? i2.page : -1);
-        } else {
-            Unpack4<D, BF16> first(p, hk, wave & 3, walk.hi);
-            first.request_values(key0(0), i0.page);
-            un.request_values(key0(1), 1 < n ? i1.page : -1);
-            first.put_values(key0(0), tile(0));
-        }
-        phase_end();
-        cw.template products<Cols::PV, Cols::ALL>(Vs[0], Ks[0]);
-        // (both halves walk the same barriers; past the last tile the scores are of whatever lies there, and not used)
-        auto turn = [&](int t) __attribute__((always_inline)) {
-            __builtin_amdgcn_s_setprio(1);
-            cw.template products<0, Cols::ALL>(Vs[t & 1], Ks[(t + 1) & 1]);
-            __builtin_amdgcn_s_setprio(0);
-            phase_end();
-        };
-        if (wave < 4) {
-            typename Cols::Scales first = cw.scales(tile(0));
-            cw.softmax(p, tile(0), first, key0(0), i0.gone, walk.hi);
-            phase_end();
-            auto both = [&](int t) __attribute__((always_inline)) {
-                turn(t);
-                i0 = i1;
-                i1 = i2;
-                i2 = ids.next(t + 3);
-                typename Cols::Scales sc = cw.scales(tile(t + 1));
-                un.put_keys(key0(t + 2), tile(t));               // (of a tile past the last: zeros)
-                un.request_keys(key0(t + 3), t + 3 < n ? i2.page : -1);
-                cw.softmax(p, tile(t + 1), sc, key0(t + 1), t + 1 < n ? i0.gone : 15, walk.hi);
-                phase_end();
-            };
-            for (int t = 0; t < n; ++t) {
-                both(t);
-
-            }
-        } else {
-            phase_end();
-            auto both = [&](int t) __attribute__((always_inline)) {
-                typename Cols::Scales sc = cw.scales(tile(t));
-                un.put_values(key0(t + 1), tile(t + 1));
-                un.request_values(key0(t + 2), t + 2 < n ? i2.page : -1);
-                cw.softmax(p, tile(t), sc, key0(t), i0.gone, walk.hi);
-                i0 = i1;
-                i1 = i2;
-                i2 = ids.next(t + 3);
-                phase_end();
-                turn(t);
-            };
-            for (int t = 0; t < n; ++t) {
-                both(t);
-
-            }
-        }
-    }
-    cw.template put<SPLIT>(p, s, z, range.ranges);
-}
-
 template <int D, bool BF16>
-static hipError_t chunk4_form(const PagedAttnDev& a, int groups, hipStream_t stream) {
+static hipError_t chunk4_form(const PagedAttnDev& a, hipStream_t stream) {
     const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.items) * a.ranges * a.nkv));
-    if (groups == 0) {
-        if (a.ranges > 1) hipLaunchKernelGGL((paged4_wide_kernel<D, BF16, true>), grid, dim3(512), 0, stream, a);
-        else hipLaunchKernelGGL((paged4_wide_kernel<D, BF16, false>), grid, dim3(512), 0, stream, a);
-    } else if (a.ranges > 1) {
-        hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, true>), grid, dim3(256), 0, stream, a);
-    } else {
-        hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, false>), grid, dim3(256), 0, stream, a);
-    }
+    if (a.ranges > 1) hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((paged4_chunk_kernel<D, BF16, false>), grid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
-hipError_t launch_paged4_chunk(const PagedAttnDev& a, int groups, int d, hipStream_t stream) {
-    if (d == 128) return a.bf16 ? chunk4_form<128, true>(a, groups, stream) : chunk4_form<128, false>(a, groups, stream);
-    return a.bf16 ? chunk4_form<64, true>(a, groups, stream) : chunk4_form<64, false>(a, groups, stream);
+hipError_t launch_paged4_chunk(const PagedAttnDev& a, int d, hipStream_t stream) {
+    if (d == 128) return a.bf16 ? chunk4_form<128, true>(a, stream) : chunk4_form<128, false>(a, stream);
+    return a.bf16 ? chunk4_form<64, true>(a, stream) : chunk4_form<64, false>(a, stream);
 }
 
 }  // namespace qtale

@@ -6,15 +6,14 @@ namespace qtale {
 
 constexpr int kTileKeys = kChunkTileKeys;
 
-// Work of a call, in tiles per kv head, for column tiles of PER: the column tiles of a sequence see a number of key tiles that grows evenly from the first to the last.
-template <int PER = kChunkCols>
+// Work of a call, in tiles per kv head: the column tiles of a sequence see a number of key tiles that grows evenly from the first to the last.
 __device__ __forceinline__ int chunk_work(const PagedAttnDev& p, int b) {
     const SeqView s(p, b);
     const int cols = s.n * p.rep;
     if (cols == 0 || (p.take != 0 && cols <= kDecodeCols)) return 0;
-    const int nt = (cols + PER - 1) / PER;
-    const int least = KeySteps<kTileKeys>(s.first, s.first + (min(PER, cols) - 1) / p.rep, s.len, p.window, p.sinks).steps;
-    const int most = KeySteps<kTileKeys>(s.first + (nt - 1) * PER / p.rep, s.first + s.n - 1, s.len, p.window, p.sinks).steps;
+    const int nt = (cols + kChunkCols - 1) / kChunkCols;
+    const int least = KeySteps<kTileKeys>(s.first, s.first + (min(kChunkCols, cols) - 1) / p.rep, s.len, p.window, p.sinks).steps;
+    const int most = KeySteps<kTileKeys>(s.first + (nt - 1) * kChunkCols / p.rep, s.first + s.n - 1, s.len, p.window, p.sinks).steps;
     return nt * (least + most) / 2;
 }
 

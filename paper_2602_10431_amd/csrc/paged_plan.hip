@@ -24,13 +24,12 @@ static size_t decode_bytes(int nkv, int d, int B) {
     const size_t pieces = (static_cast<size_t>(std::min(B, kSpanSeqs)) * sizeof(int4) + 255) / 256 * 256;
     return pieces + static_cast<size_t>(decode_spans(nkv, d)) * nkv * 2 * kDecodeCols * part_stride(d) * 4;
 }
-// Pages in 4 bits: whether sixteen columns at a time, which unpack in registers, take less time than tiles of 128 or 256 columns, which unpack once for all
+// Pages in 4 bits: whether sixteen columns at a time, which unpack in registers, take less time than tiles of 128 columns, which unpack once for all
 // of them but pass LDS and barriers.  Estimates in us, from runs of either alone.  A workgroup of the decode kernel walks a key in 6.2 ns (heads of 64: 5.6)
-// until a CU's others hold it up, 4.0 (3.1) ns for each of those.  A workgroup of the wide chunk kernel, one per CU, takes 15 us and 2.9 us per tile of 64
-// keys; the other's 8 and 2.4, two on a CU 3.1 per tile; ranges cost 14 us and 0.5 ns per row of sums.  us, decode / chunk kernel, heads of 128, 4 per kv
-// head (8): 1 x 32 tokens on 1500 keys 15 / 58, on 4000 29 / 33; 1 x 64 on 24000 138 / 65; 4 x 64 on 1500 23 / 50; 64 x 8 on 2000 42 / 100; 64 x 32 on 1000
-// 92 / 68; 1 x 500 on 700 27 / 51; 8 x 128 on 2000 78 / 111; 4 x 1000 on 0 110 / 90, 2 x 2000 159 / 129; one per kv head (32) 1 x 2000 on 0 87 / 105,
-// 4 x 1000 110 / 97; heads of 64 48 x 6 on 3000 37 / 104, 64 x 16 on 3000 83 / 112.
+// until a CU's others hold it up, 4.0 (3.1) ns for each of those.  A workgroup of the chunk kernel takes 8 us and 2.4 us per tile of 64 keys, two on a CU 3.1
+// per tile; ranges cost 14 us and 0.5 ns per row of sums.  us, decode / chunk kernel, heads of 128, 4 per kv head (8): 1 x 32 tokens on 1500 keys 15 /
+// 58, on 4000 29 / 33; 1 x 64 on 24000 138 / 68; 64 x 8 on 2000 42 / 100; 64 x 32 on 1000 92 / 68; 4 x 1000 on 0 110 / 81, 2 x 2000 159 / 123; one per kv
+// head (32) 4 x 1000 110 / 83; heads of 64 48 x 6 on 3000 37 / 104.
 static bool decode4_pays(int nh, int nkv, int d, int T, int B, int64_t max_new, int64_t seen, bool window) {
     const int rep = nh / nkv, cus = device_cus();
     const int64_t cols = max_new * rep, sixteens = (cols + kDecodeCols - 1) / kDecodeCols, live = std::min(B, T);
@@ -40,12 +39,10 @@ static bool decode4_pays(int nh, int nkv, int d, int T, int B, int64_t max_new, 
     };
     const double longest = static_cast<double>(seen), mean = window ? longest : std::max(longest - 0.5 * static_cast<double>(max_new), 0.0);
     const double by = workgroups(kDecodeCols), decode = 5.0 + 1.2 * by + 0.001 * mean * (d == 64 ? std::max(5.6, 3.1 * by) : std::max(6.2, 4.0 * by));
-    const bool wide = cols > kChunkCols;
-    const double r = std::max(workgroups(wide ? kWideCols : kChunkCols), 1e-3), begin = wide ? 15.0 : 8.0, tile = wide ? 2.9 : 2.4, shared = wide ? 2.9 : 1.55;
-    const double most = longest / kChunkTileKeys, some = mean / kChunkTileKeys;
-    const double whole = begin * std::max(r, 1.0) + std::max(tile * most, shared * r * some + (r > 1.0 ? tile * (most - some) : 0.0));
-    const double ranges = std::max(std::min({(wide ? 1.0 : 2.0) / r, most / 8, 32.0}), 1.0);
-    const double cut = begin + 14.0 + std::max(tile * most / ranges, shared * r * some) + 0.0005 * T * nh * ranges;
+    const double r = std::max(workgroups(kChunkCols), 1e-3), most = longest / kChunkTileKeys, some = mean / kChunkTileKeys;
+    const double whole = 8.0 * std::max(0.5 * r, 1.0) + std::max(2.4 * most, 1.55 * r * some + (r > 2.0 ? 2.4 * (most - some) : 0.0));
+    const double ranges = std::max(std::min({2.0 / r, most / 8, 32.0}), 1.0);
+    const double cut = 22.0 + std::max(2.4 * most / ranges, 1.55 * r * some) + 0.0005 * T * nh * ranges;
     return decode < std::min(whole, cut);
 }
 PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks) {
@@ -79,16 +76,9 @@ PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B,
     l.stream_keys = pairs >= 4 * cus;
     l.ranges = l.groups = 1;
     if (l.chunk && q4) {
-        // (the wide form, one workgroup per CU)
-        const int64_t wide = (static_cast<int64_t>(T) * rep + static_cast<int64_t>(kWideCols - 1) * std::min(B, T)) / kWideCols, wide_wgs = std::max<int64_t>(wide * nkv, 1);
-        if (cols > kChunkCols) {
-            l.groups = 0;
-            items = wide;
-            if (tiles * (cus - wide_wgs) > 12 * cus) {
-                l.target = cus;
-                l.ranges = static_cast<int>(std::max<int64_t>(std::min<int64_t>({2 * ((cus + wide_wgs - 1) / wide_wgs), tiles / 8, 32}), 1));
-            }
-        } else if (cut) {
+        // Ranges for two workgroups per CU.  us, with / without: heads of 128, 4 per kv head, 64 rows on 24000 keys 68 / 961, 500 295 / 985, 1000 on 6000 173 / 295;
+        // one per kv head 700 on 4000 113 / 206.
+        if (cut) {
             l.target = static_cast<int>(two);
             l.ranges = static_cast<int>(std::max<int64_t>(std::min<int64_t>({2 * ((two + wgs - 1) / wgs), tiles / 8, 32}), 1));
         }
@@ -137,7 +127,7 @@ hipError_t launch_paged_attention(PagedAttnDev a, const PagedAttnPlan& plan, int
     hipError_t e = hipSuccess;
     if (a.q4) {
         if (plan.decode && (e = launch_paged4_decode(a, d, stream)) != hipSuccess) return e;
-        if (plan.chunk && (e = launch_paged4_chunk(a, plan.groups, d, stream)) != hipSuccess) return e;
+        if (plan.chunk && (e = launch_paged4_chunk(a, d, stream)) != hipSuccess) return e;
         a.scale_log2 = 1.0f;                                     // (reference points of these kernels are scaled scores)
         return plan.ranges > 1 ? launch_chunk_combine(a, d, bf16, T, stream) : e;
     }
