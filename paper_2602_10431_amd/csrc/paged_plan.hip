@@ -26,7 +26,7 @@ static size_t decode_bytes(int nkv, int d, int B) {
 }
 // Pages in 4 bits: whether sixteen columns at a time, which unpack in registers, take less time than tiles of 128 columns, which unpack once for all
 // of them but pass LDS and barriers.  Estimates in us, from runs of either alone.  A workgroup of the decode kernel walks a key in 6.2 ns (heads of 64: 5.6)
-// until a CU's others hold it up, 4.0 (3.1) ns for each of those.  A workgroup of the chunk kernel takes 8 us and 2.4 us per tile of 64 keys, two on a CU 3.1
+// until a CU's others hold it up, 4.0 (3.1) ns for each of those.  A workgroup of the chunk kernel takes 8 us and 2.2 us per tile of 64 keys, two on a CU 2.9
 // per tile; ranges cost 14 us and 0.5 ns per row of sums.  us, decode / chunk kernel, heads of 128, 4 per kv head (8): 1 x 32 tokens on 1500 keys 15 /
 // 58, on 4000 29 / 33; 1 x 64 on 24000 138 / 68; 64 x 8 on 2000 42 / 100; 64 x 32 on 1000 92 / 68; 4 x 1000 on 0 110 / 81, 2 x 2000 159 / 123; one per kv
 // head (32) 4 x 1000 110 / 83; heads of 64 48 x 6 on 3000 37 / 104.
@@ -40,9 +40,9 @@ static bool decode4_pays(int nh, int nkv, int d, int T, int B, int64_t max_new, 
     const double longest = static_cast<double>(seen), mean = window ? longest : std::max(longest - 0.5 * static_cast<double>(max_new), 0.0);
     const double by = workgroups(kDecodeCols), decode = 5.0 + 1.2 * by + 0.001 * mean * (d == 64 ? std::max(5.6, 3.1 * by) : std::max(6.2, 4.0 * by));
     const double r = std::max(workgroups(kChunkCols), 1e-3), most = longest / kChunkTileKeys, some = mean / kChunkTileKeys;
-    const double whole = 8.0 * std::max(0.5 * r, 1.0) + std::max(2.4 * most, 1.55 * r * some + (r > 2.0 ? 2.4 * (most - some) : 0.0));
+    const double whole = 8.0 * std::max(0.5 * r, 1.0) + std::max(2.2 * most, 1.45 * r * some + (r > 2.0 ? 2.2 * (most - some) : 0.0));
     const double ranges = std::max(std::min({2.0 / r, most / 8, 32.0}), 1.0);
-    const double cut = 22.0 + std::max(2.4 * most / ranges, 1.55 * r * some) + 0.0005 * T * nh * ranges;
+    const double cut = 22.0 + std::max(2.2 * most / ranges, 1.45 * r * some) + 0.0005 * T * nh * ranges;
     return decode < std::min(whole, cut);
 }
 PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B, int max_new, int max_len, int window, int sinks) {
