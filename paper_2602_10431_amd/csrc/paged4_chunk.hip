@@ -8,8 +8,9 @@
 // reference point, the lift (kChunkLift) and log2 of t_ref, a power of two above all t so far: so p t fits fp16 whatever the values' size, for
 // one multiplication.
 //
-// What bounds it: a wave has 350 vector instructions and 110 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is a quarter
-// and the values' scales another.  4 x 4096 tokens, 32 heads on 8 of 128, 0.78 ms, 710 TFLOP/s (16-bit pages 0.59 ms); 500 tokens on 24000 keys 295 us.
+// What bounds it: a wave has 445 vector instructions and 120 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is two fifths
+// and the values' scales a tenth.  4 x 4096 tokens, 32 heads on 8 of 128, 0.72 to 0.75 ms, 730 to 760 TFLOP/s (16-bit pages 0.59 ms); 500 tokens on 24000 keys
+// 282 us.  Unpacking the next tile behind the scores' products, which run on, instead of before them: 0.78 -> 0.72 ms.
 // Eight waves on 256 columns whose halves take turns with the matrix cores and the vector ALUs, the best form for 16-bit pages, lose here, since the vector half
 // takes more than twice the other's time: 0.83 ms, 2 x 300 tokens on 6000 keys 139 us instead of 117, heads of 64 4 x 4096 700 instead of 548.
 #include <algorithm>
@@ -252,8 +253,7 @@ struct Columns4 {
         }
     }
 
-    // Keys' scales of the first half of a tile and the largest of the values': asked for before the wave unpacks, since beside the other half's operands a
-    // read takes long.
+    // Keys' scales of the first half of a tile and the largest of the values': asked for together; the others follow as these are used.
     struct Scales { float4_t k[4]; u32x4_t most; };
     __device__ __forceinline__ Scales scales(const Tile4<D>& tile) const {
         const int quad = here(4 * ((threadIdx.x & 63) >> 5));

@@ -28,8 +28,8 @@ static size_t decode_bytes(int nkv, int d, int B) {
 // of them but pass LDS and barriers.  Estimates in us, from runs of either alone.  A workgroup of the decode kernel walks a key in 6.2 ns (heads of 64: 5.6)
 // until a CU's others hold it up, 4.0 (3.1) ns for each of those.  A workgroup of the chunk kernel takes 8 us and 2.2 us per tile of 64 keys, two on a CU 2.9
 // per tile; ranges cost 14 us and 0.5 ns per row of sums.  us, decode / chunk kernel, heads of 128, 4 per kv head (8): 1 x 32 tokens on 1500 keys 15 /
-// 58, on 4000 29 / 33; 1 x 64 on 24000 138 / 68; 64 x 8 on 2000 42 / 100; 64 x 32 on 1000 92 / 68; 4 x 1000 on 0 110 / 81, 2 x 2000 159 / 123; one per kv
-// head (32) 4 x 1000 110 / 83; heads of 64 48 x 6 on 3000 37 / 104.
+// 56, on 4000 30 / 31; 1 x 64 on 24000 138 / 64; 64 x 8 on 2000 46 / 98; 64 x 32 on 1000 96 / 64; 4 x 1000 on 0 113 / 76, 2 x 2000 162 / 119; 8 x 128 on
+// 2000 74 / 81; one per kv head (32) 4 x 1000 111 / 75; heads of 64 48 x 6 on 3000 34 / 101, 64 x 16 on 3000 82 / 108.
 static bool decode4_pays(int nh, int nkv, int d, int T, int B, int64_t max_new, int64_t seen, bool window) {
     const int rep = nh / nkv, cus = device_cus();
     const int64_t cols = max_new * rep, sixteens = (cols + kDecodeCols - 1) / kDecodeCols, live = std::min(B, T);
@@ -77,7 +77,7 @@ PagedAttnPlan plan_paged_attention(int q4, int nh, int nkv, int d, int T, int B,
     l.ranges = l.groups = 1;
     if (l.chunk && q4) {
         // Ranges for two workgroups per CU.  us, with / without: heads of 128, 4 per kv head, 64 rows on 24000 keys 68 / 961, 500 295 / 985, 1000 on 6000 173 / 295;
-        // one per kv head 700 on 4000 113 / 206.
+        // one per kv head 700 on 4000 113 / 206 (unpacking before the scores' products, as the forms then were).
         if (cut) {
             l.target = static_cast<int>(two);
             l.ranges = static_cast<int>(std::max<int64_t>(std::min<int64_t>({2 * ((two + wgs - 1) / wgs), tiles / 8, 32}), 1));
