@@ -4,9 +4,10 @@
 // queries' elements or taken from the result), exact, into LDS, K as [key][d], V transposed as [column][key] in the order of the second product's
 // operand, which the layout of a value page gives without permutations.  Scales stay outside the products:
 //   score = s_j (q . (c_j - z_j)),   out = sum_j (p_j t_j) (c'_j - z'_j) / sum_j p_j.
-// Queries are fp16; a row that is too large for it, or small, comes relative to its power of two.  Probabilities are 2^(score - m_run), where m_run holds the
-// reference point, the lift (kChunkLift) and log2 of t_ref, a power of two above all t so far: so p t fits fp16 whatever the values' size, for
-// one multiplication.
+// Queries are fp16; a row that is too large for it, or small, comes relative to its power of two.  Probabilities are 2^(score - m_ref + off): m_ref is a whole
+// number next to a score, off = kChunkLift4 - log2 t_ref with a power of two t_ref above all t so far, so that p t fits fp16 whatever the values' size, for one
+// multiplication.  Below 2^22 m_ref - off is exact and goes in as one number; larger scores, whose spacing in 32 bits is that of whole numbers and more, take
+// off apart, where an addition per score more does not show.
 //
 // What bounds it: a wave has 445 vector instructions and 120 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is two fifths
 // and the values' scales a tenth.  4 x 4096 tokens, 32 heads on 8 of 128, 0.72 to 0.75 ms, 730 to 760 TFLOP/s (16-bit pages 0.59 ms); 500 tokens on 24000 keys
@@ -175,8 +176,9 @@ struct Columns4 {
     float up;                                    // the power of two that a score's unit stands for
     int k_at[KS], v_at[4];                       // LDS elements that this lane reads
     float16_t st[2], o[DF];
-    float m_run, l_run;
+    float m_ref, l_run;
     int t_exp;                                   // log2 of t_ref
+    bool far;                                    // some row's m_ref is too large to hold `off` too (the same in all lanes)
 
     // columns .. c_hi; c0: the wave's first
     __device__ __forceinline__ Columns4(const PagedAttnDev& p, const SeqView& s, int hk, int c0, int c_hi, int hi) {
@@ -218,10 +220,12 @@ struct Columns4 {
         for (int f = 0; f < DF; ++f)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[f][r] = 0.0f;
-        m_run = kPagedNone;
+        m_ref = kPagedNone;
         l_run = 0.0f;
         t_exp = -60;
+        far = false;
     }
+    __device__ __forceinline__ float off() const { return kChunkLift4 - static_cast<float>(t_exp); }
 
     __device__ __forceinline__ u32x4_t operand(const uint16_t* V, const uint16_t* K, int i) const {
         if (i < PV) {
@@ -310,25 +314,26 @@ struct Columns4 {
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kf][r]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * up;
-        // The reference point stays as long as no probability passes 2^15 and no value's scale t_ref.  It moves so that the largest probability is 2^kChunkLift4,
-        // and t_ref to the next power of two but one.
+        // The reference point stays as long as no probability passes 2^15 t_ref^-1 and no value's scale t_ref.  It moves so that the largest probability is about
+        // 2^kChunkLift4 t_ref^-1, and t_ref to the next power of two but one.
         const bool larger = tx > ldexpf(1.0f, t_exp);
-        const float above = mx + static_cast<float>(t_exp) - m_run;
-        if (larger || __any(above > 15.0f)) {
+        if (larger || __any(mx - m_ref > 15.0f - kChunkLift4)) {
             const int e = larger ? min(static_cast<int>(__float_as_uint(tx) >> 23) - 127 + 2, 126) : t_exp;
-            const float m_same = m_run > kPagedNone ? m_run + static_cast<float>(e - t_exp) : m_run, m_new = fmaxf(m_same, mx - (kChunkLift4 - static_cast<float>(e)));
-            rescale(__builtin_amdgcn_exp2f(m_run - m_new));
+            const float m_new = fmaxf(m_ref, rintf(mx));
+            rescale(__builtin_amdgcn_exp2f((m_ref - m_new) + static_cast<float>(t_exp - e)));
             t_exp = e;
-            m_run = m_new;
+            m_ref = m_new;
+            far = __any((fabsf(m_ref) >= 0x1p22f) & (m_ref > kPagedNone));
         }
-        if (odd) weigh<true>(x, ts);
+        if (odd | far) weigh<true>(x, ts);
         else weigh<false>(x, ts);
     }
-    // Scores -> probabilities, times their values' scales, as operands; the probabilities' sum.  ODD: a scale may be no number, and a probability of zero then
-    // takes no part; one of a key that is seen is never zero.
+    // Scores -> probabilities, times their values' scales, as operands; the probabilities' sum.  ODD: m_ref and off apart, and a scale may be no number: a key
+    // that is not seen then takes no part.
     template <bool ODD>
     __device__ __forceinline__ void weigh(Scales& x, const float* ts) {
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float m = ODD ? m_ref : m_ref - off();
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
             const float4_t t4 = x.k[g & 3];
@@ -339,9 +344,9 @@ struct Columns4 {
                 float w[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float at = fmaf(st[kf][4 * q4 + r + i], up, -m_run), e = __builtin_amdgcn_exp2f(ODD ? (at < -100.0f && at > -INFINITY ? -100.0f : at) : at);
+                    const float at = fmaf(st[kf][4 * q4 + r + i], up, -m), e = __builtin_amdgcn_exp2f(ODD ? at + off() : at);
                     sum[q4] += e;
-                    w[i] = ODD && e == 0.0f ? 0.0f : e * t4[r + i];
+                    w[i] = ODD && at == -INFINITY ? 0.0f : e * t4[r + i];
                 }
                 pf[kf * 2 + (q4 >> 1)][2 * (q4 & 1) + (r >> 1)] = H::pack(w[0], w[1]);
             }
@@ -367,13 +372,16 @@ struct Columns4 {
             float* dst = p.part + ((static_cast<size_t>(s.row0 + qi) * p.nh + head) * p.ranges + z) * part_stride(D);
             if (lhi == 0) dst[D + 2] = static_cast<float>(ranges);
             if (ranges > 1) {
+                // `off` goes into the reference point, or (m_ref too large to hold it) into the sums
+                const bool whole = fabsf(m_ref) < 0x1p22f;
+                const float by = whole ? 1.0f : __builtin_amdgcn_exp2f(-off());
 #pragma unroll
                 for (int f = 0; f < DF; ++f)
 #pragma unroll
                     for (int q4 = 0; q4 < 4; ++q4)
                         *reinterpret_cast<float4_t*>(dst + f * 32 + 8 * q4 + 4 * lhi) =
-                            float4_t{o[f][4 * q4] * 0x1p24f, o[f][4 * q4 + 1] * 0x1p20f, o[f][4 * q4 + 2] * 0x1p24f, o[f][4 * q4 + 3] * 0x1p20f};
-                if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{m_run, l_tot};
+                            float4_t{o[f][4 * q4] * 0x1p24f * by, o[f][4 * q4 + 1] * 0x1p20f * by, o[f][4 * q4 + 2] * 0x1p24f * by, o[f][4 * q4 + 3] * 0x1p20f * by};
+                if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{whole ? m_ref - off() : m_ref, l_tot * by};
                 return;
             }
         }

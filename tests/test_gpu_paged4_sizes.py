@@ -1,0 +1,89 @@
+"""Attention over pages in 4 bits on the GPU (run with -m gpu) where sizes meet: scores of any size with values of any size, values near the end of
+their type, values that a row does not see and that are far larger than its own.  Every kernel form: a workgroup per sequence, spans, few columns, chunks with
+and without key ranges."""
+import math
+
+import pytest
+import torch
+
+from tests.kv4_helpers import pack, random_cache4, unpack, values64
+from tests.paged_helpers import TINY, U, attend64, ints, offsets
+
+pytestmark = pytest.mark.gpu
+
+# new tokens, tokens before them, heads per kv head, kv heads, room for as many tokens in a slot (where it is the call's bound on the keys, and large, small
+# calls take the chunk kernel with key ranges)
+FORMS = {"one": ([1, 1, 1], [700, 90, 5], 4, 2, 0), "spans": ([1, 1], [5000, 900], 4, 2, 0), "few": ([9, 5], [247, 60], 4, 2, 0),
+         "ranges": ([150, 90], [106, 40], 4, 2, 1 << 18), "long": ([150], [7000], 4, 2, 0), "full": ([600] * 4, [0, 37, 64, 5], 4, 8, 0)}
+
+
+@pytest.fixture(scope="module")
+def qt():
+    import paper_2602_10431_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def _rescaled(kv, dense, keys, factor):
+    """Scales of keys or values times `factor` ([n_pages, nkv, page] or a number), in the pages and beside them."""
+    pool, d, dtype = (kv.k if keys else kv.v), kv.head_dim, kv.dtype
+    codes, scale, zero = unpack(pool, d, keys, dtype)
+    scale = (scale.double() * factor).to(dtype)
+    pool.copy_(pack(codes, scale, zero, keys))
+    setattr(dense, "k" if keys else "v", values64(codes, scale, zero).cuda())
+    return torch.nan_to_num(scale.double()).cuda()
+
+
+def _call(qt, form, dtype, d, seed, q_size=1.0, page=32):
+    new, old, rep, nkv, room = FORMS[form]
+    lens = [o + n for o, n in zip(old, new)]
+    kv, slots, dense = random_cache4(qt, lens, page, nkv, d, dtype, seed, max_extra=max(room // page, 1))
+    q = (q_size * torch.randn(sum(new), rep * nkv, d, generator=torch.Generator().manual_seed(seed + 1))).to(dtype).cuda()
+    def attend(scale=None, window=0, sinks=0):
+        return qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), scale=scale, window=window, sinks=sinks,
+                                        max_new=max(new), max_len=room or max(lens))
+    return kv, slots, dense, q, new, old, attend
+
+
+def _best(kv, dense, q, new, old, slots):
+    """Of each (row, head): the value of the key with the largest score, how far the next one is behind, sum of |query| times the largest |key|."""
+    T, nh, d = q.shape
+    want, gap, size = torch.zeros(T, nh, d, dtype=torch.float64, device="cuda"), torch.zeros(T, nh, device="cuda"), torch.zeros(T, nh, device="cuda")
+    at, rep = 0, nh // kv.n_kv_heads
+    for b, n in enumerate(new):
+        length, row = int(kv.kv_len[0, slots[b]]), kv.table[0, slots[b]].tolist()
+        where = torch.arange(length, device="cuda")
+        page, place = torch.tensor([row[j // kv.page_size] for j in range(length)], device="cuda"), where % kv.page_size
+        hidden = where[None] > (old[b] + torch.arange(n, device="cuda"))[:, None]
+        for h in range(nh):
+            k, v = (x[page, h // rep, place] for x in (dense.k, dense.v))
+            x = q[at: at + n, h].double()
+            z, i = (x @ k.t().contiguous()).masked_fill(hidden, -math.inf).topk(2, 1)
+            want[at: at + n, h], gap[at: at + n, h] = v[i[:, 0]], (z[:, 0] - z[:, 1]).float()
+            size[at: at + n, h] = (x.abs().sum(1) * k.abs().max()).float()
+        at += n
+    return want, gap, size
+
+
+VALUES = [(torch.float16, f) for f in (2.0 ** -18, 2.0 ** -10, 1.0, 2.0 ** 4)] + [(torch.bfloat16, f) for f in (2.0 ** -40, 2.0 ** -18, 1.0, 2.0 ** 20, 2.0 ** 60)]
+
+
+@pytest.mark.parametrize("dtype,factor", VALUES)
+@pytest.mark.parametrize("form", list(FORMS))
+def test_scores_of_any_size_with_values_of_any_size(qt, form, dtype, factor):
+    # one key per row is far ahead of all others: the output is its value.  Scores from 2^20 to 2^75.
+    for d in (64, 128):
+        kv, slots, dense, q, new, old, attend = _call(qt, form, dtype, d, 13, q_size=30.0)
+        scales = _rescaled(kv, dense, False, factor)
+        want, gap, size = _best(kv, dense, q, new, old, slots)
+        for scale in (2.0 ** 13, 2.0 ** 16, 2.0 ** 18, 2.0 ** 19, 1.3 * 2.0 ** 20, 2.0 ** 22, 1e20):
+            out = attend(scale)
+            # ahead by 100 nats, and by more than two scores are off: sums of d products and of the zero point's, 2^-24 of the magnitudes' sum per addition
+            # (the magnitude of a code apart from its zero point is at most twice the row's largest value)
+            clear = (gap * scale > 100) & (gap > 4 * (d + 8) * 2.0 ** -24 * size)
+            assert int(clear.sum()) > clear.numel() // 3
+            # a probability of one times the value's scale as fp16, sums of codes and zero points up to 15 apart in 32 bits, the output's rounding
+            bound = (2 * U[dtype] if dtype == torch.float16 else U[dtype] + 2.0 ** -11) * want.abs() + 2.0 ** -20 * want.abs() \
+                + 30 * scales.max() * 4 * 2.0 ** -24 + TINY[dtype]
+            wrong = ~((out.double() - want).abs() <= bound) & clear[..., None]
+            assert not bool(wrong.any()), (d, scale, wrong.nonzero()[:3].tolist(), out[wrong][:3].tolist(), want[wrong][:3].tolist())
