@@ -22,7 +22,7 @@ namespace qtale {
 
 constexpr int kStepKeys = 32;                    // per wave
 constexpr int kUnitSteps = 4;                    // spans are cut at multiples of this: a step per wave
-constexpr float kLift4 = 12.0f;                  // the largest probability is 2^12 when the reference point moves (kDecodeLift)
+constexpr float kLift4 = 0x1p12f;                // the largest probability goes in as 2^12 when the reference point moves (kDecodeLift)
 
 // Units of a sequence in a call with spans; 0: not this kernel's.  A sequence without keys has one, in which its zeros are written.
 __device__ __forceinline__ int seq_units4(const PagedAttnDev& p, int b) {
@@ -159,8 +159,9 @@ again:                                                           // the pieces o
         unq = ldexpf(p.scale_log2, e + 24 - 13);
     }
 
-    // probabilities are 2^(score - m_run), the largest about 2^kLift4; values' scales go in relative to t_ref
-    float m_run = kPagedNone, l_run = 0.0f, t_ref = 0x1p-100f, t_inv = 0x1p100f;
+    // probabilities are 2^(score - m_run), m_run a score itself (less a lift it would be rounded, and from 2^27 on by more than fp16 has room for); the lift goes
+    // in with the values' scales, which are relative to t_ref
+    float m_run = kPagedNone, l_run = 0.0f, t_ref = 0x1p-100f, t_inv = kLift4 * 0x1p100f;
     float4_t o[F + 1];                                           // (the last: zero points)
 #pragma unroll
     for (int f = 0; f <= F; ++f) o[f] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -193,12 +194,12 @@ again:                                                           // the pieces o
         float mx = sc[0], tx = t[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) { mx = fmaxf(mx, sc[e]); tx = fmaxf(tx, t[e]); }
-        if (__any((mx - m_run > kLift4 + kDecodeHead) | (tx > t_ref))) {
+        if (__any((mx - m_run > kDecodeHead) | (tx > t_ref))) {
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));              // the column's largest: all its lanes move together
             tx = fmaxf(tx, __shfl_xor(tx, 16, 64));
             tx = fmaxf(tx, __shfl_xor(tx, 32, 64));
-            const float m_new = mx - m_run > kLift4 + kDecodeHead ? mx - kLift4 : m_run;
+            const float m_new = mx - m_run > kDecodeHead ? mx : m_run;
             const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
             // the next power of two but one
             const float t_new = tx > t_ref ? fminf(ldexpf(1.0f, static_cast<int>(__float_as_uint(tx) >> 23) - 127 + 2), 0x1p126f) : t_ref;
@@ -210,7 +211,7 @@ again:                                                           // the pieces o
                 for (int r = 0; r < 4; ++r) o[f][r] *= beta;
             m_run = m_new;
             t_ref = t_new;
-            t_inv = 1.0f / t_new;
+            t_inv = kLift4 / t_new;
         }
         u32x4_t ph, zv;
 #pragma unroll
@@ -260,7 +261,7 @@ again:                                                           // the pieces o
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
     if (c < cols) {
-        const float unit = t_ref * 0x1p24f;
+        const float unit = t_ref * (0x1p24f / kLift4);
 #pragma unroll
         for (int f = 0; f < F; ++f)
 #pragma unroll

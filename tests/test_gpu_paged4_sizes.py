@@ -87,3 +87,32 @@ def test_scores_of_any_size_with_values_of_any_size(qt, form, dtype, factor):
                 + 30 * scales.max() * 4 * 2.0 ** -24 + TINY[dtype]
             wrong = ~((out.double() - want).abs() <= bound) & clear[..., None]
             assert not bool(wrong.any()), (d, scale, wrong.nonzero()[:3].tolist(), out[wrong][:3].tolist(), want[wrong][:3].tolist())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_the_largest_scale_meets_the_largest_score(qt, form, dtype):
+    # scales of a power of two, as references are made of, at the keys with the largest scores (one head per kv head, so that each has its own)
+    for d in (64, 128):
+        new, old, rep, nkv, room = FORMS[form]
+        lens = [o + n for o, n in zip(old, new)]
+        kv, slots, dense = random_cache4(qt, lens, 32, nkv, d, dtype, 41, max_extra=max(room // 32, 1))
+        q = torch.randn(1, nkv, d, generator=torch.Generator().manual_seed(42)).expand(sum(new), nkv, d).contiguous().to(dtype).cuda()
+        factor = torch.full((kv.n_pages, nkv, kv.page_size), 0.3125, dtype=torch.float64)
+        for b, n in enumerate(lens):
+            row = kv.table[0, slots[b]].tolist()
+            for h in range(nkv):
+                k = torch.stack([dense.k[row[j // 32], h, j % 32] for j in range(n)])
+                j = int((k @ q[0, h].double()).argmax())
+                factor[row[j // 32], h, j % 32] = 1.0
+        codes, scale, zero = unpack(kv.v, d, False, dtype)
+        scale = torch.where(scale.isnan(), scale, factor.to(dtype))
+        kv.v.copy_(pack(codes, scale, zero, False))
+        dense.v = values64(codes, scale, zero).cuda()
+        want, gap, size = _best(kv, dense, q, new, old, slots)
+        for scale in [2.0 ** x for x in (18.3, 19.6, 20.2, 20.7, 21.1, 21.6, 22.2, 22.7, 23.3, 24.1, 25.2)]:
+            out = qt.qtale_paged_attention(kv, 0, q, offsets(new), first=ints(old), slots=ints(slots), scale=scale, max_new=max(new), max_len=room or max(lens))
+            clear = (gap * scale > 100) & (gap > 4 * (d + 8) * 2.0 ** -24 * size)
+            bound = (U[dtype] + 2.0 ** -11 + 2.0 ** -20) * want.abs() + 120 * 2.0 ** -24 + TINY[dtype]
+            wrong = ~((out.double() - want).abs() <= bound) & clear[..., None]
+            assert not bool(wrong.any()), (d, scale, wrong.nonzero()[:3].tolist(), out[wrong][:3].tolist(), want[wrong][:3].tolist())
