@@ -385,15 +385,15 @@ struct Columns4 {
                 return;
             }
         }
-        const float inv = l_tot != 0.0f ? 0x1p20f / l_tot : 0.0f;   // a row that sees no key is zero
+        const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;   // (l_tot may be 2^-117); a row that sees no key is zero
         uint16_t* orow = p.out + (s.row0 + qi) * p.out_stride + head * D;
 #pragma unroll
         for (int f = 0; f < DF; ++f)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
                 u32x2_t w;
-                w[0] = Act16<BF16>::pack(o[f][4 * q4] * 16.0f * inv, o[f][4 * q4 + 1] * inv);
-                w[1] = Act16<BF16>::pack(o[f][4 * q4 + 2] * 16.0f * inv, o[f][4 * q4 + 3] * inv);
+                w[0] = Act16<BF16>::pack(o[f][4 * q4] * inv * 0x1p24f, o[f][4 * q4 + 1] * inv * 0x1p20f);
+                w[1] = Act16<BF16>::pack(o[f][4 * q4 + 2] * inv * 0x1p24f, o[f][4 * q4 + 3] * inv * 0x1p20f);
                 *reinterpret_cast<u32x2_t*>(orow + f * 32 + 8 * q4 + 4 * lhi) = w;
             }
     }

@@ -261,11 +261,11 @@ again:                                                           // the pieces o
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
     if (c < cols) {
-        const float unit = t_ref * (0x1p24f / kLift4);
+        constexpr float UNIT = 0x1p24f / kLift4;                 // (apart from t_ref, which may be 2^126)
 #pragma unroll
         for (int f = 0; f < F; ++f)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sm[wave][c][F * (4 * g + r) + f] = ((f & 1 ? o[f][r] * 0.0625f : o[f][r]) - o[F][r]) * unit;
+            for (int r = 0; r < 4; ++r) sm[wave][c][F * (4 * g + r) + f] = ((f & 1 ? o[f][r] * 0.0625f : o[f][r]) - o[F][r]) * UNIT * t_ref;
         if (g == 0) { sm[wave][c][D] = m_run; sm[wave][c][D + 1] = l_run; }
     }
     __syncthreads();

@@ -2,6 +2,7 @@
 their type, values that a row does not see and that are far larger than its own.  Every kernel form: a workgroup per sequence, spans, few columns, chunks with
 and without key ranges."""
 import math
+import types
 
 import pytest
 import torch
@@ -116,3 +117,27 @@ def test_the_largest_scale_meets_the_largest_score(qt, form, dtype):
             bound = (U[dtype] + 2.0 ** -11 + 2.0 ** -20) * want.abs() + 120 * 2.0 ** -24 + TINY[dtype]
             wrong = ~((out.double() - want).abs() <= bound) & clear[..., None]
             assert not bool(wrong.any()), (d, scale, wrong.nonzero()[:3].tolist(), out[wrong][:3].tolist(), want[wrong][:3].tolist())
+
+
+def _close(dense_scales, kv, dense, q, out, new, old, slots, window, sinks, scale, rows=None):
+    """Row by row, relative to what the row sees: probabilities with the value's scale as fp16 (2^-11 each, whatever the order of codes and zero points), scores
+    1e-4 (sums of up to 128 products whose magnitudes add up to less than 100 with the inputs here), exponentials and sums 2e-5, codes and zero points
+    summed apart 2^-24 * 30 per 32 keys of the row's mean scale."""
+    want, size = attend64(dense, 0, q, new, old, slots, window, sinks, scale)
+    step, _ = attend64(dense_scales, 0, q, new, old, slots, window, sinks, scale)
+    keys = max(o + n for o, n in zip(old, new))
+    bound = U[q.dtype] * want.abs() + (2.0 ** -11 + 1.2e-4) * size + 30 * (keys / 32 + 8) * 2.0 ** -24 * step + TINY[q.dtype]
+    wrong = ~((out.double() - want).abs() <= bound)
+    if rows is not None:
+        wrong &= rows[:, None, None]
+    assert not bool(wrong.any()), (wrong.nonzero()[:4].tolist(), out[wrong][:4].tolist(), want[wrong][:4].tolist())
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_values_near_the_end_of_their_type(qt, form):
+    # bf16 up to 10^34; their sums with probabilities stay in 32 bits
+    for d in (64, 128):
+        kv, slots, dense, q, new, old, attend = _call(qt, form, torch.bfloat16, d, 31)
+        scales = _rescaled(kv, dense, False, 2.0 ** 108)
+        steps = types.SimpleNamespace(k=dense.k, v=scales[..., None].expand_as(dense.v), table=kv.table, kv_len=kv.kv_len, n_kv_heads=kv.n_kv_heads, page_size=kv.page_size)
+        _close(steps, kv, dense, q, attend(), new, old, slots, 0, 0, d ** -0.5)
