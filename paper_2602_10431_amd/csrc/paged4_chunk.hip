@@ -87,7 +87,7 @@ struct Unpack4 {
     u32x4_t vp;
 
     __device__ __forceinline__ Unpack4(const PagedAttnDev& p, int hk, int part, int hi)
-        : p(p), hk(hk), part(part), hi(hi), params_at(static_cast<uint32_t>(D / 2) << p.shift), block(params_at + (4u << p.shift)), unit(p.scale_log2 * 0x1p24f) {}
+        : p(p), hk(hk), part(part), hi(hi), params_at(static_cast<uint32_t>(D / 2) << p.shift), block(params_at + (4u << p.shift)), unit(p.scale_log2 * 0x1p12f) {}
     static __device__ __forceinline__ Words load(__amdgpu_buffer_rsrc_t buf, uint32_t off, uint32_t base) {
         if constexpr (S == 4) return __builtin_amdgcn_raw_buffer_load_b128(buf, off, base, 0);
         else return __builtin_amdgcn_raw_buffer_load_b64(buf, off, base, 0);
@@ -173,7 +173,7 @@ struct Columns4 {
     bool mine;                                   // the lane's column exists
     int whole_from, whole_to, first_to;          // a tile that every query of the wave sees whole begins in whole_from .. whole_to, or not after first_to
     u32x4_t qf[KS], pf[4];
-    float up;                                    // the power of two that a score's unit stands for
+    float up;                                    // the power of two that a score's unit stands for, with half of the codes' 2^24 (keys' scales have the other)
     int k_at[KS], v_at[4];                       // LDS elements that this lane reads
     float16_t st[2], o[DF];
     float m_ref, l_run;
@@ -209,7 +209,7 @@ struct Columns4 {
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int w = 0; w < 4; ++w) qf[k][w] = H::pack(Act16<BF16>::low(qf[k][w]) * (w & 1 ? f16 : f), Act16<BF16>::high(qf[k][w]) * (w & 1 ? f16 : f));
-        up = ldexpf(1.0f, -move);
+        up = ldexpf(1.0f, 12 - move);
         // chunk 2 k + lhi of key l32; chunk 2 s2 + lhi of column 32 f + l32: v_at[(f ^ s2) & 3] + 32 f rows (the swizzle of that column is l32's with 2 f
         // flipped in)
 #pragma unroll

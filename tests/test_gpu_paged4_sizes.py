@@ -141,3 +141,15 @@ def test_values_near_the_end_of_their_type(qt, form):
         scales = _rescaled(kv, dense, False, 2.0 ** 108)
         steps = types.SimpleNamespace(k=dense.k, v=scales[..., None].expand_as(dense.v), table=kv.table, kv_len=kv.kv_len, n_kv_heads=kv.n_kv_heads, page_size=kv.page_size)
         _close(steps, kv, dense, q, attend(), new, old, slots, 0, 0, d ** -0.5)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_keys_near_the_end_of_their_type(qt, form):
+    # bf16 keys of 10^34 meet queries of 10^-34: ordinary scores
+    for d in (64, 128):
+        kv, slots, dense, q, new, old, attend = _call(qt, form, torch.bfloat16, d, 37, q_size=2.0 ** -112)
+        _rescaled(kv, dense, True, 2.0 ** 112)
+        _, scale, _ = unpack(kv.v, d, False, kv.dtype)
+        steps = types.SimpleNamespace(k=dense.k, v=torch.nan_to_num(scale.double()).cuda()[..., None].expand_as(dense.v), table=kv.table, kv_len=kv.kv_len,
+                                      n_kv_heads=kv.n_kv_heads, page_size=kv.page_size)
+        _close(steps, kv, dense, q, attend(), new, old, slots, 0, 0, d ** -0.5)
