@@ -5,9 +5,9 @@
 // operand, which the layout of a value page gives without permutations.  Scales stay outside the products:
 //   score = s_j (q . (c_j - z_j)),   out = sum_j (p_j t_j) (c'_j - z'_j) / sum_j p_j.
 // Queries are fp16; a row that is too large for it, or small, comes relative to its power of two.  Probabilities are 2^(score - m_ref + off): m_ref is a whole
-// number next to a score, off = kChunkLift4 - log2 t_ref with a power of two t_ref above all t so far, so that p t fits fp16 whatever the values' size, for one
-// multiplication.  Below 2^22 m_ref - off is exact and goes in as one number; larger scores, whose spacing in 32 bits is that of whole numbers and more, take
-// off apart, where an addition per score more does not show.
+// number next to a score, off = kChunkLift4 - log2 t_ref with a power of two t_ref above all t that the row has seen, so that p t fits fp16 whatever the values'
+// size, for one multiplication; it is off by 2^-11 of itself or 2^-31 of the largest p times the largest t.  Below 2^22 m_ref - off is exact and goes in as
+// one number; larger scores, whose spacing in 32 bits is that of whole numbers and more, take off apart, where an addition per score more does not show.
 //
 // What bounds it: a wave has 445 vector instructions and 120 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is two fifths
 // and the values' scales a tenth.  4 x 4096 tokens, 32 heads on 8 of 128, 0.72 to 0.75 ms, 730 to 760 TFLOP/s (16-bit pages 0.59 ms); 500 tokens on 24000 keys
@@ -176,8 +176,7 @@ struct Columns4 {
     float up;                                    // the power of two that a score's unit stands for, with half of the codes' 2^24 (keys' scales have the other)
     int k_at[KS], v_at[4];                       // LDS elements that this lane reads
     float16_t st[2], o[DF];
-    float m_ref, l_run;
-    int t_exp;                                   // log2 of t_ref
+    float m_ref, l_run, off;
     bool far;                                    // some row's m_ref is too large to hold `off` too (the same in all lanes)
 
     // columns .. c_hi; c0: the wave's first
@@ -222,10 +221,9 @@ struct Columns4 {
             for (int r = 0; r < 16; ++r) o[f][r] = 0.0f;
         m_ref = kPagedNone;
         l_run = 0.0f;
-        t_exp = -60;
+        off = kChunkLift4 + 60.0f;
         far = false;
     }
-    __device__ __forceinline__ float off() const { return kChunkLift4 - static_cast<float>(t_exp); }
 
     __device__ __forceinline__ u32x4_t operand(const uint16_t* V, const uint16_t* K, int i) const {
         if (i < PV) {
@@ -283,7 +281,6 @@ struct Columns4 {
             odds |= u;
         }
         const bool odd = (odds >> 31) != 0;
-        const float tx = __uint_as_float(most);
         // products -> scores (in units of `up`)
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
@@ -316,12 +313,22 @@ struct Columns4 {
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * up;
         // The reference point stays as long as no probability passes 2^15 t_ref^-1 and no value's scale t_ref.  It moves so that the largest probability is about
         // 2^kChunkLift4 t_ref^-1, and t_ref to the next power of two but one.
-        const bool larger = tx > ldexpf(1.0f, t_exp);
-        if (larger || __any(mx - m_ref > 15.0f - kChunkLift4)) {
-            const int e = larger ? min(static_cast<int>(__float_as_uint(tx) >> 23) - 127 + 2, 126) : t_exp;
-            const float m_new = fmaxf(m_ref, rintf(mx));
-            rescale(__builtin_amdgcn_exp2f((m_ref - m_new) + static_cast<float>(t_exp - e)));
-            t_exp = e;
+        auto room = [](uint32_t t) { return kChunkLift4 + 127.0f - static_cast<float>(t >> 23); };   // of `off`: with less than 1 left such a scale may pass t_ref
+        if (__any((mx - m_ref > 15.0f - kChunkLift4) | (room(most) < off + 1.0f))) {
+            if (!all && __any(room(most) < off + 1.0f)) {        // the largest scale that the row sees (others may be anything)
+                most = 0;
+#pragma unroll
+                for (int kf = 0; kf < 2; ++kf)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t t = __float_as_uint(ts[kf * 32 + 8 * (r >> 2) + (r & 3)]) & 0x7fffffffu;
+                        most = max(most, ((st[kf][r] > -INFINITY) & (t < 0x7f800000u)) ? t : 0u);
+                    }
+                most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32, 64)));
+            }
+            const float m_new = fmaxf(m_ref, rintf(mx)), off_new = room(most) < off + 1.0f ? room(most) - 2.0f : off;
+            rescale(__builtin_amdgcn_exp2f((m_ref - m_new) + (off_new - off)));
+            off = off_new;
             m_ref = m_new;
             far = __any((fabsf(m_ref) >= 0x1p22f) & (m_ref > kPagedNone));
         }
@@ -333,7 +340,7 @@ struct Columns4 {
     template <bool ODD>
     __device__ __forceinline__ void weigh(Scales& x, const float* ts) {
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        const float m = ODD ? m_ref : m_ref - off();
+        const float m = ODD ? m_ref : m_ref - off;
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
             const float4_t t4 = x.k[g & 3];
@@ -344,7 +351,7 @@ struct Columns4 {
                 float w[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float at = fmaf(st[kf][4 * q4 + r + i], up, -m), e = __builtin_amdgcn_exp2f(ODD ? at + off() : at);
+                    const float at = fmaf(st[kf][4 * q4 + r + i], up, -m), e = __builtin_amdgcn_exp2f(ODD ? at + off : at);
                     sum[q4] += e;
                     w[i] = ODD && at == -INFINITY ? 0.0f : e * t4[r + i];
                 }
@@ -374,18 +381,18 @@ struct Columns4 {
             if (ranges > 1) {
                 // `off` goes into the reference point, or (m_ref too large to hold it) into the sums
                 const bool whole = fabsf(m_ref) < 0x1p22f;
-                const float by = whole ? 1.0f : __builtin_amdgcn_exp2f(-off());
+                const float by = whole ? 1.0f : __builtin_amdgcn_exp2f(-off);
 #pragma unroll
                 for (int f = 0; f < DF; ++f)
 #pragma unroll
                     for (int q4 = 0; q4 < 4; ++q4)
                         *reinterpret_cast<float4_t*>(dst + f * 32 + 8 * q4 + 4 * lhi) =
                             float4_t{o[f][4 * q4] * 0x1p24f * by, o[f][4 * q4 + 1] * 0x1p20f * by, o[f][4 * q4 + 2] * 0x1p24f * by, o[f][4 * q4 + 3] * 0x1p20f * by};
-                if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{whole ? m_ref - off() : m_ref, l_tot * by};
+                if (lhi == 0) *reinterpret_cast<float2_t*>(dst + D) = float2_t{whole ? m_ref - off : m_ref, l_tot * by};
                 return;
             }
         }
-        const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;   // (l_tot may be 2^-117); a row that sees no key is zero
+        const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;   // (l_tot may be 2^-120); a row that sees no key is zero
         uint16_t* orow = p.out + (s.row0 + qi) * p.out_stride + head * D;
 #pragma unroll
         for (int f = 0; f < DF; ++f)

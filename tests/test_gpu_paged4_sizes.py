@@ -153,3 +153,26 @@ def test_keys_near_the_end_of_their_type(qt, form):
         steps = types.SimpleNamespace(k=dense.k, v=torch.nan_to_num(scale.double()).cuda()[..., None].expand_as(dense.v), table=kv.table, kv_len=kv.kv_len,
                                       n_kv_heads=kv.n_kv_heads, page_size=kv.page_size)
         _close(steps, kv, dense, q, attend(), new, old, slots, 0, 0, d ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,own,other", [(torch.float16, 2.0 ** -13, 2.0 ** 13), (torch.bfloat16, 1.0, 2.0 ** 70), (torch.bfloat16, 2.0 ** -70, 1.0)])
+@pytest.mark.parametrize("form", ["few", "ranges", "long", "full"])
+def test_values_that_a_row_does_not_see(qt, form, dtype, own, other):
+    # the last token of each sequence, which its last row alone sees, has far larger values; and the first token, which no row sees under the window
+    for d, window in ((64, 0), (128, 0), (128, 40)):
+        kv, slots, dense, q, new, old, attend = _call(qt, form, dtype, d, 29)
+        factor = torch.full((kv.n_pages, 1, kv.page_size), own, dtype=torch.float64)
+        for b, n in enumerate(new):
+            row, last = kv.table[0, slots[b]].tolist(), old[b] + n - 1
+            factor[row[last // kv.page_size], 0, last % kv.page_size] = other
+            if window:
+                factor[row[0], 0, 0] = other
+        scales = _rescaled(kv, dense, False, factor)
+        steps = types.SimpleNamespace(k=dense.k, v=scales[..., None].expand_as(dense.v), table=kv.table, kv_len=kv.kv_len, n_kv_heads=kv.n_kv_heads, page_size=kv.page_size)
+        rows = torch.ones(sum(new), dtype=torch.bool, device="cuda")
+        rows[(offsets(new)[1:] - 1).long()] = False               # (their sums are those of the large values)
+        out = attend(window=window)
+        if window:                                                # rows whose window reaches the first token
+            place = torch.cat([torch.arange(o, o + n) for o, n in zip(old, new)]).cuda()
+            rows &= place >= window
+        _close(steps, kv, dense, q, out, new, old, slots, window, 0, d ** -0.5, rows)
