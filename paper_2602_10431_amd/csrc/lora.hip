@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(256)
 lora_pack_kernel(LoraPack p) {
     const LoraDev& l = p.l[blockIdx.y];
     const int M = p.rows.count ? min(*p.rows.count, p.rows.M) : p.rows.M;
+    if (static_cast<int>(blockIdx.x) * 16 >= M) return;          // (M on the device may be 0: there is no row then to load in the others' place)
     const int row = blockIdx.x * 16 + (threadIdx.x >> 4), r0 = 8 * (threadIdx.x & 15), at_row = min(row, M - 1);
     const size_t stride = static_cast<size_t>(p.rows.M) * l.R;
     const float* from = p.inner[blockIdx.y] + static_cast<size_t>(at_row) * l.R + min(r0, l.R - 8);
