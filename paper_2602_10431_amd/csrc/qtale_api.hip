@@ -788,6 +788,12 @@ int check_layer_lora(const qtale_layer_cfg* c, const qtale_layer_lora* l, int* m
     return QTALE_OK;
 }
 
+bool has_adapters(const qtale_layer_lora& l) {
+    for (const qtale_lora* x : {&l.q, &l.k, &l.v, &l.o, &l.gate, &l.up, &l.down})
+        if (x->n_adapters > 0) return true;
+    return false;
+}
+
 // loras and adapter: both or neither
 int paged_stack(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, const qtale_layer_lora* loras, int n_layers, int first_layer,
                 void* x, int T, const int32_t* seq_offsets, int B, const int32_t* positions, const qtale_paged_kv* kv, const int32_t* slots,
@@ -836,9 +842,11 @@ int paged_stack(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_we
         }
         pc.layer = first_layer + l;
         pc.missing = missing ? missing + l : nullptr;
-        if (max_rank > 0) lc.layer = &loras[l];
+        // (a layer without adapters runs as it does in a stack that has none)
+        const bool adapted = max_rank > 0 && has_adapters(loras[l]);
+        if (adapted) lc.layer = &loras[l];
         e = layer_forward_impl(ctx, cfg, &layers[l], x, T, seq_offsets, B, positions, nullptr, sel_idx ? sel_idx + static_cast<size_t>(l) * T : nullptr,
-                               sel_count ? sel_count + l : nullptr, scores ? scores + static_cast<size_t>(l) * T : nullptr, ws, s, &link, &pc, max_rank > 0 ? &lc : nullptr);
+                               sel_count ? sel_count + l : nullptr, scores ? scores + static_cast<size_t>(l) * T : nullptr, ws, s, &link, &pc, adapted ? &lc : nullptr);
         if (e) return e;
         scores_ready = link.next_scored;
     }
