@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import synth_inputs as si
+from tests.kv4_precision import ADAPTERS16, GATED16, norm_error
 from tests.test_gpu_lora import _adapters, _base, _expect, _ids
 from tests.test_gpu_serving_stack import NAMES, _run
 
@@ -78,3 +79,16 @@ def test_layers(qt, r, names):
 def test_layers_of_more_rows_than_a_small_tile_is_for(qt):
     shape = si.LayerShape(256, 4, 2, 64, 512, 4, 32, "fp16")
     _run(qt, shape, 4, NAMES, [[600, 300, 640, 620]], "ratio", 1.0, 71, r=72, page=64)
+
+
+@pytest.mark.parametrize("M", [1, 3, 16, 64, 200, 300, 2100])
+@pytest.mark.parametrize("r", [16, 60, 128])
+def test_precision(qt, M, r):
+    N, K = 1032, 1024
+    (qg, g64), (qu, u64) = _base(qt, N, K, 4, 128, 5), _base(qt, N, K, 4, 128, 6)
+    (lg, dg, ug), (lu, du, uu) = _adapters(qt, 4, r, N, K, 7), _adapters(qt, 4, r, N, K, 8)
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).half().cuda()
+    ids = torch.arange(M, dtype=torch.int32).cuda() % 4
+    (g, _), (u, _) = _expect(g64, lg, dg, ug, x, ids), _expect(u64, lu, du, uu, x, ids)
+    assert norm_error(qt.qtale_linear_lora_w4a16(qg, lg, x, ids), g) <= ADAPTERS16
+    assert norm_error(qt.qtale_swiglu_lora_w4a16(qg, qu, lg, lu, x, ids), g * torch.sigmoid(g) * u) <= GATED16
