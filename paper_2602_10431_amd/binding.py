@@ -555,11 +555,12 @@ def _lora_out(out, M, N, A):
 def qtale_linear_lora_w4a16(qlin, lora, A, adapter, out=None, workspace=None):
     """qtale_linear_w4a16 with row i's adapter adapter[i] of `lora` beside it (int32 [M]; a number that names none: no adapter)."""
     M = A.shape[0]
+    ids, rows = _lora_rows(adapter, A, lora, qlin.K)
+    assert qlin.prepacked.device == lora.device
     out = _lora_out(out, M, qlin.N, A)
     if workspace is None:
         workspace = alloc_lora_workspace([lora], M)
     s = qlin.c_struct()
-    ids, rows = _lora_rows(adapter, A, lora, qlin.K)
     _check(load_library().qtale_linear_lora_w4a16(C.byref(s), qlin.bits, qlin.group, lora._ref, ids, rows, M, out.data_ptr(),
                                                   *_scratch(workspace, lora), _stream_of(lora)), "qtale_linear_lora_w4a16")
     return out
@@ -568,12 +569,13 @@ def qtale_linear_lora_w4a16(qlin, lora, A, adapter, out=None, workspace=None):
 def qtale_swiglu_lora_w4a16(gate, up, lora_gate, lora_up, A, adapter, out=None, workspace=None):
     """qtale_swiglu_w4a16 with adapters on gate and up (either may be None)."""
     M, lora = A.shape[0], lora_gate or lora_up
+    ids, rows = _lora_rows(adapter, A, lora, gate.K)
+    assert up.bits == gate.bits and up.group == gate.group
+    assert gate.prepacked.device == up.prepacked.device == lora.device and (lora_up is None or lora_up.device == lora.device)
     out = _lora_out(out, M, gate.N, A)
     if workspace is None:
         workspace = alloc_lora_workspace([lora_gate, lora_up], M)
     g, u = gate.c_struct(), up.c_struct()
-    ids, rows = _lora_rows(adapter, A, lora, gate.K)
-    assert up.bits == gate.bits and up.group == gate.group
     _check(load_library().qtale_swiglu_lora_w4a16(
         C.byref(g), C.byref(u), gate.bits, gate.group, lora_gate._ref if lora_gate else None, lora_up._ref if lora_up else None, ids, rows, M,
         out.data_ptr(), *_scratch(workspace, lora), _stream_of(lora)), "qtale_swiglu_lora_w4a16")
@@ -803,6 +805,7 @@ class StackLora:
             assert set(l) <= set(names), sorted(l)
         self.layers, self.n = layers, len(layers)
         self.max_rank = max([x.max_rank for l in layers for x in l.values()] + [0])
+        self.devices = {x.device for l in layers for x in l.values()}
         none = qtale_lora(None, None, None, None, 0, 0, 0, 0)
         self._c = (qtale_layer_lora * self.n)(*[qtale_layer_lora(*[l[n].c_struct() if n in l else none for n in names]) for l in layers])
 
@@ -825,7 +828,8 @@ def qtale_paged_stack_forward(ctx, stack, x, seq_offsets, positions, kv, rope, s
     T = x.shape[0]
     B = seq_offsets.numel() - 1
     assert stack.kvs is None and rope.freqs.device == kv.device and x.device == kv.device and x.is_contiguous()
-    assert (loras is None) == (adapter is None) and (loras is None or loras.n == stack.n)
+    assert (loras is None) == (adapter is None) and (loras is None or (loras.n == stack.n and loras.devices <= {kv.device}))
+    ids = _ints(adapter, kv, B)
     if workspace is None:
         workspace = alloc_paged_stack_workspace(stack.cfg, kv, T, B, loras)
     attn = _paged_attn(kv, stack.cfg.n_heads, max_new, max_len, window, sinks, scale)
@@ -836,7 +840,7 @@ def qtale_paged_stack_forward(ctx, stack, x, seq_offsets, positions, kv, rope, s
     if loras is None:
         _check(lib.qtale_paged_stack_forward(*before, *tokens, *after), "qtale_paged_stack_forward")
     else:
-        _check(lib.qtale_paged_stack_lora_forward(*before, loras._c, *tokens, _ints(adapter, kv, B), *after), "qtale_paged_stack_lora_forward")
+        _check(lib.qtale_paged_stack_lora_forward(*before, loras._c, *tokens, ids, *after), "qtale_paged_stack_lora_forward")
 
 
 def qtale_profile_enable(ctx, on):
