@@ -92,3 +92,16 @@ def test_precision(qt, M, r):
     (g, _), (u, _) = _expect(g64, lg, dg, ug, x, ids), _expect(u64, lu, du, uu, x, ids)
     assert norm_error(qt.qtale_linear_lora_w4a16(qg, lg, x, ids), g) <= ADAPTERS16
     assert norm_error(qt.qtale_swiglu_lora_w4a16(qg, qu, lg, lu, x, ids), g * torch.sigmoid(g) * u) <= GATED16
+
+
+@pytest.mark.parametrize("M", [1, 5, 40, 200, 300, 2100])
+def test_gated_rows_without_an_adapter_are_those_of_the_plain_pair(qt, M):
+    # the same sums in 32 bits, or in another order, and silu in 32 bits: 2^-19 of the value, so that one in a hundred rounds to the neighbouring fp16 number
+    N, K = 1032, 1024
+    (qg, _), (qu, _) = _base(qt, N, K, 4, 128, 5), _base(qt, N, K, 4, 128, 6)
+    lora, _, _ = _adapters(qt, 4, 16, N, K, 7)
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).half().cuda()
+    ids = torch.where(torch.arange(M) % 3 == 0, -1, 7).int().cuda()
+    got, want = qt.qtale_swiglu_lora_w4a16(qg, qu, lora, lora, x, ids), qt.qtale_swiglu_w4a16(qg, qu, x)
+    assert bool(((got.double() - want.double()).abs() <= 2.0 ** -10 * want.double().abs() + 2.0 ** -22).all())
+    assert float((got != want).double().mean()) <= 0.02
