@@ -4,10 +4,11 @@
 // queries' elements or taken from the result), exact, into LDS, K as [key][d], V transposed as [column][key] in the order of the second product's
 // operand, which the layout of a value page gives without permutations.  Scales stay outside the products:
 //   score = s_j (q . (c_j - z_j)),   out = sum_j (p_j t_j) (c'_j - z'_j) / sum_j p_j.
-// Queries are fp16; a row that is too large for it, or small, comes relative to its power of two.  Probabilities are 2^(score - m_ref + off): m_ref is a whole
-// number next to a score, off = kChunkLift4 - log2 t_ref with a power of two t_ref above all t that the row has seen, so that p t fits fp16 whatever the values'
-// size, for one multiplication; it is off by 2^-11 of itself or 2^-31 of the largest p times the largest t.  Below 2^22 m_ref - off is exact and goes in as
-// one number; larger scores, whose spacing in 32 bits is that of whole numbers and more, take off apart, where an addition per score more does not show.
+// Queries are fp16; a row that is too large for it, or small, comes relative to its power of two.  Probabilities are 2^(score - m_ref + off): m_ref is a score
+// (below 128: to a multiple of 2^-16), off = kChunkLift4 - log2 t_ref with a power of two t_ref above all t that the row has seen, so that p t fits fp16 whatever the values'
+// size, for one multiplication; it is off by 2^-11 of itself or 2^-31 of the largest p times the largest t (but not where p is a power of two, as that of the
+// score at m_ref is).  Mostly 32 bits hold m_ref - off exactly, and it goes in as one number; else, as for scores whose spacing is that of whole numbers, off
+// goes in apart, an addition per score more.
 //
 // What bounds it: a wave has 445 vector instructions and 120 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is two fifths
 // and the values' scales a tenth.  4 x 4096 tokens, 32 heads on 8 of 128, 0.72 to 0.75 ms, 730 to 760 TFLOP/s (16-bit pages 0.59 ms); 500 tokens on 24000 keys
@@ -177,7 +178,7 @@ struct Columns4 {
     int k_at[KS], v_at[4];                       // LDS elements that this lane reads
     float16_t st[2], o[DF];
     float m_ref, l_run, off;
-    bool far;                                    // some row's m_ref is too large to hold `off` too (the same in all lanes)
+    bool far;                                    // some row's m_ref - off is not exact (the same in all lanes)
 
     // columns .. c_hi; c0: the wave's first
     __device__ __forceinline__ Columns4(const PagedAttnDev& p, const SeqView& s, int hk, int c0, int c_hi, int hi) {
@@ -224,6 +225,9 @@ struct Columns4 {
         off = kChunkLift4 + 60.0f;
         far = false;
     }
+
+    // m_ref - off is exact: what its subtraction lost (|off| <= 120; below 128 nothing is lost) is zero.
+    __device__ __forceinline__ bool near() const { return (m_ref - (m_ref - off)) - off == 0.0f; }
 
     __device__ __forceinline__ u32x4_t operand(const uint16_t* V, const uint16_t* K, int i) const {
         if (i < PV) {
@@ -326,11 +330,11 @@ struct Columns4 {
                     }
                 most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32, 64)));
             }
-            const float m_new = fmaxf(m_ref, rintf(mx)), off_new = room(most) < off + 1.0f ? room(most) - 2.0f : off;
+            const float m_new = fmaxf(m_ref, fabsf(mx) < 128.0f ? rintf(mx * 0x1p16f) * 0x1p-16f : mx), off_new = room(most) < off + 1.0f ? room(most) - 2.0f : off;
             rescale(__builtin_amdgcn_exp2f((m_ref - m_new) + (off_new - off)));
             off = off_new;
             m_ref = m_new;
-            far = __any((fabsf(m_ref) >= 0x1p22f) & (m_ref > kPagedNone));
+            far = __any(!near() & (m_ref > kPagedNone));
         }
         if (odd | far) weigh<true>(x, ts);
         else weigh<false>(x, ts);
@@ -379,8 +383,8 @@ struct Columns4 {
             float* dst = p.part + ((static_cast<size_t>(s.row0 + qi) * p.nh + head) * p.ranges + z) * part_stride(D);
             if (lhi == 0) dst[D + 2] = static_cast<float>(ranges);
             if (ranges > 1) {
-                // `off` goes into the reference point, or (m_ref too large to hold it) into the sums
-                const bool whole = fabsf(m_ref) < 0x1p22f;
+                // `off` goes into the reference point, or (not exact there) into the sums
+                const bool whole = near();
                 const float by = whole ? 1.0f : __builtin_amdgcn_exp2f(-off);
 #pragma unroll
                 for (int f = 0; f < DF; ++f)
