@@ -239,7 +239,7 @@ int qtale_swiglu_w4a16(const qtale_qlinear* gate, const qtale_qlinear* up, int b
  * Row i of a call has adapter a = adapter[i] (int32 device [M]; a number outside 0 .. n_adapters - 1: none):
  *   y_i = W A_i + scale[a] * up_a (down_a A_i),   W the quantized linear, sums in 32 bits.
  * The inner values down_a A_i are held in 32 bits between the two products; they enter the second one as fp16 of their row's power of two.
- * The shared product is rounded to fp16 where it leaves its kernel, and the sum once more. */
+ * The shared product, of weights fp16((code - zero) * scale) as in qtale_linear_w4a16, stays in 32 bits; the sum is rounded, once. */
 typedef struct {
     const void* down;          /* [n_adapters][max_rank][K] fp16, 16-byte aligned */
     const void* up;            /* [n_adapters][N][max_rank] fp16, 16-byte aligned */
@@ -431,7 +431,8 @@ int qtale_paged_stack_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const 
 
 /* qtale_paged_stack_forward with adapters: loras host [n_layers], whose linears without an adapter have n_adapters = 0 (the rest is then not read);
  * adapter [B] int32 device: that of each sequence of the call, one number for all linears and layers (outside a linear's adapters: none).
- * workspace >= qtale_paged_stack_lora_workspace_bytes(cfg, kv, max_rank, T, B) with the largest max_rank. */
+ * workspace >= qtale_paged_stack_lora_workspace_bytes(cfg, kv, max_rank, T, B) with the largest max_rank.  (All rows of a layer are done at once: 8 * inter bytes
+ * of it per token for gate and up, 2.9 GB for 32768 tokens with inter = 11008.  Calls of fewer tokens need less.) */
 typedef struct { qtale_lora q, k, v, o, gate, up, down; } qtale_layer_lora;
 size_t qtale_paged_stack_lora_workspace_bytes(const qtale_layer_cfg* cfg, const qtale_paged_kv* kv, int max_rank, int max_tokens, int max_seqs);
 int qtale_paged_stack_lora_forward(qtale_ctx* ctx, const qtale_layer_cfg* cfg, const qtale_layer_weights* layers, const qtale_layer_lora* loras,

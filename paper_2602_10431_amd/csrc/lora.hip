@@ -485,8 +485,10 @@ constexpr int kLoraAlone = 256;
 
 // Parts of K: workgroups that fill the chip, each wave with a unit of 128 columns at least.
 constexpr int kManyFill = 512;
-// Rows of a tile: more read less of down, if few adapters meet in one.  Tiles of 16 / 64, us: 3500 rows in requests of 500, 14336 -> 4096, 42 / 29; but 900
-// rows that all choose for themselves, 4096 -> 4096 as a whole, 116 / 205.
+// Rows of a tile: more read less of down, if few adapters meet in one.  Tiles of 16 / 64, us, the whole linear, 14336 -> 4096 with rank 32 in requests of 100: 512 rows
+// 112 / 121, 1024 160 / 166, 1536 241 / 238, 2048 302 / 281, 3000 445 / 436, 4000 549 / 518; of 500: 1024 158 / 166, 2048 282 / 278, 4000 522 / 506; of 25: 2048 306 / 314,
+// 4000 553 / 565.  4096 -> 4096 with rank 16 in requests of 100: 1024 62.5 / 64.7, 2048 103 / 100, 4000 178 / 174.  Rows that all choose for themselves lose by 64 at
+// every size (4096 -> 4096: 1024 121 / 212, 4000 332 / 423): so many rows are prompts.
 static int inner_tile(int M) { return M <= 2048 ? 16 : 64; }
 static int inner_parts(int M, int K, int n) {
     const int units = (K + 127) / 128;

@@ -10,9 +10,10 @@
 // score at m_ref is).  Mostly 32 bits hold m_ref - off exactly, and it goes in as one number; else, as for scores whose spacing is that of whole numbers, off
 // goes in apart, an addition per score more.
 //
-// What bounds it: a wave has 445 vector instructions and 120 scalar ones per tile beside 32 MFMAs (16-bit pages: 160), of which taking codes apart is two fifths
-// and the values' scales a tenth.  4 x 4096 tokens, 32 heads on 8 of 128, 0.72 to 0.75 ms, 730 to 760 TFLOP/s (16-bit pages 0.59 ms); 500 tokens on 24000 keys
-// 282 us.  Unpacking the next tile behind the scores' products, which run on, instead of before them: 0.78 -> 0.72 ms.
+// What bounds it: a wave has 449 vector instructions and 123 scalar ones per tile beside 32 MFMAs (counted, 4 x 4096 tokens; 16-bit pages: 163): nine for each of the
+// eight words that it takes apart, 64 multiplications by scales, and their loads, exchanges and addresses.  4 x 4096 tokens, 32 heads on 8 of 128, 0.73 to 0.75 ms, 730
+// to 755 TFLOP/s, after some 100 calls in a row (the first ones after a pause take up to 1.0: clocks; 16-bit pages 0.59 ms); 500 tokens on 24000 keys 273 us and 8 for
+// the ranges' sums.  Unpacking the next tile behind the scores' products, which run on, instead of before them: 0.78 -> 0.72 ms.
 // Eight waves on 256 columns whose halves take turns with the matrix cores and the vector ALUs, the best form for 16-bit pages, lose here, since the vector half
 // takes more than twice the other's time: 0.83 ms, 2 x 300 tokens on 6000 keys 139 us instead of 117, heads of 64 4 x 4096 700 instead of 548.
 #include <algorithm>

@@ -7,12 +7,12 @@
 //   score = s_j (q . c_j - z_j sum(q)),   out = sum_j (p_j t_j) (c'_j - z'_j) / sum_j p_j,
 // the sum with z' as one more fragment of the second product whose operand rows are all z', so that both parts see the same rounded p t.
 // Queries are fp16 relative to their row's power of two (exact, but for elements 2^-34 of the largest), whatever the cache's type, and p t is fp16
-// relative to a running power of two of t, which it follows upwards: it is off by 2^-11 of itself or 2^-37 of the largest, as the
-// output's own rounding is.  All codes are finite, so that a row reaches a NaN (scale) only through a key that it sees.
+// relative to a running power of two of the t that the row has seen, which it follows upwards: it is off by 2^-11 of itself, as the output's own rounding is, or by
+// 2^-35 of the largest p times the largest t.  (fp16 caches hardly reach that; a bf16 row that sees values 2^24 above those that it weighs loses bits.)  All codes are finite, so that a row reaches a NaN (scale) only through a key that it sees.
 //
 // A wave's step of 32 keys takes sixteen words of codes per lane apart (five instructions each) for 18 or 9 MFMAs.  What bounds it: HBM where all CUs are
-// filled, 64 x 4000 keys, 32 heads of 128, 171 us, 6.5 TB/s; else the time that a CU's own loads take: 33 x 3000 keys, 8 heads, 29 us and 4.2 for the
-// pieces, 3.3 TB/s; 48 x 4 tokens under a window of 1024, heads of 64, 17 us.  (The 16-bit cache takes 69 us for 33 x 3000, four times the bytes.)
+// filled, 64 x 4000 keys, 32 heads of 128, 171 us, 6.5 TB/s; else the time that a CU's own loads take: 33 x 3000 keys, 8 heads, 28 us and 5 for the
+// pieces, 3.4 TB/s (spans for three workgroups per CU; compiled for four, with 7 registers of 128 spilled); 48 x 4 tokens under a window of 1024, heads of 64, 17 us.  (The 16-bit cache takes 69 us for 33 x 3000, four times the bytes.)
 #include <algorithm>
 
 #include "paged4.h"
